@@ -66,7 +66,8 @@ typedef enum {
   THK_OP_DECODE = 1, /* thk_decode_attn                 */
   THK_OP_PRUNE = 2,  /* thk_prune                       */
   THK_OP_SCORE_VALUE = 3, /* thk_score_value            */
-  THK_OP_PRUNE_VALUE = 4  /* thk_prune_value            */
+  THK_OP_PRUNE_VALUE = 4, /* thk_prune_value            */
+  THK_OP_DECODE_PAGED = 5 /* thk_decode_attn_paged      */
 } thk_op;
 
 /* Problem statement in the paper's B x S x L x N x D terms (Sec. 1). */
@@ -393,6 +394,98 @@ thk_status thk_cache_append(const thk_shape *shape, const void *k_new, const voi
 thk_status thk_tail_flush(const thk_shape *shape, const int16_t *idx, void *k_pruned,
                           void *k_tail, void *v, void *v_tail, int32_t s_tail,
                           int32_t s_tail_cap, int32_t n_flush, void *stream);
+
+/*
+ * Paged caches: key and value rows in a pool of equal pages, found through a table of page
+ * numbers, for batches whose sequences differ in length -- as they are, or as 4-bit or 8-bit
+ * codes (Appendix "Implementation with quantization": the pruned cache is quantised as it
+ * grows, new tokens wait in a full-width tail until there are enough of them).
+ *
+ * thk_pages describes the pool.  A pool holds, per layer, n_pages pages of page_rows rows of all
+ * KV heads; the same table serves every layer:
+ *   table   [B][max_pages]  int32, device: page numbers, 0 .. n_pages - 1
+ *   pool    thk_paged_pool_bytes() bytes, device, 16-byte aligned; its content is the library's own
+ *           (written by thk_paged_write, read by thk_paged_read and thk_decode_attn_paged)
+ * Row counts are per sequence, on the DEVICE, int32 [B], so that they can change between replays
+ * of a captured graph; the host gives upper bounds.  Counts are clamped to those bounds (and to
+ * zero from below), and a table entry outside the pool stands for no page: its rows are not
+ * written, not read back, and take no part in attention.  Two sequences may share a page if
+ * their index lists agree; writing it through both at once is a race.
+ * int32 arrays need 4-byte alignment only.
+ *
+ * A TILE is 64 rows, and pages hold whole tiles: page_rows is a power of two from 64 to 65536.
+ * Codes (bits = 4 or 8) come in groups: the 64 rows of a tile in one kept key channel (fewer in
+ * a sequence's last tile), and 64 channels (0-63 or 64-127) of one value row.  With
+ * N = 2^bits - 1 and fl() rounding to fp32, a group of elements x has
+ *     m = min x,   s = fl(fl(max x - m) / N) rounded to the element type,
+ *     code of x = min(N, rint(fl(fl(x - m) / s))), ties to even; 0 where s == 0
+ * and a code c stands for m + c s.  m and s are held in the element type.  An element is off by
+ * at most s / 2 (plus, for bf16 caches of 8-bit codes, what rounding s to 8 bits moves the last
+ * code: s / 2).  max x - min x must be finite.
+ */
+typedef struct {
+  int32_t bits;      /* 0: rows in the element type; 4 or 8: codes                      */
+  int32_t page_rows; /* rows of a page: a power of two, 64 .. 65536                     */
+  int32_t max_pages; /* entries of a sequence's row of the table; max_pages * page_rows < 2^31 */
+  int64_t n_pages;   /* pages of one layer's part of the pool, < 2^31                   */
+} thk_pages;
+
+/* Bytes of the pool for all layers of `shape` (L, N_kv, T, dtype are used); 0 if either is invalid. */
+size_t thk_paged_pool_bytes(const thk_shape *shape, const thk_pages *pages);
+
+/*
+ * Stores rows of prompts, or full tails, in the pages: kept channels of the keys, whole values.
+ *   rows 0 .. n_rows[b] - 1 of k, v [L][B][N_kv][src_rows][D]  ->  rows row0[b] .. of sequence b
+ * row0 may be NULL (all zeros).  n_rows is bounded by the smaller of shape->S and src_rows.
+ * Whole tiles are written: row0[b] must be a multiple of 64 (a sequence where it is not, or is
+ * negative, is left alone), and where n_rows[b] is not, the rest of its last tile is zeros, so
+ * a sequence that grows is stored in multiples of 64 rows and its remainder appended to the tail.
+ *   in : k, v, n_rows, row0, idx, table      in/out: pool
+ */
+thk_status thk_paged_write(const thk_shape *shape, const thk_pages *pages, const void *k,
+                           const void *v, int64_t src_rows, const int32_t *n_rows,
+                           const int32_t *row0, const int16_t *idx, const int32_t *table,
+                           void *pool, void *stream);
+
+/*
+ * Reads rows back: rows row0[b] .. row0[b] + n_rows[b] - 1 of sequence b, any row0 >= 0, to rows
+ * 0 .. of k_out [L][B][N_kv][out_rows][ld_keep] (kept channels; columns past T are zeros) and
+ * v_out [L][B][N_kv][out_rows][D], in the element type: m + c s rounded once.  Other rows of the
+ * outputs stay as they are.  Either output may be NULL.  n_rows is bounded by the smaller of
+ * shape->S and out_rows; what was never written there reads as whatever the pool holds.
+ */
+thk_status thk_paged_read(const thk_shape *shape, const thk_pages *pages, const void *pool,
+                          const int32_t *table, const int32_t *row0, const int32_t *n_rows,
+                          void *k_out, void *v_out, int64_t out_rows, void *stream);
+
+/*
+ * thk_tail_append for sequences of different lengths, and for more than one row:
+ *   rows src_row0[b] .. of k_new, v_new [L][B][N_kv][src_rows][D], n_new[b] of them
+ *     ->  rows s_tail[b] .. of k_tail, v_tail [L][B][N_kv][s_tail_cap][D]
+ * src_row0 may be NULL (zeros), n_new may be NULL (one row each).  Rows that the source does not
+ * have or the tail has no room for are left out.  s_tail is not changed: the caller adds n_new.
+ */
+thk_status thk_tail_append_ragged(const thk_shape *shape, const void *k_new, const void *v_new,
+                                  int32_t src_rows, const int32_t *src_row0, const int32_t *n_new,
+                                  void *k_tail, void *v_tail, const int32_t *s_tail,
+                                  int32_t s_tail_cap, void *stream);
+
+/*
+ * thk_decode_attn over a paged cache: s_pages[b] rows in pages (at most shape->S), s_tail[b] rows in
+ * the full-width tail (at most s_tail_cap; s_tail_cap = 0: no tail, and k_tail, v_tail, s_tail are
+ * not looked at).  One softmax over both; a sequence without any row gets zeros.  Rows past the
+ * counts are not used, whatever they hold: rows of the tail are not read, rows of a tile have
+ * weight zero.  fp32 arithmetic: codes enter the matrix cores as whole numbers, what multiplies
+ * them as two (bf16) or three (fp32) bf16 terms.
+ * The pieces of a long sequence (n_split; by shape->S, so that the host need not know the lengths)
+ * are joined in an order fixed by the lengths: repeated calls give identical bits.
+ *   ws : thk_workspace_bytes(shape, THK_OP_DECODE_PAGED) bytes, 16-byte aligned.
+ */
+thk_status thk_decode_attn_paged(const thk_shape *shape, const thk_pages *pages, const void *q,
+                                 const void *pool, const int32_t *table, const int32_t *s_pages,
+                                 const int16_t *idx, const void *k_tail, const void *v_tail,
+                                 const int32_t *s_tail, int32_t s_tail_cap, void *out, void *ws,
+                                 size_t ws_bytes, void *stream);
 
 /*
  * Timing hook for benchmarks: the main kernel of the NEXT call made by this host

@@ -13,7 +13,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libthk.so")
 
 THK_F32, THK_BF16 = 0, 1
-THK_OP_SCORE, THK_OP_DECODE, THK_OP_PRUNE, THK_OP_SCORE_VALUE, THK_OP_PRUNE_VALUE = 0, 1, 2, 3, 4
+THK_OP_SCORE, THK_OP_DECODE, THK_OP_PRUNE, THK_OP_SCORE_VALUE, THK_OP_PRUNE_VALUE, THK_OP_DECODE_PAGED = 0, 1, 2, 3, 4, 5
 
 
 class ThkError(RuntimeError):
@@ -28,6 +28,11 @@ class thk_shape(ctypes.Structure):
                 ("S_obs", ctypes.c_int32), ("T", ctypes.c_int32), ("ld_keep", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("n_split", ctypes.c_int32), ("S_recent", ctypes.c_int32),
                 ("S_cap", ctypes.c_int64)]
+
+
+class thk_pages(ctypes.Structure):
+    _fields_ = [("bits", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("n_pages", ctypes.c_int64)]
 
 
 _lib = None
@@ -101,6 +106,17 @@ def load():
     L.thk_cache_append.argtypes = [sp, vp, vp, vp, vp, i32, i32, vp]
     L.thk_tail_flush.restype = ctypes.c_int
     L.thk_tail_flush.argtypes = [sp, vp, vp, vp, vp, vp, i32, i32, i32, vp]
+    pp = ctypes.POINTER(thk_pages)
+    L.thk_paged_pool_bytes.restype = ctypes.c_size_t
+    L.thk_paged_pool_bytes.argtypes = [sp, pp]
+    L.thk_paged_write.restype = ctypes.c_int
+    L.thk_paged_write.argtypes = [sp, pp, vp, vp, i64, vp, vp, vp, vp, vp, vp]
+    L.thk_paged_read.restype = ctypes.c_int
+    L.thk_paged_read.argtypes = [sp, pp, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.thk_tail_append_ragged.restype = ctypes.c_int
+    L.thk_tail_append_ragged.argtypes = [sp, vp, vp, i32, vp, vp, vp, vp, vp, i32, vp]
+    L.thk_decode_attn_paged.restype = ctypes.c_int
+    L.thk_decode_attn_paged.argtypes = [sp, pp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, ctypes.c_size_t, vp]
     L.thk_bench_stream.restype = ctypes.c_int
     L.thk_bench_stream.argtypes = [i32, vp, vp, ctypes.c_int64, i32, vp]
     L.thk_profile_next.restype = None
@@ -416,6 +432,97 @@ def thk_tail_flush(shape, idx, k_pruned, k_tail, v, v_tail, s_tail, s_tail_cap, 
     _check(load().thk_tail_flush(ctypes.byref(shape), _arg(idx, U * T, "idx", w), _arg(k_pruned, rows * ld, "k_pruned", w),
                                  _arg(k_tail, m, "k_tail", w), _arg(v, rows * D, "v", w), _arg(v_tail, m, "v_tail", w),
                                  s_tail, s_tail_cap, n_flush, _stream(stream)), w)
+
+
+# ---- paged caches: sequences of different lengths, rows found through a table of pages ----
+
+def make_pages(bits, page_rows, max_pages, n_pages):
+    """bits 0 (rows in the element type), 4 or 8; rows of a page; entries of a table row; pages of the pool per layer."""
+    return thk_pages(bits, page_rows, max_pages, n_pages)
+
+
+def thk_paged_pool_bytes(shape, pages):
+    return int(load().thk_paged_pool_bytes(ctypes.byref(shape), ctypes.byref(pages)))
+
+
+class _Tensors:
+    """Checks of a call's tensors: on the current device (their kernels run there), of the type the call reads them as,
+    contiguous, large enough.  Integers (raw addresses) and None pass through."""
+
+    def __init__(self, shape, where):
+        import torch
+        self.torch, self.where = torch, where
+        self.element = {THK_F32: torch.float32, THK_BF16: torch.bfloat16}.get(shape.dtype)
+
+    def address(self, x, n, name, dtype):
+        if x is None or isinstance(x, int):
+            return x
+        if not x.is_cuda or x.get_device() != self.torch.cuda.current_device():
+            raise ValueError(f"{self.where}: {name} must be on the current GPU")
+        if dtype is not None and x.dtype != dtype:
+            raise ValueError(f"{self.where}: {name} must be {dtype}, is {x.dtype}")
+        return _arg(x, n, name, self.where)
+
+    def rows(self, x, n, name):
+        return self.address(x, n, name, self.element)
+
+    def ints(self, x, n, name):
+        return self.address(x, n, name, self.torch.int32)
+
+    def idx(self, x, n):
+        return self.address(x, n, "idx", self.torch.int16)
+
+    def raw(self, x, nbytes, name):
+        if x is None or isinstance(x, int):
+            return x
+        return self.address(x, -(-nbytes // x.element_size()), name, None)
+
+
+def thk_paged_write(shape, pages, k, v, src_rows, n_rows, row0, idx, table, pool, stream=None):
+    w = "thk_paged_write"
+    t = _Tensors(shape, w)
+    U, _, D, _, _, T, _, _, _ = _dims(shape)
+    n = U * src_rows * D
+    _check(load().thk_paged_write(ctypes.byref(shape), ctypes.byref(pages), t.rows(k, n, "k"), t.rows(v, n, "v"), src_rows,
+                                  t.ints(n_rows, shape.B, "n_rows"), t.ints(row0, shape.B, "row0"), t.idx(idx, U * T),
+                                  t.ints(table, shape.B * pages.max_pages, "table"),
+                                  t.raw(pool, thk_paged_pool_bytes(shape, pages), "pool"), _stream(stream)), w)
+
+
+def thk_paged_read(shape, pages, pool, table, row0, n_rows, k_out, v_out, out_rows, stream=None):
+    w = "thk_paged_read"
+    t = _Tensors(shape, w)
+    U, _, D, _, _, _, ld, _, _ = _dims(shape)
+    _check(load().thk_paged_read(ctypes.byref(shape), ctypes.byref(pages), t.raw(pool, thk_paged_pool_bytes(shape, pages), "pool"),
+                                 t.ints(table, shape.B * pages.max_pages, "table"), t.ints(row0, shape.B, "row0"),
+                                 t.ints(n_rows, shape.B, "n_rows"), t.rows(k_out, U * out_rows * ld, "k_out"),
+                                 t.rows(v_out, U * out_rows * D, "v_out"), out_rows, _stream(stream)), w)
+
+
+def thk_tail_append_ragged(shape, k_new, v_new, src_rows, src_row0, n_new, k_tail, v_tail, s_tail, s_tail_cap, stream=None):
+    w = "thk_tail_append_ragged"
+    t = _Tensors(shape, w)
+    U, _, D, _, _, _, _, _, _ = _dims(shape)
+    n, m = U * src_rows * D, U * s_tail_cap * D
+    _check(load().thk_tail_append_ragged(ctypes.byref(shape), t.rows(k_new, n, "k_new"), t.rows(v_new, n, "v_new"), src_rows,
+                                         t.ints(src_row0, shape.B, "src_row0"), t.ints(n_new, shape.B, "n_new"),
+                                         t.rows(k_tail, m, "k_tail"), t.rows(v_tail, m, "v_tail"),
+                                         t.ints(s_tail, shape.B, "s_tail"), s_tail_cap, _stream(stream)), w)
+
+
+def thk_decode_attn_paged(shape, pages, q, pool, table, s_pages, idx, k_tail, v_tail, s_tail, s_tail_cap, out, ws, stream=None):
+    w = "thk_decode_attn_paged"
+    t = _Tensors(shape, w)
+    U, H, D, _, _, T, _, _, _ = _dims(shape)
+    m = U * s_tail_cap * D
+    if s_tail_cap <= 0:   # no tail: the library does not look at its arguments
+        k_tail = v_tail = s_tail = None
+    _check(load().thk_decode_attn_paged(ctypes.byref(shape), ctypes.byref(pages), t.rows(q, H * D, "q"),
+                                        t.raw(pool, thk_paged_pool_bytes(shape, pages), "pool"),
+                                        t.ints(table, shape.B * pages.max_pages, "table"), t.ints(s_pages, shape.B, "s_pages"),
+                                        t.idx(idx, U * T), t.rows(k_tail, m, "k_tail"), t.rows(v_tail, m, "v_tail"),
+                                        t.ints(s_tail, shape.B, "s_tail"), s_tail_cap, t.rows(out, H * D, "out"), *_ws(ws),
+                                        _stream(stream)), w)
 
 
 THK_STREAM_READ, THK_STREAM_COPY, THK_STREAM_WRITE = 0, 1, 2

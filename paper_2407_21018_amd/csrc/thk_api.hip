@@ -10,6 +10,7 @@
 #include <mutex>
 
 #include "thk_internal.h"
+#include "thk_paged.h"
 
 using namespace thk;
 
@@ -695,6 +696,49 @@ size_t prune_value_ws_bytes(const thk_shape *s, int n) {
   return ((a + 15) & ~(size_t)15) + (size_t)units_of(s) * kD * sizeof(float);
 }
 
+// ---- paged caches ----
+bool aligned4(const void *p) { return ((uintptr_t)p & 3u) == 0; }
+constexpr uint64_t kMaxThreads = 0xffffffffull;   // of a launch
+
+thk_status check_pages(const thk_shape *s, const thk_pages *p) {
+  const thk_status st = check_shape(s, false);
+  if (st != THK_OK) return st;
+  if (p == nullptr) return THK_ERR_NULL;
+  if (p->bits != 0 && p->bits != 4 && p->bits != 8) return THK_ERR_UNSUPPORTED;
+  if (p->page_rows < kTile || p->page_rows > 65536 || (p->page_rows & (p->page_rows - 1)) != 0) return THK_ERR_SHAPE;
+  if (p->max_pages < 1 || (int64_t)p->max_pages * p->page_rows > INT32_MAX) return THK_ERR_SHAPE;
+  if (p->n_pages < 1 || p->n_pages > INT32_MAX || s->S > INT32_MAX) return THK_ERR_SHAPE;
+  return THK_OK;
+}
+int64_t paged_rows(const thk_shape *s, const thk_pages *p) { return std::min<int64_t>(s->S, (int64_t)p->max_pages * p->page_rows); }
+
+PagedPool paged_pool(const thk_shape *s, const thk_pages *p, const void *pool, const int32_t *table) {
+  PagedPool a;
+  a.pool = const_cast<void *>(pool);
+  a.table = table;
+  a.n_pages = p->n_pages;
+  a.max_pages = p->max_pages;
+  a.tpp_shift = __builtin_ctz((unsigned)p->page_rows / kTile);
+  a.N_kv = s->N_kv;
+  a.B = s->B;
+  a.lay = paged_layout(s->dtype, p->bits, s->T);
+  return a;
+}
+
+int64_t paged_groups(const thk_shape *s) { return ceil_div(s->N_q / s->N_kv, 16); }
+
+// Pieces of whole tiles; by the length's bound, since the lengths are on the device.
+Split paged_split(const thk_shape *s) {
+  const int64_t tiles = ceil_div(s->S, kTile), blocks = units_of(s) * paged_groups(s);
+  int64_t n = s->n_split;
+  if (n == 0) n = std::min(ceil_div(4 * kCUs, blocks), ceil_div(tiles, 4));
+  const int64_t per = ceil_div(tiles, std::max<int64_t>(n, 1));
+  return {(int)ceil_div(tiles, per), per * kTile};
+}
+size_t paged_ws_bytes(const thk_shape *s, int n_split) {
+  return n_split == 1 ? 16 : (size_t)s->L * s->B * s->N_q * n_split * (kD + 2) * sizeof(float);
+}
+
 size_t score_ws_bytes(const thk_shape *s, int64_t units) {
   return (size_t)units * score_split(s, units).n * kD * sizeof(double);
 }
@@ -754,6 +798,7 @@ int32_t thk_default_split(const thk_shape *s, int32_t op) {
   if (op == THK_OP_DECODE) return decode_split(&t).n;
   if (op == THK_OP_SCORE) return score_split(&t, units_of(&t)).n;
   if (op == THK_OP_PRUNE) return score_split(&t, prune_group_units(&t)).n;
+  if (op == THK_OP_DECODE_PAGED) return t.S <= INT32_MAX ? paged_split(&t).n : 0;
   if (op == THK_OP_SCORE_VALUE || op == THK_OP_PRUNE_VALUE) return (t.S_obs >= 1 && t.S_obs <= t.S) ? value_split(&t).n : 0;
   return 0;
 }
@@ -789,6 +834,8 @@ size_t thk_workspace_bytes(const thk_shape *s, int32_t op) {
       const Split sp = decode_split(s);
       return sp.n == 1 ? 16 : decode_ws_bytes(s, sp.n);
     }
+    case THK_OP_DECODE_PAGED:
+      return s->S <= INT32_MAX ? paged_ws_bytes(s, paged_split(s).n) : 0;
     case THK_OP_SCORE_VALUE:
       if (s->S_obs < 1 || (int64_t)s->S_obs > s->S) return 0;
       return value_ws_bytes(s, value_split(s).n);
@@ -1193,6 +1240,104 @@ thk_status thk_tail_append(const thk_shape *s, const void *k_new, const void *v_
                          s_tail, (hipStream_t)stream)))
     return THK_ERR_HIP;
   return THK_OK;
+}
+
+// ---- paged caches -----------------------------------------------------------------------
+size_t thk_paged_pool_bytes(const thk_shape *s, const thk_pages *p) {
+  if (check_pages(s, p) != THK_OK) return 0;
+  return (size_t)s->L * p->n_pages * s->N_kv * (p->page_rows / kTile) * paged_layout(s->dtype, p->bits, s->T).tile_bytes;
+}
+
+thk_status thk_paged_write(const thk_shape *s, const thk_pages *p, const void *k, const void *v, int64_t src_rows,
+                           const int32_t *n_rows, const int32_t *row0, const int16_t *idx, const int32_t *table,
+                           void *pool, void *stream) {
+  const thk_status st = check_pages(s, p);
+  if (st != THK_OK) return st;
+  if (k == nullptr || v == nullptr || n_rows == nullptr || idx == nullptr || table == nullptr || pool == nullptr) return THK_ERR_NULL;
+  if (src_rows < 1 || src_rows > INT32_MAX) return THK_ERR_SHAPE;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(idx) || !aligned16(pool) || !aligned4(n_rows) || !aligned4(row0) || !aligned4(table))
+    return THK_ERR_ALIGN;
+  PagedWriteArgs a;
+  a.p = paged_pool(s, p, pool, table);
+  a.k = k; a.v = v; a.idx = idx; a.n_rows = n_rows; a.row0 = row0;
+  a.src_rows = src_rows;
+  a.most = std::min(paged_rows(s, p), src_rows);
+  a.units = units_of(s);
+  a.T = s->T;
+  a.tiles = (int32_t)ceil_div(a.most, kTile);
+  if ((uint64_t)a.units * a.tiles * 256 > kMaxThreads) return THK_ERR_SHAPE;
+  return failed(launch_paged_write(s->dtype, p->bits, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
+}
+
+thk_status thk_paged_read(const thk_shape *s, const thk_pages *p, const void *pool, const int32_t *table,
+                          const int32_t *row0, const int32_t *n_rows, void *k_out, void *v_out, int64_t out_rows,
+                          void *stream) {
+  const thk_status st = check_pages(s, p);
+  if (st != THK_OK) return st;
+  if (pool == nullptr || table == nullptr || n_rows == nullptr || (k_out == nullptr && v_out == nullptr)) return THK_ERR_NULL;
+  if (out_rows < 1 || out_rows > INT32_MAX) return THK_ERR_SHAPE;
+  if (!aligned16(pool) || !aligned16(k_out) || !aligned16(v_out) || !aligned4(n_rows) || !aligned4(row0) || !aligned4(table))
+    return THK_ERR_ALIGN;
+  PagedReadArgs a;
+  a.p = paged_pool(s, p, pool, table);
+  a.k_out = k_out; a.v_out = v_out; a.n_rows = n_rows; a.row0 = row0;
+  a.out_rows = out_rows;
+  a.most = std::min(paged_rows(s, p), out_rows);
+  a.units = units_of(s);
+  a.T = s->T; a.ld = ld_of(s);
+  a.tiles = (int32_t)ceil_div(a.most + (row0 != nullptr ? kTile - 1 : 0), kTile);   // rows that begin inside a tile
+  if ((uint64_t)a.units * a.tiles * 256 > kMaxThreads) return THK_ERR_SHAPE;
+  return failed(launch_paged_read(s->dtype, p->bits, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
+}
+
+thk_status thk_tail_append_ragged(const thk_shape *s, const void *k_new, const void *v_new, int32_t src_rows,
+                                  const int32_t *src_row0, const int32_t *n_new, void *k_tail, void *v_tail,
+                                  const int32_t *s_tail, int32_t s_tail_cap, void *stream) {
+  const thk_status st = check_shape(s, false);
+  if (st != THK_OK) return st;
+  if (k_new == nullptr || v_new == nullptr || k_tail == nullptr || v_tail == nullptr || s_tail == nullptr) return THK_ERR_NULL;
+  if (src_rows < 1 || s_tail_cap < 1) return THK_ERR_SHAPE;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_tail) || !aligned16(v_tail) || !aligned4(s_tail) ||
+      !aligned4(src_row0) || !aligned4(n_new))
+    return THK_ERR_ALIGN;
+  RaggedAppendArgs a;
+  a.k_new = k_new; a.v_new = v_new; a.k_tail = k_tail; a.v_tail = v_tail;
+  a.src_row0 = src_row0; a.n_new = n_new; a.s_tail = s_tail;
+  a.units = units_of(s);
+  a.N_kv = s->N_kv; a.B = s->B; a.src_rows = src_rows; a.cap = s_tail_cap;
+  a.rows = n_new != nullptr ? std::min(src_rows, s_tail_cap) : 1;
+  if ((uint64_t)a.units * a.rows > kMaxThreads / 32 - 8) return THK_ERR_SHAPE;   // up to 32 threads a row
+  return failed(launch_append_ragged(s->dtype, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
+}
+
+thk_status thk_decode_attn_paged(const thk_shape *s, const thk_pages *p, const void *q, const void *pool,
+                                 const int32_t *table, const int32_t *s_pages, const int16_t *idx, const void *k_tail,
+                                 const void *v_tail, const int32_t *s_tail, int32_t s_tail_cap, void *out, void *ws,
+                                 size_t ws_bytes, void *stream) {
+  const thk_status st = check_pages(s, p);
+  if (st != THK_OK) return st;
+  if (q == nullptr || pool == nullptr || table == nullptr || s_pages == nullptr || idx == nullptr || out == nullptr) return THK_ERR_NULL;
+  if (s_tail_cap < 0) return THK_ERR_SHAPE;
+  const bool tail = s_tail_cap > 0;
+  if (tail && (k_tail == nullptr || v_tail == nullptr || s_tail == nullptr)) return THK_ERR_NULL;
+  if (!aligned16(q) || !aligned16(pool) || !aligned16(idx) || !aligned16(out) || !aligned4(table) || !aligned4(s_pages) ||
+      (tail && (!aligned16(k_tail) || !aligned16(v_tail) || !aligned4(s_tail))))
+    return THK_ERR_ALIGN;
+  const Split sp = paged_split(s);
+  if (sp.n > 1 && (ws == nullptr || !aligned16(ws) || ws_bytes < paged_ws_bytes(s, sp.n))) return THK_ERR_WORKSPACE;
+  PagedDecodeArgs a;
+  a.p = paged_pool(s, p, pool, table);
+  a.q = q; a.idx = idx; a.s_pages = s_pages; a.out = out; a.ws = (float *)ws;
+  a.kt = tail ? k_tail : nullptr; a.vt = tail ? v_tail : nullptr; a.s_tail = tail ? s_tail : nullptr;
+  a.S = paged_rows(s, p);
+  a.units = units_of(s);
+  a.T = s->T; a.G = s->N_q / s->N_kv; a.cap = s_tail_cap;
+  a.n_split = sp.n;
+  a.tiles_per_split = (int32_t)(sp.rows / kTile);
+  a.groups = (int32_t)paged_groups(s);
+  a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)s->D));
+  if ((uint64_t)a.units * a.groups > kMaxThreads / 256 / sp.n || (uint64_t)a.units * a.G > kMaxThreads / 256) return THK_ERR_SHAPE;
+  return failed(launch_paged_decode(s->dtype, p->bits, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
 }
 
 }  // extern "C"

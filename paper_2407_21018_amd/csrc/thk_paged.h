@@ -1,0 +1,117 @@
+// The paged cache: where a tile's codes and parameters lie, and the launchers' arguments.
+//
+// A tile is 64 rows of one unit.  Its bytes, in this order: key codes, value codes, key parameters, value parameters (the
+// last two only with codes).  Codes come in units of eight -- eight kept channels of one row for keys, eight rows of one
+// channel for values -- which is what one lane hands to a 16x16x32 matrix instruction as its share of an operand, so that a
+// lane's loads are its operands and no data crosses lanes or LDS between memory and the matrix cores.  64 units form a group:
+//   keys:   group c = channels 8 c .. 8 c + 7; its unit (j, m) is row 16 j + m;
+//   values: group (g, h, half) = rows {32 g + 16 x + 4 h + r}, element 4 x + r of a unit; its unit (j, m) is channel
+//           64 half + 4 m + j.  (The rows are those whose logits a lane of quarter h holds after the first product.)
+// Inside a group the units lie so that lane m finds its four (j = 0..3) in 16-byte cells that are contiguous over the 16
+// lanes: cell k of lane m is at (16 k + m) * 16.
+//   unit of 4 bytes (4-bit codes):  cell 0 = j 0..3
+//   unit of 8 bytes (8-bit codes):  cell k = j 2 k, 2 k + 1
+//   unit of 16 bytes (bf16):        cell k = j k
+//   unit of 32 bytes (fp32):        cells 2 j, 2 j + 1
+// 4-bit units hold code 2 p at bits 4 p and code 2 p + 1 at bits 16 + 4 p: two neighbours are one shift and one mask away
+// from the two halves of a word.
+// A parameter is a pair (scale, minimum) of the element type; the pairs of a group's eight channels (keys) or rows (values)
+// lie together, groups in order.
+#pragma once
+#include "thk_internal.h"
+
+namespace thk {
+
+constexpr int kTile = 64;          // rows of a tile
+constexpr int kValueGroups = 16;   // groups of a tile's values: 2 x 4 row octets, 2 halves of the channels
+
+struct PagedLayout {
+  int32_t chunks;      // groups of a tile's keys: T / 8, rounded up
+  int32_t unit_bytes;
+  int32_t v_codes;     // byte offsets from the tile's start
+  int32_t k_params, v_params;
+  int32_t tile_bytes;
+};
+inline PagedLayout paged_layout(int dtype, int bits, int T) {
+  const int e = dtype == THK_BF16 ? 2 : 4;
+  PagedLayout p;
+  p.chunks = (T + 7) / 8;
+  p.unit_bytes = bits != 0 ? bits : 8 * e;
+  p.v_codes = p.chunks * 64 * p.unit_bytes;
+  p.k_params = p.v_codes + kValueGroups * 64 * p.unit_bytes;
+  p.v_params = p.k_params + (bits != 0 ? p.chunks * 8 * 2 * e : 0);
+  p.tile_bytes = p.v_params + (bits != 0 ? kValueGroups * 8 * 2 * e : 0);
+  return p;
+}
+
+// The pool and the tables of a call.
+struct PagedPool {
+  void *pool;
+  const int32_t *table;    // [B][max_pages]
+  int64_t n_pages;         // pages of one layer's part of the pool
+  int32_t max_pages;
+  int32_t tpp_shift;       // log2 of the tiles of a page
+  int32_t N_kv, B;
+  PagedLayout lay;
+
+  // Tile `tile` of sequence b's KV head h in layer l; nullptr where the table has no page of the pool for it.
+  __device__ __forceinline__ char *tile(int64_t l, int b, int h, int64_t tile) const {
+    const int64_t slot = tile >> tpp_shift;
+    if (slot >= max_pages) return nullptr;
+    return in_page(l, h, table[(int64_t)b * max_pages + slot], (int)(tile & ((1 << tpp_shift) - 1)));
+  }
+  __device__ __forceinline__ char *in_page(int64_t l, int h, int page, int t) const {
+    if (page < 0 || page >= n_pages) return nullptr;
+    return (char *)pool + ((((l * n_pages + page) * N_kv + h) << tpp_shift) + t) * (int64_t)lay.tile_bytes;
+  }
+};
+
+struct PagedWriteArgs {
+  PagedPool p;
+  const void *k, *v;
+  const int16_t *idx;
+  const int32_t *n_rows, *row0;   // [B]; row0 may be nullptr (0)
+  int64_t src_rows;               // rows per unit of k and v
+  int64_t most;                   // most rows of a sequence in this call
+  int64_t units;
+  int32_t T, tiles;               // tiles: blocks per unit, those of `most` rows
+};
+hipError_t launch_paged_write(int dtype, int bits, const PagedWriteArgs &a, hipStream_t st);
+
+struct PagedReadArgs {
+  PagedPool p;
+  void *k_out, *v_out;            // either may be nullptr
+  const int32_t *n_rows, *row0;   // [B]; row0 may be nullptr (0)
+  int64_t out_rows;               // rows per unit of the outputs
+  int64_t most;                   // most rows of a sequence in this call
+  int64_t units;
+  int32_t T, ld, tiles;           // tiles: blocks per unit
+};
+hipError_t launch_paged_read(int dtype, int bits, const PagedReadArgs &a, hipStream_t st);
+
+struct RaggedAppendArgs {
+  const void *k_new, *v_new;
+  void *k_tail, *v_tail;
+  const int32_t *src_row0, *n_new, *s_tail;   // [B]; src_row0 and n_new may be nullptr (0, 1)
+  int64_t units;
+  int32_t N_kv, B, src_rows, cap, rows;       // rows: most rows of a sequence in this call
+};
+hipError_t launch_append_ragged(int dtype, const RaggedAppendArgs &a, hipStream_t st);
+
+struct PagedDecodeArgs {
+  PagedPool p;
+  const void *q, *kt, *vt;
+  const int16_t *idx;
+  const int32_t *s_pages, *s_tail;   // [B]; s_tail may be nullptr (no tail)
+  void *out;
+  float *ws;                         // split records [head][n_split]: (max, sum, acc[128])
+  int64_t S;                         // most rows of a sequence in pages
+  int64_t units;
+  int32_t T, G, cap, n_split, tiles_per_split, groups;   // groups: blocks of 16 query heads per unit
+  float scale_log2;
+};
+hipError_t launch_paged_decode(int dtype, int bits, const PagedDecodeArgs &a, hipStream_t st);
+hipError_t launch_paged_decode_bf16(int bits, const PagedDecodeArgs &a, hipStream_t st);
+hipError_t launch_paged_decode_f32(int bits, const PagedDecodeArgs &a, hipStream_t st);
+
+}  // namespace thk

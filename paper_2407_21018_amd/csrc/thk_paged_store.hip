@@ -1,0 +1,331 @@
+// The paged cache's rows: written (compacted, and quantised where the pages hold codes), read back, and appended to the
+// ragged tails.  Memory bounds all three: every row is read once and written once.
+#include "thk_paged.h"
+
+namespace thk {
+namespace {
+
+// The lanes m = 0..15 of a group form a row of the wave's data paths, so a reduction over them is four rotations.
+template <int N>
+__device__ __forceinline__ float ror16(float x) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x120 + N, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float min16(float x) {
+  x = fminf(x, ror16<8>(x)); x = fminf(x, ror16<4>(x)); x = fminf(x, ror16<2>(x));
+  return fminf(x, ror16<1>(x));
+}
+__device__ __forceinline__ float max16(float x) {
+  x = fmaxf(x, ror16<8>(x)); x = fmaxf(x, ror16<4>(x)); x = fmaxf(x, ror16<2>(x));
+  return fmaxf(x, ror16<1>(x));
+}
+
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  return (uint32_t)Elem<THK_BF16>::round_bf16(a) | ((uint32_t)Elem<THK_BF16>::round_bf16(b) << 16);
+}
+
+// Scale of a group with extremes lo, hi: its range over the number of steps, held in the element type.
+template <int DT, int BITS>
+__device__ __forceinline__ float group_scale(float lo, float hi) {
+  const float s = (hi - lo) / (float)((1 << BITS) - 1);
+  if constexpr (DT == THK_BF16) return __uint_as_float((uint32_t)Elem<THK_BF16>::round_bf16(s) << 16);
+  return s;
+}
+
+// x[j][e], j = 0..3, e = 0..7: this lane's 32 elements of a group (unit j, element e).  Element e of all the group's units
+// shares a scale.  ok[j] = false: unit j is written as zeros.  dst: the group's first byte; par: its eight parameters.
+template <int DT, int BITS>
+__device__ __forceinline__ void encode_group(const float (&x)[4][8], const bool (&ok)[4], char *dst, char *par, int m) {
+  if constexpr (BITS == 0) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (DT == THK_BF16) {
+        u32x4 u;
+#pragma unroll
+        for (int p = 0; p < 4; ++p)   // the elements are bf16 values: their upper halves are all there is
+          u[p] = ok[j] ? (__float_as_uint(x[j][2 * p]) >> 16) | (__float_as_uint(x[j][2 * p + 1]) & 0xffff0000u) : 0u;
+        st_stream((u32x4 *)(dst + (j * 16 + m) * 16), u);
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u32x4 u;
+#pragma unroll
+          for (int p = 0; p < 4; ++p) u[p] = ok[j] ? __float_as_uint(x[j][4 * h + p]) : 0u;
+          st_stream((u32x4 *)(dst + ((2 * j + h) * 16 + m) * 16), u);
+        }
+      }
+    }
+    return;
+  }
+  constexpr float top = (float)((1 << BITS) - 1);
+  uint32_t code[4][8];
+  uint32_t pair_lo = 0, pair_hi = 0;   // this lane's parameter pair, element m & 7
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float lo = min16(fminf(fminf(x[0][e], x[1][e]), fminf(x[2][e], x[3][e])));
+    const float hi = max16(fmaxf(fmaxf(x[0][e], x[1][e]), fmaxf(x[2][e], x[3][e])));
+    const float s = group_scale<DT, BITS>(lo, hi);
+    const float d = s > 0.f ? s : 1.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float c = fminf(rintf((x[j][e] - lo) / d), top);
+      code[j][e] = s > 0.f && ok[j] ? (uint32_t)c : 0u;
+    }
+    if ((m & 7) == e) {
+      pair_lo = __float_as_uint(s);
+      pair_hi = __float_as_uint(lo);
+    }
+  }
+  if (m < 8) {
+    if constexpr (DT == THK_BF16) *(uint32_t *)(par + m * 4) = (pair_lo >> 16) | (pair_hi & 0xffff0000u);
+    else *(uint2 *)(par + m * 8) = make_uint2(pair_lo, pair_hi);
+  }
+  if constexpr (BITS == 4) {
+    u32x4 u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      u[j] = 0;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) u[j] |= (code[j][2 * p] << (4 * p)) | (code[j][2 * p + 1] << (16 + 4 * p));
+    }
+    st_stream((u32x4 *)(dst + m * 16), u);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      u32x4 u;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int j = 2 * k + (w >> 1), e = 4 * (w & 1);
+        u[w] = code[j][e] | (code[j][e + 1] << 8) | (code[j][e + 2] << 16) | (code[j][e + 3] << 24);
+      }
+      st_stream((u32x4 *)(dst + (k * 16 + m) * 16), u);
+    }
+  }
+}
+
+// One block per (unit, tile of the call).  Keys go through LDS, where their kept channels are picked; values go straight
+// from memory to the lane that encodes them.
+template <int DT, int BITS>
+__global__ __launch_bounds__(256) void k_paged_write(PagedWriteArgs a) {
+  using E = Elem<DT>;
+  constexpr int EB = E::EB, PITCH = kD * EB + 16;
+  __shared__ __align__(16) char rows_lds[kTile * PITCH];
+  __shared__ int16_t idx_lds[kD];
+  const int tid = threadIdx.x, m = tid & 15, grp = tid >> 4;
+  const int64_t u = blockIdx.x / (uint32_t)a.tiles;
+  const int t = blockIdx.x % (uint32_t)a.tiles;
+  const int h = (int)(u % a.p.N_kv), b = (int)(u / a.p.N_kv % a.p.B);
+  const int64_t l = u / a.p.N_kv / a.p.B;
+  const int64_t n = min((int64_t)a.n_rows[b], a.most);
+  const int64_t row0 = a.row0 != nullptr ? a.row0[b] : 0;
+  const int64_t r0 = (int64_t)t * kTile;
+  if (r0 >= n || row0 < 0 || (row0 & (kTile - 1)) != 0) return;
+  char *const dst = a.p.tile(l, b, h, row0 / kTile + t);
+  if (dst == nullptr) return;
+  const int rows = (int)min(n - r0, (int64_t)kTile);
+  const size_t base = ((size_t)u * a.src_rows + r0) * kD;   // first element of the tile's rows
+
+  // values: lane m of group (g, q, half) takes channels 64 half + 4 m .. + 3 of its eight rows
+  float xv[4][8];
+  {
+    const int half = grp & 1, q = (grp >> 1) & 3, g = grp >> 3;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int r = 32 * g + 16 * (e >> 2) + 4 * q + (e & 3);
+      const size_t at = base + (size_t)min(r, rows - 1) * kD + 64 * half + 4 * m;
+      if constexpr (DT == THK_BF16) {
+        const uint2 w = *(const uint2 *)((const uint16_t *)a.v + at);
+        xv[0][e] = __uint_as_float(w.x << 16); xv[1][e] = __uint_as_float(w.x & 0xffff0000u);
+        xv[2][e] = __uint_as_float(w.y << 16); xv[3][e] = __uint_as_float(w.y & 0xffff0000u);
+      } else {
+        const float4 w = *(const float4 *)((const float *)a.v + at);
+        xv[0][e] = w.x; xv[1][e] = w.y; xv[2][e] = w.z; xv[3][e] = w.w;
+      }
+      if (r >= rows) xv[0][e] = xv[1][e] = xv[2][e] = xv[3][e] = 0.f;   // a group of zeros: codes and parameters are zero
+    }
+  }
+  constexpr int CPR = kD * EB / 16;   // 16-byte pieces of a row
+  for (int i = tid; i < rows * CPR; i += 256) {
+    const int r = i / CPR, c = i % CPR;
+    *(u32x4 *)(rows_lds + r * PITCH + c * 16) = ld_stream((const u32x4 *)((const char *)a.k + base * EB) + i);
+  }
+  if (tid < kD) idx_lds[tid] = tid < a.T ? a.idx[(size_t)u * a.T + tid] & (kD - 1) : 0;
+  const bool all[4] = {true, true, true, true};
+  encode_group<DT, BITS>(xv, all, dst + a.p.lay.v_codes + grp * 64 * a.p.lay.unit_bytes,
+                         dst + a.p.lay.v_params + grp * 8 * 2 * EB, m);
+  __syncthreads();
+  if (grp >= a.p.lay.chunks) return;
+  float xk[4][8];
+  bool ok[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int r = 16 * j + m;
+    ok[j] = r < rows;
+    const char *const src = rows_lds + min(r, rows - 1) * PITCH;   // a row outside repeats one inside: the extremes stay
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int c = 8 * grp + e;
+      xk[j][e] = c < a.T ? E::load1(src, idx_lds[c]) : 0.f;
+    }
+  }
+  encode_group<DT, BITS>(xk, ok, dst + grp * 64 * a.p.lay.unit_bytes, dst + a.p.lay.k_params + grp * 8 * 2 * EB, m);
+}
+
+// The inverse of encode_group: what the lane's 32 codes stand for, rounded once to the element type.
+template <int DT, int BITS>
+__device__ __forceinline__ void decode_group(const char *src, const char *par, int m, float (&x)[4][8]) {
+  constexpr int UB = BITS != 0 ? BITS : DT == THK_BF16 ? 16 : 32;
+  u32x4 w[UB / 4];
+#pragma unroll
+  for (int k = 0; k < UB / 4; ++k) w[k] = ld_stream((const u32x4 *)(src + (k * 16 + m) * 16));
+  if constexpr (BITS == 0) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (DT == THK_BF16) {
+        Elem<DT>::unpack(w[j], x[j]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[j][e] = __uint_as_float(w[2 * j + (e >> 2)][e & 3]);
+      }
+    }
+    return;
+  }
+  float s[8], lo[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if constexpr (DT == THK_BF16) {
+      const uint32_t p = ((const uint32_t *)par)[e];
+      s[e] = __uint_as_float(p << 16);
+      lo[e] = __uint_as_float(p & 0xffff0000u);
+    } else {
+      const float2 p = ((const float2 *)par)[e];
+      s[e] = p.x;
+      lo[e] = p.y;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      uint32_t c;
+      if constexpr (BITS == 4) c = (w[0][j] >> (4 * (e >> 1) + 16 * (e & 1))) & 15u;
+      else c = (w[j >> 1][2 * (j & 1) + (e >> 2)] >> (8 * (e & 3))) & 255u;
+      x[j][e] = fmaf((float)c, s[e], lo[e]);
+    }
+}
+
+// One block per (unit, tile that holds rows of the call).
+template <int DT, int BITS>
+__global__ __launch_bounds__(256) void k_paged_read(PagedReadArgs a) {
+  using E = Elem<DT>;
+  constexpr int EB = E::EB;
+  __shared__ __align__(16) char rows_lds[16 + kTile * kD * EB];
+  const int tid = threadIdx.x, m = tid & 15, grp = tid >> 4;
+  const int64_t u = blockIdx.x / (uint32_t)a.tiles;
+  const int h = (int)(u % a.p.N_kv), b = (int)(u / a.p.N_kv % a.p.B);
+  const int64_t l = u / a.p.N_kv / a.p.B;
+  const int64_t row0 = a.row0 != nullptr ? a.row0[b] : 0;
+  if (row0 < 0) return;
+  const int64_t end = row0 + min((int64_t)a.n_rows[b], a.most);
+  const int64_t t = row0 / kTile + blockIdx.x % (uint32_t)a.tiles;
+  const int64_t lo = max(row0, t * kTile), hi = min(end, (t + 1) * kTile);   // rows of this block
+  if (lo >= hi) return;
+  const char *const src = a.p.tile(l, b, h, t);
+  if (src == nullptr) return;
+  const size_t out_row = (size_t)u * a.out_rows + (lo - row0);
+  const int first = (int)(lo - t * kTile), rows = (int)(hi - lo);
+  float x[4][8];
+  if (a.v_out != nullptr) {
+    const int half = grp & 1, q = (grp >> 1) & 3, g = grp >> 3;
+    decode_group<DT, BITS>(src + a.p.lay.v_codes + grp * 64 * a.p.lay.unit_bytes, src + a.p.lay.v_params + grp * 8 * 2 * EB, m, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int r = 32 * g + 16 * (e >> 2) + 4 * q + (e & 3) - first;
+      if (r < 0 || r >= rows) continue;
+      const size_t at = (out_row + r) * kD + 64 * half + 4 * m;
+      if constexpr (DT == THK_BF16) *(uint2 *)((uint16_t *)a.v_out + at) = make_uint2(bf16_pair(x[0][e], x[1][e]), bf16_pair(x[2][e], x[3][e]));
+      else *(float4 *)((float *)a.v_out + at) = make_float4(x[0][e], x[1][e], x[2][e], x[3][e]);
+    }
+  }
+  if (a.k_out == nullptr) return;
+  // The block's key rows are one run of the output.  They are put together in LDS at the output's offset from a 16-byte
+  // boundary, so that whole aligned 16-byte pieces can be stored; the two ends go element by element.
+  char *const dst = (char *)a.k_out + out_row * a.ld * EB;
+  const int skew = (int)((uintptr_t)dst & 15);
+  if (a.ld > a.T)
+    for (int i = tid; i < rows * (a.ld - a.T); i += 256) {
+      const int r = i / (a.ld - a.T), c = a.T + i % (a.ld - a.T);
+      E::store1(rows_lds + skew, r * a.ld + c, 0.f);
+    }
+  if (grp < a.p.lay.chunks) {
+    decode_group<DT, BITS>(src + grp * 64 * a.p.lay.unit_bytes, src + a.p.lay.k_params + grp * 8 * 2 * EB, m, x);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = 16 * j + m - first;
+      if (r < 0 || r >= rows) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (8 * grp + e < a.T) E::store1(rows_lds + skew, r * a.ld + 8 * grp + e, x[j][e]);
+    }
+  }
+  __syncthreads();
+  const int bytes = rows * a.ld * EB;
+  const int lead = min((16 - skew) & 15, bytes), whole = (bytes - lead) / 16;
+  for (int i = tid; i < whole; i += 256)
+    st_stream((u32x4 *)(dst + lead) + i, ((const u32x4 *)(rows_lds + skew + lead))[i]);
+  const int rest = bytes - whole * 16;   // of both ends, in bytes
+  for (int i = tid; i < rest / EB; i += 256) {
+    const int at = i * EB < lead ? i * EB : i * EB + whole * 16;
+    *(typename E::Bits *)(dst + at) = *(const typename E::Bits *)(rows_lds + skew + at);
+  }
+}
+
+// One thread per 16-byte piece of a row.
+template <int DT>
+__global__ __launch_bounds__(256) void k_append_ragged(RaggedAppendArgs a) {
+  constexpr int CPR = kD * Elem<DT>::EB / 16;
+  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int c = (int)(i % CPR);
+  i /= CPR;
+  const int r = (int)(i % a.rows);
+  const int64_t u = i / a.rows;
+  if (u >= a.units) return;
+  const int b = (int)(u / a.N_kv % a.B);
+  const int64_t src = (a.src_row0 != nullptr ? (int64_t)a.src_row0[b] : 0) + r;
+  const int64_t dst = (int64_t)a.s_tail[b] + r;
+  if (r >= (a.n_new != nullptr ? a.n_new[b] : 1) || src < 0 || src >= a.src_rows || dst < 0 || dst >= a.cap) return;
+  const int64_t from = (u * a.src_rows + src) * CPR + c, to = (u * a.cap + dst) * CPR + c;
+  ((u32x4 *)a.k_tail)[to] = ((const u32x4 *)a.k_new)[from];
+  ((u32x4 *)a.v_tail)[to] = ((const u32x4 *)a.v_new)[from];
+}
+
+template <class A>
+hipError_t launch(void (*k)(A), const A &a, int64_t blocks, hipStream_t st) {
+  clear_stale_hip_error();
+  A copy = a;
+  void *args[] = {&copy};
+  return launch_main_kernel((const void *)k, dim3((unsigned)blocks), dim3(256), args, 0, st);
+}
+
+}  // namespace
+
+hipError_t launch_paged_write(int dtype, int bits, const PagedWriteArgs &a, hipStream_t st) {
+  const bool f32 = dtype == THK_F32;
+  return launch(bits == 0   ? (f32 ? k_paged_write<THK_F32, 0> : k_paged_write<THK_BF16, 0>)
+                : bits == 4 ? (f32 ? k_paged_write<THK_F32, 4> : k_paged_write<THK_BF16, 4>)
+                            : (f32 ? k_paged_write<THK_F32, 8> : k_paged_write<THK_BF16, 8>), a, a.units * a.tiles, st);
+}
+hipError_t launch_paged_read(int dtype, int bits, const PagedReadArgs &a, hipStream_t st) {
+  const bool f32 = dtype == THK_F32;
+  return launch(bits == 0   ? (f32 ? k_paged_read<THK_F32, 0> : k_paged_read<THK_BF16, 0>)
+                : bits == 4 ? (f32 ? k_paged_read<THK_F32, 4> : k_paged_read<THK_BF16, 4>)
+                            : (f32 ? k_paged_read<THK_F32, 8> : k_paged_read<THK_BF16, 8>), a, a.units * a.tiles, st);
+}
+hipError_t launch_paged_decode(int dtype, int bits, const PagedDecodeArgs &a, hipStream_t st) {
+  return dtype == THK_F32 ? launch_paged_decode_f32(bits, a, st) : launch_paged_decode_bf16(bits, a, st);
+}
+hipError_t launch_append_ragged(int dtype, const RaggedAppendArgs &a, hipStream_t st) {
+  const int64_t pieces = a.units * a.rows * (dtype == THK_F32 ? 32 : 16);
+  return launch(dtype == THK_F32 ? k_append_ragged<THK_F32> : k_append_ragged<THK_BF16>, a, (pieces + 255) / 256, st);
+}
+
+}  // namespace thk

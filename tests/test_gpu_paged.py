@@ -1,0 +1,451 @@
+"""Paged, ragged, quantised caches on the GPU against fp64 (oracle/paged.py): stored and read back, appended, attended over.
+
+Everything a call must not use holds NaN: the pool before it is written, source rows past a sequence's count, tail rows
+past theirs, outputs before the call.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2407_21018_amd as thk
+from oracle import paged as P
+from helpers import DT, TDT, ws_tensor
+
+pytestmark = pytest.mark.gpu
+D = 128
+HALF_STEP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}   # of the value, when it is rounded once
+
+
+def _ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _np(t):
+    return t.detach().cpu().double().numpy()
+
+
+class Cache:
+    """A ragged batch: sources, index lists, pages in no order, tails; and the same on the host."""
+
+    def __init__(self, dtype, bits, L, B, N_kv, G, T, rows, page_rows=64, tails=None, cap=0, seed=0, S=None, spare=2, n_split=0):
+        g = torch.Generator(device="cuda"); g.manual_seed(9000 + seed)
+        self.dtype, self.bits, self.L, self.B, self.N_kv, self.G, self.T = dtype, bits, L, B, N_kv, G, T
+        self.rows, self.tails, self.cap, self.page_rows = list(rows), list(tails or [0] * B), cap, page_rows
+        self.S = S or max(max(rows), 1)
+        self.g, self.U = g, L * B * N_kv
+        rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+        scale, off = torch.exp(rnd(L, 1, N_kv, 1, D)), rnd(L, 1, N_kv, 1, D)
+        self.k = (rnd(L, B, N_kv, self.S, D) * scale + off * scale).to(TDT[dtype])
+        self.v = (rnd(L, B, N_kv, self.S, D) + 0.3 * rnd(L, 1, N_kv, 1, D)).to(TDT[dtype])
+        for b, n in enumerate(self.rows):
+            self.k[:, b, :, n:] = float("nan")
+            self.v[:, b, :, n:] = float("inf")
+        self.q = (rnd(L, B, N_kv * G, D) / scale[:, :, :, 0].repeat_interleave(G, 2)).to(TDT[dtype])
+        self.idx = torch.rand(L, B, N_kv, D, generator=g, device="cuda").argsort(-1)[..., :T].sort(-1).values.to(torch.int16).contiguous()
+        self.kt = (rnd(L, B, N_kv, max(cap, 1), D) * scale + off * scale).to(TDT[dtype])
+        self.vt = rnd(L, B, N_kv, max(cap, 1), D).to(TDT[dtype])
+        for b, n in enumerate(self.tails):
+            self.kt[:, b, :, n:] = float("nan")
+            self.vt[:, b, :, n:] = float("nan")
+        need = [-(-n // page_rows) for n in self.rows]
+        order = torch.randperm(sum(need) + spare, generator=g, device="cuda").cpu().numpy()
+        self.max_pages = max(max(need), 1)
+        table = np.full((B, self.max_pages), -1, np.int32)
+        at = 0
+        for b, n in enumerate(need):
+            table[b, :n] = order[at:at + n]
+            at += n
+        self.table = torch.from_numpy(table).cuda()
+        self.shape = thk.make_shape(L, B, N_kv * G, N_kv, D, self.S, 1, T, 0, DT[dtype], n_split)
+        self.pages = thk.make_pages(bits, page_rows, self.max_pages, sum(need) + spare)
+        self.pool = torch.full((thk.thk_paged_pool_bytes(self.shape, self.pages),), 255, dtype=torch.uint8, device="cuda")
+        self.s_pages, self.s_tail = _ints(self.rows), _ints(self.tails)
+
+    def write(self, stream=None):
+        thk.thk_paged_write(self.shape, self.pages, self.k, self.v, self.S, self.s_pages, None, self.idx, self.table, self.pool, stream)
+
+    def decode(self, out=None, ws=None, stream=None, shape=None):
+        shape = shape or self.shape
+        if out is None:
+            out = torch.full_like(self.q, float("nan"))
+        if ws is None:
+            ws = ws_tensor(thk.thk_workspace_bytes(shape, thk.THK_OP_DECODE_PAGED))
+        tail = (self.kt, self.vt, self.s_tail, self.cap) if self.cap else (None, None, None, 0)
+        thk.thk_decode_attn_paged(shape, self.pages, self.q, self.pool, self.table, self.s_pages, self.idx, *tail, out, ws, stream)
+        return out
+
+    def unit(self, l, b, h):
+        """(kept rows, value rows) of a unit as stored, fp64; (tail rows); index list."""
+        n, t, idx = self.rows[b], self.tails[b], _np(self.idx[l, b, h]).astype(int)
+        k, v = P.stored(_np(self.k[l, b, h, :n])[:, idx], _np(self.v[l, b, h, :n]), self.bits, self.dtype)
+        return k, v, _np(self.kt[l, b, h, :t]), _np(self.vt[l, b, h, :t]), idx
+
+
+# (L, B, N_kv, G, T, rows, page_rows, S): lengths around a tile and a page, none, odd channel counts, several layers
+STORE = [
+    (1, 1, 1, 1, 64, [1], 64, None), (1, 1, 2, 1, 51, [64], 64, None), (1, 3, 2, 1, 76, [65, 0, 63], 64, None),
+    (2, 2, 3, 1, 128, [200, 129], 128, None), (1, 4, 1, 2, 1, [500, 64, 1, 257], 256, None), (3, 2, 1, 1, 97, [130, 191], 64, None),
+    (1, 1, 8, 4, 8, [1000], 512, None), (1, 2, 2, 1, 33, [70, 10], 64, 90),
+]
+
+
+@pytest.mark.parametrize("case", STORE, ids=[str(i) for i in range(len(STORE))])
+@pytest.mark.parametrize("bits", [0, 4, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_come_back_as_what_they_were_stored_as(dtype, bits, case):
+    L, B, N_kv, G, T, rows, page_rows, S = case
+    print("store", dtype, bits, case, flush=True)
+    c = Cache(dtype, bits, L, B, N_kv, G, T, rows, page_rows, seed=T, S=S)
+    c.write()
+    for ld in (T, min(D, T + 5)):
+        c.shape.ld_keep = ld
+        out_rows = c.S + 3
+        ko = torch.full((L, B, N_kv, out_rows, ld), 7.0, dtype=TDT[dtype], device="cuda")
+        vo = torch.full((L, B, N_kv, out_rows, D), 7.0, dtype=TDT[dtype], device="cuda")
+        thk.thk_paged_read(c.shape, c.pages, c.pool, c.table, None, c.s_pages, ko, vo, out_rows)
+        torch.cuda.synchronize()
+        for l in range(L):
+            for b in range(B):
+                for h in range(N_kv):
+                    n = rows[b]
+                    k, v, _, _, _ = c.unit(l, b, h)
+                    for got, want in ((_np(ko[l, b, h])[:n, :T], k), (_np(vo[l, b, h])[:n], v)):
+                        assert np.all(np.abs(got - want) <= (0 if bits == 0 else HALF_STEP[dtype]) * np.abs(want))
+                    assert not _np(ko[l, b, h])[:n, T:].any()                      # the columns past T are zeros
+        for b in range(B):
+            assert torch.all(ko[:, b, :, rows[b]:] == 7) and torch.all(vo[:, b, :, rows[b]:] == 7)   # the rest as it was
+
+
+@pytest.mark.parametrize("bits", [0, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_any_range_of_rows_is_read(dtype, bits):
+    c = Cache(dtype, bits, 1, 3, 2, 1, 51, [300, 129, 64], 128, seed=3)
+    c.write()
+    for row0, n in (([0, 0, 0], [300, 129, 64]), ([1, 63, 64], [299, 66, 0]), ([65, 128, 10], [64, 1, 1]), ([255, 100, 63], [45, 29, 1])):
+        ko = torch.full((1, 3, 2, 300, 51), 7.0, dtype=TDT[dtype], device="cuda")
+        vo = torch.full((1, 3, 2, 300, D), 7.0, dtype=TDT[dtype], device="cuda")
+        thk.thk_paged_read(c.shape, c.pages, c.pool, c.table, _ints(row0), _ints(n), ko, None, 300)
+        thk.thk_paged_read(c.shape, c.pages, c.pool, c.table, _ints(row0), _ints(n), None, vo, 300)
+        torch.cuda.synchronize()
+        for b in range(3):
+            for h in range(2):
+                k, v, _, _, _ = c.unit(0, b, h)
+                for got, want in ((_np(ko[0, b, h]), k), (_np(vo[0, b, h]), v)):
+                    want = want[row0[b]:row0[b] + n[b]]
+                    assert np.all(np.abs(got[:n[b]] - want) <= (0 if bits == 0 else HALF_STEP[dtype]) * np.abs(want))
+                    assert np.all(got[n[b]:] == 7)
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_groups_without_range_and_with_extreme_ones(dtype, bits):
+    """Equal elements, scales that round to zero, the largest finite range, elements on the border between two codes."""
+    c = Cache(dtype, bits, 1, 1, 1, 1, 128, [128], 64, seed=1)
+    x = c.v[0, 0, 0]
+    x[0] = -3.25
+    x[1] = 0
+    x[2, :64], x[2, 64:] = 0, 2.0 ** -133                          # subnormal in both types
+    x[3] = 0
+    x[3, 5] = 2.0 ** -133                                          # the scale is below half the least bf16 number
+    x[4, ::2], x[4, 1::2] = 1.5e38, -1.5e38
+    step = torch.arange(128, device="cuda") % 64
+    x[5] = (step.float() * 0.5).clamp(max=15).to(x.dtype)            # with 4 bits: every second one half way between two codes
+    x[6] = 1e-30 * torch.randn(128, generator=c.g, device="cuda").to(x.dtype)
+    x[7] = 1e-38 * torch.randn(128, generator=c.g, device="cuda").to(x.dtype)    # subnormal scales
+    c.k[0, 0, 0, :, :64] = x[:8].repeat(16, 1)[:, :64]
+    c.write()
+    ko, vo = (torch.empty(1, 1, 1, 128, D, dtype=TDT[dtype], device="cuda") for _ in range(2))
+    thk.thk_paged_read(c.shape, c.pages, c.pool, c.table, None, c.s_pages, ko, vo, 128)
+    torch.cuda.synchronize()
+    k, v, _, _, _ = c.unit(0, 0, 0)
+    least = 2.0 ** (-149 if dtype == "f32" else -133)   # half a step of a subnormal result is up to half of this
+    for got, want in ((_np(ko[0, 0, 0]), k), (_np(vo[0, 0, 0]), v)):
+        assert np.all(np.abs(got - want) <= HALF_STEP[dtype] * np.abs(want) + least / 2)
+
+
+@pytest.mark.parametrize("dtype,bits", [("bf16", 4), ("bf16", 0), ("f32", 8)])
+def test_a_chunk_after_a_chunk(dtype, bits):
+    """A prompt stored in two calls is the prompt stored in one; sequences whose first row is not a tile's are left alone."""
+    a = Cache(dtype, bits, 1, 3, 2, 1, 76, [320, 200, 128], 64, seed=11)
+    a.write()
+    want = a.pool.clone()
+    a.pool.fill_(255)
+    cut = [128, 64, 0]
+    thk.thk_paged_write(a.shape, a.pages, a.k, a.v, a.S, _ints(cut), None, a.idx, a.table, a.pool)
+    rest = a.S
+    k2, v2 = torch.full_like(a.k, float("nan")), torch.full_like(a.v, float("nan"))
+    for b, n in enumerate(cut):
+        k2[:, b, :, :a.S - n], v2[:, b, :, :a.S - n] = a.k[:, b, :, n:], a.v[:, b, :, n:]
+    n2 = [x - y for x, y in zip(a.rows, cut)]
+    before = a.pool.clone()
+    for bad in (1, 63, -64, 65):
+        thk.thk_paged_write(a.shape, a.pages, k2, v2, rest, _ints(n2), _ints([bad] * 3), a.idx, a.table, a.pool)
+    torch.cuda.synchronize()
+    assert torch.equal(a.pool, before)
+    thk.thk_paged_write(a.shape, a.pages, k2, v2, rest, _ints(n2), _ints(cut), a.idx, a.table, a.pool)
+    torch.cuda.synchronize()
+    assert torch.equal(a.pool, want)
+
+
+def test_counts_and_tables_past_the_bounds_write_nothing_outside():
+    """Counts above the bounds are clamped to them, negative ones to zero; tables with entries outside the pool."""
+    c = Cache("bf16", 4, 1, 4, 1, 1, 64, [256, 256, 256, 256], 64, seed=2, spare=4)
+    table = c.table.clone()
+    table[0, 1], table[1, 2], table[2, 0], table[3, 3] = -1, c.pages.n_pages, 1 << 30, -(1 << 31)
+    guard = torch.full((c.pool.numel() + 2048,), 255, dtype=torch.uint8, device="cuda")
+    pool = guard[1024:-1024]
+    thk.thk_paged_write(c.shape, c.pages, c.k, c.v, c.S, _ints([1 << 30, 256, 300, -5]), None, c.idx, table, pool)
+    torch.cuda.synchronize()
+    assert torch.all(guard[:1024] == 255) and torch.all(guard[-1024:] == 255)
+    tile = c.pool.numel() // c.pages.n_pages
+    written = {int(p) for p in range(c.pages.n_pages) if not torch.all(pool[p * tile:(p + 1) * tile] == 255)}
+    assert written == {int(table[b, i]) for b in range(3) for i in range(4) if 0 <= table[b, i] < c.pages.n_pages}
+    ko = torch.full((1, 4, 1, 256, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    thk.thk_paged_read(c.shape, c.pages, pool, table, None, _ints([1 << 30, 256, 256, -1]), ko, None, 256)
+    thk.thk_paged_read(c.shape, c.pages, pool, table, _ints([-64, 1 << 30, (1 << 31) - 1, 256]), _ints([256] * 4), ko, None, 256)
+    torch.cuda.synchronize()
+    assert torch.all(ko[0, 0, 0, 64:128] == 7) and torch.all(ko[0, 1, 0, 128:192] == 7) and torch.all(ko[0, 2, 0, :64] == 7) and torch.all(ko[0, 3] == 7)
+    assert not torch.all(ko[0, 0, 0, :64] == 7, dim=1).any()   # (single elements may well stand for 7)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_ragged_append(dtype):
+    L, B, N_kv, cap, src = 2, 5, 3, 16, 9
+    g = torch.Generator(device="cuda"); g.manual_seed(4)
+    new = [torch.randn(L, B, N_kv, src, D, generator=g, device="cuda").to(TDT[dtype]) for _ in range(2)]
+    tail = [torch.randn(L, B, N_kv, cap, D, generator=g, device="cuda").to(TDT[dtype]) for _ in range(2)]
+    shape = thk.make_shape(L, B, N_kv, N_kv, D, 1, 1, 64, 0, DT[dtype])
+    for row0, n, s in (([0, 0, 0, 0, 0], [1, 1, 1, 1, 1], [0, 3, 15, 16, 7]), ([0, 8, 2, 5, -1], [9, 4, 0, -3, 2], [0, 0, 5, 5, 5]),
+                       ([3, 0, 0, 0, 0], [6, 9, 9, 9, 99], [10, 12, -2, 1 << 30, 0])):
+        got = [t.clone() for t in tail]
+        thk.thk_tail_append_ragged(shape, *new, src, _ints(row0), _ints(n), *got, _ints(s), cap)
+        torch.cuda.synchronize()
+        for x, y, z in zip(new, tail, got):
+            want = y.clone()
+            for b in range(B):
+                for r in range(min(max(n[b], 0), src)):
+                    if 0 <= row0[b] + r < src and 0 <= s[b] + r < cap:
+                        want[:, b, :, s[b] + r] = x[:, b, :, row0[b] + r]
+            assert torch.equal(z, want)
+    got = [t.clone() for t in tail]
+    one = [x[..., :1, :].contiguous() for x in new]
+    thk.thk_tail_append_ragged(shape, *one, 1, None, None, *got, _ints([0, 1, 2, 15, 16]), cap)
+    for x, y, z in zip(one, tail, got):
+        want = y.clone()
+        for b, s in enumerate([0, 1, 2, 15]):
+            want[:, b, :, s] = x[:, b, :, 0]
+        assert torch.equal(z, want)
+
+
+def _check_attention(c, out):
+    """Every output against fp64 attention over what is stored.  An output is rounded once; a logit is off by what the
+    products' terms and their fp32 sums are -- c_z of the sum of the products' sizes, the sizes being at most those of
+    q (|m| + 31 s), 31 s <= 31 / 15 (max k - min k) <= 4.2 max |k| -- and moves an output by at most twice that times the
+    largest value; the values' products by c_z of at most 5.2 times the largest value."""
+    c_z = {"bf16": 2.0 ** -16, "f32": 2.0 ** -20}[c.dtype]   # terms: 2^-17, 2^-25; sums of some 256 roundings of 2^-24, as random ones
+    for l in range(c.L):
+        for b in range(c.B):
+            for h in range(c.N_kv):
+                k, v, kt, vt, idx = c.unit(l, b, h)
+                q = _np(c.q[l, b, h * c.G:(h + 1) * c.G])
+                want = P.attend(q, idx, k, v, kt, vt)
+                got = _np(out[l, b, h * c.G:(h + 1) * c.G])
+                if len(k) + len(kt) == 0:
+                    assert not got.any(), (l, b, h)
+                    continue
+                top = max(np.abs(v).max(initial=0), np.abs(vt).max(initial=0))
+                size = 5.2 * np.abs(q[:, idx]) @ np.abs(k).max(0, initial=0) + np.abs(q) @ np.abs(kt).max(0, initial=0)
+                tol = HALF_STEP[c.dtype] * np.abs(want) + c_z * top * (2 * size[:, None] / np.sqrt(D) + 5.2)
+                bad = np.abs(got - want) > tol
+                assert not bad.any(), (l, b, h, np.abs(got - want).max(), tol.min())
+
+
+# (L, B, N_kv, G, T, rows, page_rows, tails, cap, n_split)
+ATTEND = [
+    (1, 1, 1, 1, 64, [1], 64, None, 0, 0), (1, 1, 1, 1, 1, [64], 64, [1], 1, 0), (1, 2, 2, 4, 51, [0, 65], 64, [0, 3], 16, 0),
+    (1, 3, 2, 8, 76, [129, 0, 300], 128, [64, 65, 0], 128, 0), (2, 2, 3, 2, 128, [63, 512], 256, [0, 17], 64, 3),
+    (1, 1, 2, 16, 97, [700], 64, [200], 200, 4), (1, 1, 1, 17, 96, [260], 64, [1], 64, 2), (1, 2, 1, 40, 65, [64, 130], 64, [5, 0], 8, 0),
+    (1, 4, 2, 5, 33, [2000, 1, 640, 0], 128, [0, 0, 64, 2], 64, 0), (1, 1, 4, 4, 64, [5000], 512, None, 0, 100),
+    (3, 1, 2, 3, 8, [257], 64, [33], 64, 1), (1, 2, 2, 1, 128, [0, 0], 64, [0, 64], 64, 0), (1, 2, 1, 7, 64, [4096, 30], 1024, [63, 1], 64, 7),
+]
+
+
+@pytest.mark.parametrize("case", ATTEND, ids=[str(i) for i in range(len(ATTEND))])
+@pytest.mark.parametrize("bits", [0, 4, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_over_pages_and_tail(dtype, bits, case):
+    L, B, N_kv, G, T, rows, page_rows, tails, cap, n_split = case
+    print("attend", dtype, bits, case, flush=True)
+    c = Cache(dtype, bits, L, B, N_kv, G, T, rows, page_rows, tails, cap, seed=sum(rows) + G, n_split=n_split)
+    c.write()
+    out = c.decode()
+    torch.cuda.synchronize()
+    _check_attention(c, out)
+    assert torch.equal(c.decode(), out)          # the same bits again
+
+
+@pytest.mark.parametrize("dtype,bits", [("bf16", 0), ("bf16", 4), ("f32", 8)])
+def test_rows_of_a_tile_past_the_count_do_not_matter(dtype, bits):
+    """A sequence that was stored longer than it now is, as after rejected guesses of a draft model."""
+    c = Cache(dtype, bits, 1, 2, 2, 4, 64, [300, 200], 64, seed=8)
+    c.write()
+    full = [c.unit(0, b, h) for b in range(2) for h in range(2)]
+    for rows in ([299, 193], [257, 1], [64, 0]):
+        c.s_pages, c.rows = _ints(rows), rows
+        out = c.decode()
+        torch.cuda.synchronize()
+        for b in range(2):
+            for h in range(2):
+                k, v, kt, vt, idx = full[b * 2 + h]
+                q = _np(c.q[0, b, h * 4:(h + 1) * 4])
+                want = P.attend(q, idx, k[:rows[b]], v[:rows[b]], kt, vt)
+                tol = {"bf16": 2.0 ** -8, "f32": 2e-5}[dtype] * max(np.abs(want).max(initial=0), 1e-30) + {"bf16": 1e-3, "f32": 1e-5}[dtype]
+                assert np.abs(_np(out[0, b, h * 4:(h + 1) * 4]) - want).max() <= tol
+
+
+def test_pages_outside_the_pool_take_no_part():
+    c = Cache("bf16", 4, 1, 2, 1, 4, 64, [256, 256], 64, tails=[3, 0], cap=64, seed=21)
+    c.write()
+    keep = c.table.clone()
+    c.table = keep.clone()
+    c.table[0, 1], c.table[1, 0], c.table[1, 1], c.table[1, 2], c.table[1, 3] = -1, c.pages.n_pages, 1 << 30, -7, -(1 << 31)
+    out = c.decode()
+    torch.cuda.synchronize()
+    k, v, kt, vt, idx = c.unit(0, 0, 0)
+    live = np.r_[0:64, 128:256]
+    want = P.attend(_np(c.q[0, 0]), idx, k[live], v[live], kt, vt)
+    assert np.abs(_np(out[0, 0]) - want).max() <= 2.0 ** -8 * np.abs(want).max() + 1e-3
+    assert not out[0, 1].any()                   # all of its pages are missing
+
+
+def test_counts_past_the_bounds_are_clamped():
+    c = Cache("bf16", 8, 1, 3, 2, 2, 64, [128, 128, 128], 64, tails=[8, 8, 8], cap=8, seed=5)
+    c.write()
+    want = c.decode()
+    c.s_pages, c.s_tail = _ints([1 << 30, 129, 128]), _ints([9, 1 << 30, 8])
+    assert torch.equal(c.decode(), want)
+    c.s_pages, c.s_tail = _ints([-1, 0, -(1 << 31)]), _ints([0, -1, -(1 << 31)])
+    assert not c.decode().any()
+
+
+@pytest.mark.parametrize("dtype,bits", [("bf16", 4), ("f32", 0)])
+def test_every_split_gives_the_same_attention(dtype, bits):
+    c = Cache(dtype, bits, 1, 2, 2, 4, 64, [1900, 700], 128, tails=[70, 3], cap=128, seed=31)
+    c.write()
+    for n in (1, 2, 5, 8, 30, 4096):
+        c.shape.n_split = n
+        _check_attention(c, c.decode())
+
+
+def test_offsets_past_32_bits():
+    """A pool of more than 4 GiB whose first and last pages are in use, and tails likewise."""
+    c = Cache("bf16", 0, 1, 2, 8, 4, 128, [256, 130], 256, tails=[10, 64], cap=64, seed=6, spare=0)
+    page = thk.thk_paged_pool_bytes(c.shape, c.pages) // c.pages.n_pages
+    n_pages = (5 << 30) // page
+    c.pages.n_pages = n_pages
+    c.table = torch.tensor([[n_pages - 1], [n_pages // 2 + 7]], dtype=torch.int32, device="cuda")
+    c.pool = torch.empty(n_pages * page, dtype=torch.uint8, device="cuda")
+    c.write()
+    out = c.decode()
+    torch.cuda.synchronize()
+    _check_attention(c, out)
+    ko = torch.empty(1, 2, 8, 256, 128, dtype=torch.bfloat16, device="cuda")
+    thk.thk_paged_read(c.shape, c.pages, c.pool, c.table, None, c.s_pages, ko, None, 256)
+    want = c.k.gather(4, c.idx.long()[..., None, :].expand(1, 2, 8, 256, 128))
+    for b, n in enumerate(c.rows):
+        assert torch.equal(ko[:, b, :, :n], want[:, b, :, :n])
+
+
+@pytest.mark.parametrize("dtype,bits", [("bf16", 4), ("bf16", 0), ("f32", 8)])
+def test_a_ragged_batch_grows(dtype, bits):
+    """Prompts stored in whole tiles, their rests in the tails; tokens appended one by one; a full tail goes into pages.
+    The whole step is captured once and replayed: lengths, and which sequences flush, change on the device."""
+    L, B, N_kv, G, T, cap = 1, 3, 2, 4, 76, 64
+    prompts, page_rows, steps = [130, 64, 20], 64, 110
+    most = max(prompts) + steps
+    c = Cache(dtype, bits, L, B, N_kv, G, T, [most] * B, page_rows, seed=40, S=most)
+    idx = _np(c.idx).astype(int)
+    # the host's account
+    whole = [n // 64 * 64 for n in prompts]
+    s_pages, s_tail = _ints([0] * B), _ints([0] * B)
+    kt = torch.full((L, B, N_kv, cap, D), float("nan"), dtype=TDT[dtype], device="cuda")
+    vt = kt.clone()
+    n_prompt, n_whole = _ints(prompts), _ints(whole)
+    thk.thk_paged_write(c.shape, c.pages, c.k, c.v, c.S, n_whole, None, c.idx, c.table, c.pool)
+    thk.thk_tail_append_ragged(c.shape, c.k, c.v, c.S, n_whole, n_prompt - n_whole, kt, vt, s_tail, cap)
+    s_pages += n_whole
+    s_tail += n_prompt - n_whole
+    k_new = torch.zeros(L, B, N_kv, D, dtype=TDT[dtype], device="cuda")
+    v_new = torch.zeros_like(k_new)
+    q, out = torch.zeros(L, B, N_kv * G, D, dtype=TDT[dtype], device="cuda"), torch.zeros(L, B, N_kv * G, D, dtype=TDT[dtype], device="cuda")
+    ws = ws_tensor(thk.thk_workspace_bytes(c.shape, thk.THK_OP_DECODE_PAGED))
+
+    def step():
+        full = torch.where(s_tail == cap, s_tail, torch.zeros_like(s_tail))
+        thk.thk_paged_write(c.shape, c.pages, kt, vt, cap, full, s_pages, c.idx, c.table, c.pool)
+        s_pages.add_(full)
+        s_tail.sub_(full)
+        thk.thk_tail_append_ragged(c.shape, k_new, v_new, 1, None, None, kt, vt, s_tail, cap)
+        s_tail.add_(1)
+        thk.thk_decode_attn_paged(c.shape, c.pages, q, c.pool, c.table, s_pages, c.idx, kt, vt, s_tail, cap, out, ws)
+
+    state = [t.clone() for t in (s_pages, s_tail, kt, vt, c.pool)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    for t, x in zip((s_pages, s_tail, kt, vt, c.pool), state):
+        t.copy_(x)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for t, x in zip((s_pages, s_tail, kt, vt, c.pool), state):
+        t.copy_(x)
+    stored, tail = list(whole), [n - w for n, w in zip(prompts, whole)]
+    for i in range(steps):
+        at = [n + i for n in prompts]
+        for b in range(B):
+            k_new[:, b], v_new[:, b] = c.k[:, b, :, at[b]], c.v[:, b, :, at[b]]
+            if tail[b] == cap:
+                stored[b], tail[b] = stored[b] + cap, 0
+            tail[b] += 1
+        q.copy_(torch.randn(q.shape, generator=c.g, device="cuda"))
+        if i % 2:
+            step()
+        else:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert s_pages.tolist() == stored and s_tail.tolist() == tail
+        if i % 9 and tail != [1, 1, 1] and 1 not in tail:
+            continue
+        for b in range(B):
+            for h in range(N_kv):
+                kk, vv = _np(c.k[0, b, h, :stored[b] + tail[b]]), _np(c.v[0, b, h, :stored[b] + tail[b]])
+                ks, vs = P.stored(kk[:stored[b]][:, idx[0, b, h]], vv[:stored[b]], bits, dtype)
+                want = P.attend(_np(q[0, b, h * G:(h + 1) * G]), idx[0, b, h], ks, vs, kk[stored[b]:], vv[stored[b]:])
+                tol = {"bf16": 2.0 ** -8, "f32": 2e-5}[dtype] * np.abs(want).max() + {"bf16": 4e-3, "f32": 5e-5}[dtype]
+                assert np.abs(_np(out[0, b, h * G:(h + 1) * G]) - want).max() <= tol, (i, b, h)
+
+
+def test_other_streams_and_refused_tensors():
+    c = Cache("bf16", 4, 1, 2, 2, 4, 64, [500, 64], 64, tails=[3, 64], cap=64, seed=50)
+    c.write()
+    want = c.decode()
+    torch.cuda.synchronize()
+    c.pool.fill_(255)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    c.write(stream=side)
+    got = torch.full_like(c.q, float("nan"))
+    side.wait_stream(torch.cuda.current_stream())
+    c.decode(out=got, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+    for name, bad in (("q", c.q.float()), ("s_pages", c.s_pages.long()), ("idx", c.idx.int()), ("q", c.q[:, :1]), ("kt", c.kt.transpose(3, 4)),
+                      ("table", c.table[:, :1].contiguous()), ("pool", c.pool[:-16]), ("s_tail", c.s_tail[:1]), ("vt", c.vt[..., :32, :].contiguous())):
+        keep = getattr(c, name)
+        setattr(c, name, bad)
+        with pytest.raises(ValueError):
+            c.decode(out=got, ws=ws_tensor(1 << 16))
+        setattr(c, name, keep)
