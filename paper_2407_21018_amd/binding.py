@@ -127,6 +127,8 @@ def load():
         from . import _thk_call
         addr = lambda f: ctypes.cast(f, vp).value
         _thk_call.bind(addr(L.thk_decode_attn), addr(L.thk_decode_attn_kv), addr(L.thk_tail_append), addr(L.thk_prune), thk_shape)
+        _thk_call.bind_paged(addr(L.thk_decode_attn_paged), addr(L.thk_tail_append_ragged), addr(L.thk_paged_write), addr(L.thk_paged_read),
+                             addr(L.thk_paged_pool_bytes), thk_pages)
         _call = _thk_call
     except ImportError as e:
         warnings.warn(f"the native issue of the per-token calls cannot be loaded ({e}): calls go through ctypes, 2 us slower "
@@ -480,6 +482,8 @@ class _Tensors:
 
 def thk_paged_write(shape, pages, k, v, src_rows, n_rows, row0, idx, table, pool, stream=None):
     w = "thk_paged_write"
+    if _call is not None and _issued(_call.paged_write(shape, pages, k, v, src_rows, n_rows, row0, idx, table, pool, stream), w):
+        return
     t = _Tensors(shape, w)
     U, _, D, _, _, T, _, _, _ = _dims(shape)
     n = U * src_rows * D
@@ -491,6 +495,8 @@ def thk_paged_write(shape, pages, k, v, src_rows, n_rows, row0, idx, table, pool
 
 def thk_paged_read(shape, pages, pool, table, row0, n_rows, k_out, v_out, out_rows, stream=None):
     w = "thk_paged_read"
+    if _call is not None and _issued(_call.paged_read(shape, pages, pool, table, row0, n_rows, k_out, v_out, out_rows, stream), w):
+        return
     t = _Tensors(shape, w)
     U, _, D, _, _, _, ld, _, _ = _dims(shape)
     _check(load().thk_paged_read(ctypes.byref(shape), ctypes.byref(pages), t.raw(pool, thk_paged_pool_bytes(shape, pages), "pool"),
@@ -501,6 +507,9 @@ def thk_paged_read(shape, pages, pool, table, row0, n_rows, k_out, v_out, out_ro
 
 def thk_tail_append_ragged(shape, k_new, v_new, src_rows, src_row0, n_new, k_tail, v_tail, s_tail, s_tail_cap, stream=None):
     w = "thk_tail_append_ragged"
+    if _call is not None and _issued(_call.tail_append_ragged(shape, k_new, v_new, src_rows, src_row0, n_new, k_tail, v_tail, s_tail,
+                                                              s_tail_cap, stream), w):
+        return
     t = _Tensors(shape, w)
     U, _, D, _, _, _, _, _, _ = _dims(shape)
     n, m = U * src_rows * D, U * s_tail_cap * D
@@ -512,6 +521,9 @@ def thk_tail_append_ragged(shape, k_new, v_new, src_rows, src_row0, n_new, k_tai
 
 def thk_decode_attn_paged(shape, pages, q, pool, table, s_pages, idx, k_tail, v_tail, s_tail, s_tail_cap, out, ws, stream=None):
     w = "thk_decode_attn_paged"
+    if _call is not None and _issued(_call.decode_attn_paged(shape, pages, q, pool, table, s_pages, idx, k_tail, v_tail, s_tail,
+                                                             s_tail_cap, out, ws, stream), w):
+        return
     t = _Tensors(shape, w)
     U, H, D, _, _, T, _, _, _ = _dims(shape)
     m = U * s_tail_cap * D

@@ -19,7 +19,13 @@ decltype(&thk_decode_attn) f_decode = nullptr;
 decltype(&thk_decode_attn_kv) f_decode_kv = nullptr;
 decltype(&thk_tail_append) f_append = nullptr;
 decltype(&thk_prune) f_prune = nullptr;
+decltype(&thk_decode_attn_paged) f_decode_paged = nullptr;
+decltype(&thk_tail_append_ragged) f_append_ragged = nullptr;
+decltype(&thk_paged_write) f_write = nullptr;
+decltype(&thk_paged_read) f_read = nullptr;
+decltype(&thk_paged_pool_bytes) f_pool_bytes = nullptr;
 PyTypeObject *g_shape = nullptr;   // thk_shape of the Python code
+PyTypeObject *g_pages = nullptr;   // ... and thk_pages
 PyObject *g_get_stream = nullptr, *g_get_device = nullptr;   // torch's raw getters, once the runtime is up
 
 // The arguments of one call; ok turns false at the first one that is not in the plain form.
@@ -44,7 +50,48 @@ struct Args {
   }
   ~Args() {
     if (view.obj != nullptr) PyBuffer_Release(&view);
+    if (pages_view.obj != nullptr) PyBuffer_Release(&pages_view);
   }
+  // The paged calls: their tensors are on the current device, of the type that the call reads them as.
+  Args(PyObject *s, PyObject *p) : Args(s) {
+    if (p != nullptr) {
+      if (!ok || g_pages == nullptr || !PyObject_TypeCheck(p, g_pages)) {
+        ok = false;
+        return;
+      }
+      if (PyObject_GetBuffer(p, &pages_view, PyBUF_SIMPLE) != 0) {
+        PyErr_Clear();
+        ok = false;
+        return;
+      }
+      ok = pages_view.len == (Py_ssize_t)sizeof(thk_pages);
+      pages = (const thk_pages *)pages_view.buf;
+    }
+    PyObject *d = ok && g_get_device != nullptr ? PyObject_CallNoArgs(g_get_device) : nullptr;
+    device = d != nullptr ? (int)PyLong_AsLong(d) : -1;
+    Py_XDECREF(d);
+    if (PyErr_Occurred()) PyErr_Clear();
+    ok = ok && device >= 0;
+    element = shape != nullptr && shape->dtype == THK_F32 ? at::kFloat : at::kBFloat16;
+  }
+  const thk_pages *pages = nullptr;
+  Py_buffer pages_view{};
+  int device = -1;
+  at::ScalarType element = at::kBFloat16;
+
+  void *here(PyObject *x, int64_t n, at::ScalarType type) {
+    if (!ok || !plain(x)) return ok = false, nullptr;
+    const at::Tensor &t = THPVariable_Unpack(x);
+    if (!t.is_cuda() || t.get_device() != device || t.scalar_type() != type) return ok = false, nullptr;
+    return tensor(x, n);
+  }
+  void *rows_here(PyObject *x, int64_t n) { return here(x, n, element); }
+  int32_t *ints(PyObject *x, int64_t n) { return (int32_t *)here(x, n, at::kInt); }
+  int32_t *ints_if(PyObject *x, int64_t n) { return x == Py_None ? nullptr : ints(x, n); }
+  int16_t *kept(PyObject *x, int64_t n) { return (int16_t *)here(x, n, at::kShort); }
+  void *pool(PyObject *x) { return here(x, ok ? (int64_t)f_pool_bytes(shape, pages) : 0, at::kByte); }
+  int32_t *table(PyObject *x) { return ints(x, ok ? count(shape->B, pages->max_pages) : 0); }
+
   static bool plain(PyObject *x) { return THPVariable_CheckExact(x); }
   // address of a tensor of at least n elements
   void *tensor(PyObject *x, int64_t n) {
@@ -213,6 +260,110 @@ PyObject *prune(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// (shape, pages, q, pool, table, s_pages, idx, k_tail, v_tail, s_tail, s_tail_cap, out, ws, stream)
+PyObject *decode_attn_paged(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (n != 14 || f_decode_paged == nullptr) return not_taken();
+  return guarded([&]() -> PyObject * {
+    Args x(a[0], a[1]);
+    if (!x.ok) return not_taken();
+    const thk_shape *s = x.shape;
+    const int64_t U = x.layers_units(), hn = x.count(x.heads(), s->D);
+    const int32_t cap = x.integer(a[10]);
+    void *q = x.rows_here(a[2], hn), *pool = x.pool(a[3]);
+    int32_t *table = x.table(a[4]), *s_pages = x.ints(a[5], s->B);
+    int16_t *idx = x.kept(a[6], x.count(U, s->T));
+    void *kt = nullptr, *vt = nullptr;
+    int32_t *s_tail = nullptr;
+    if (cap > 0) {
+      const int64_t tail = x.count(U, cap, s->D);
+      kt = x.rows_here(a[7], tail), vt = x.rows_here(a[8], tail);
+      s_tail = x.ints(a[9], s->B);
+    }
+    void *out = x.rows_here(a[11], hn);
+    size_t bytes = 0;
+    void *ws = x.workspace(a[12], bytes), *st = x.stream(a[13]);
+    if (!x.ok) return not_taken();
+    return issue([&] { return f_decode_paged(s, x.pages, q, pool, table, s_pages, idx, kt, vt, s_tail, cap, out, ws, bytes, st); });
+  });
+}
+
+// (shape, k_new, v_new, src_rows, src_row0, n_new, k_tail, v_tail, s_tail, s_tail_cap, stream)
+PyObject *tail_append_ragged(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (n != 11 || f_append_ragged == nullptr) return not_taken();
+  return guarded([&]() -> PyObject * {
+    Args x(a[0], nullptr);
+    if (!x.ok) return not_taken();
+    const thk_shape *s = x.shape;
+    const int32_t src = x.integer(a[3]), cap = x.integer(a[9]);
+    if (src < 0 || cap < 0) return not_taken();
+    const int64_t un = x.count(x.layers_units(), s->D), rows = x.count(un, src), tail = x.count(un, cap);
+    void *kn = x.rows_here(a[1], rows), *vn = x.rows_here(a[2], rows);
+    int32_t *row0 = x.ints_if(a[4], s->B), *n_new = x.ints_if(a[5], s->B);
+    void *kt = x.rows_here(a[6], tail), *vt = x.rows_here(a[7], tail);
+    int32_t *s_tail = x.ints(a[8], s->B);
+    void *st = x.stream(a[10]);
+    if (!x.ok) return not_taken();
+    return issue([&] { return f_append_ragged(s, kn, vn, src, row0, n_new, kt, vt, s_tail, cap, st); });
+  });
+}
+
+// (shape, pages, k, v, src_rows, n_rows, row0, idx, table, pool, stream)
+PyObject *paged_write(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (n != 11 || f_write == nullptr) return not_taken();
+  return guarded([&]() -> PyObject * {
+    Args x(a[0], a[1]);
+    if (!x.ok) return not_taken();
+    const thk_shape *s = x.shape;
+    const int32_t src = x.integer(a[4]);
+    if (src < 0) return not_taken();
+    const int64_t U = x.layers_units(), rows = x.count(U, src, s->D);
+    void *k = x.rows_here(a[2], rows), *v = x.rows_here(a[3], rows);
+    int32_t *n_rows = x.ints(a[5], s->B), *row0 = x.ints_if(a[6], s->B);
+    int16_t *idx = x.kept(a[7], x.count(U, s->T));
+    int32_t *table = x.table(a[8]);
+    void *pool = x.pool(a[9]), *st = x.stream(a[10]);
+    if (!x.ok) return not_taken();
+    return issue([&] { return f_write(s, x.pages, k, v, src, n_rows, row0, idx, table, pool, st); });
+  });
+}
+
+// (shape, pages, pool, table, row0, n_rows, k_out, v_out, out_rows, stream)
+PyObject *paged_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (n != 10 || f_read == nullptr) return not_taken();
+  return guarded([&]() -> PyObject * {
+    Args x(a[0], a[1]);
+    if (!x.ok) return not_taken();
+    const thk_shape *s = x.shape;
+    const int32_t out = x.integer(a[8]);
+    if (out < 0) return not_taken();
+    const int64_t rows = x.count(x.layers_units(), out);
+    void *pool = x.pool(a[2]);
+    int32_t *table = x.table(a[3]), *row0 = x.ints_if(a[4], s->B), *n_rows = x.ints(a[5], s->B);
+    void *ko = a[6] == Py_None ? nullptr : x.rows_here(a[6], x.count(rows, x.ld()));
+    void *vo = a[7] == Py_None ? nullptr : x.rows_here(a[7], x.count(rows, s->D));
+    void *st = x.stream(a[9]);
+    if (!x.ok) return not_taken();
+    return issue([&] { return f_read(s, x.pages, pool, table, row0, n_rows, ko, vo, out, st); });
+  });
+}
+
+// bind_paged(decode_attn_paged, tail_append_ragged, paged_write, paged_read, paged_pool_bytes, thk_pages)
+PyObject *bind_paged(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (n != 6 || !PyType_Check(a[5])) return PyErr_SetString(PyExc_TypeError, "bind_paged: five addresses and a type"), nullptr;
+  void *p[5];
+  for (int i = 0; i < 5; ++i) p[i] = PyLong_AsVoidPtr(a[i]);
+  if (PyErr_Occurred()) return nullptr;
+  f_decode_paged = (decltype(f_decode_paged))p[0];
+  f_append_ragged = (decltype(f_append_ragged))p[1];
+  f_write = (decltype(f_write))p[2];
+  f_read = (decltype(f_read))p[3];
+  f_pool_bytes = (decltype(f_pool_bytes))p[4];
+  PyTypeObject *old = g_pages;
+  g_pages = (PyTypeObject *)Py_NewRef(a[5]);
+  Py_XDECREF((PyObject *)old);
+  Py_RETURN_NONE;
+}
+
 // bind(decode_attn, decode_attn_kv, tail_append, prune, thk_shape): the library's entry points, as addresses, and
 // the type of a shape
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -244,7 +395,8 @@ PyObject *stream_getters(PyObject *, PyObject *const *a, Py_ssize_t n) {
 
 #define THK_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {THK_METHOD(decode_attn), THK_METHOD(decode_attn_kv), THK_METHOD(tail_append), THK_METHOD(prune),
-                         THK_METHOD(bind), THK_METHOD(stream_getters), {nullptr, nullptr, 0, nullptr}};
+                         THK_METHOD(decode_attn_paged), THK_METHOD(tail_append_ragged), THK_METHOD(paged_write), THK_METHOD(paged_read),
+                         THK_METHOD(bind), THK_METHOD(bind_paged), THK_METHOD(stream_getters), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_thk_call", "Native issue of the per-token calls of libthk.", -1, methods};
 
 }  // namespace
