@@ -54,15 +54,14 @@ struct PagedPool {
   int32_t N_kv, B;
   PagedLayout lay;
 
-  // Tile `tile` of sequence b's KV head h in layer l; nullptr where the table has no page of the pool for it.
+  // Tile `tile` of sequence b's KV head h in layer l, the same for all lanes; nullptr where the table has no page of the
+  // pool for it.
   __device__ __forceinline__ char *tile(int64_t l, int b, int h, int64_t tile) const {
     const int64_t slot = tile >> tpp_shift;
     if (slot >= max_pages) return nullptr;
-    return in_page(l, h, table[(int64_t)b * max_pages + slot], (int)(tile & ((1 << tpp_shift) - 1)));
-  }
-  __device__ __forceinline__ char *in_page(int64_t l, int h, int page, int t) const {
+    const int page = __builtin_amdgcn_readfirstlane(table[(int64_t)b * max_pages + slot]);
     if (page < 0 || page >= n_pages) return nullptr;
-    return (char *)pool + ((((l * n_pages + page) * N_kv + h) << tpp_shift) + t) * (int64_t)lay.tile_bytes;
+    return (char *)pool + ((((l * n_pages + page) * N_kv + h) << tpp_shift) + (tile & ((1 << tpp_shift) - 1))) * (int64_t)lay.tile_bytes;
   }
 };
 
