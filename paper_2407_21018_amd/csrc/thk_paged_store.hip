@@ -2,21 +2,45 @@
 // ragged tails.  Memory bounds all three: every row is read once and written once.
 #include "thk_paged.h"
 
+#include <type_traits>
+
 namespace thk {
 namespace {
 
-// The lanes m = 0..15 of a group form a row of the wave's data paths, so a reduction over them is four rotations.
-template <int N>
-__device__ __forceinline__ float ror16(float x) {
-  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x120 + N, 0xf, 0xf, false));
+// A value of another lane of the 16 that share a group (a row of the wave's data paths); the control words of the moves.
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float x) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, false));
 }
-__device__ __forceinline__ float min16(float x) {
-  x = fminf(x, ror16<8>(x)); x = fminf(x, ror16<4>(x)); x = fminf(x, ror16<2>(x));
-  return fminf(x, ror16<1>(x));
-}
-__device__ __forceinline__ float max16(float x) {
-  x = fmaxf(x, ror16<8>(x)); x = fmaxf(x, ror16<4>(x)); x = fmaxf(x, ror16<2>(x));
-  return fmaxf(x, ror16<1>(x));
+constexpr int kXor8 = 0x128;    // rotation by 8
+constexpr int kXor7 = 0x141;    // mirror of eight lanes
+constexpr int kXor2 = 0x4e, kXor1 = 0xb1;   // permutations of four lanes
+constexpr int kLane0 = 0x150;   // + n: lane n of the 16
+
+// Extremes of two and three, as the instructions themselves: the library functions first bring every operand that is not
+// known to be the result of arithmetic into canonical form, an instruction for each element.
+__device__ __forceinline__ float smaller(float a, float b) { float r; asm("v_min_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b)); return r; }
+__device__ __forceinline__ float larger(float a, float b) { float r; asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b)); return r; }
+__device__ __forceinline__ float smaller(float a, float b, float c) { float r; asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c)); return r; }
+__device__ __forceinline__ float larger(float a, float b, float c) { float r; asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c)); return r; }
+
+// v[e], e = 0..7, each over all 16 lanes: lane m returns the extreme of v[m / 2].  Every step halves what a lane looks
+// after (it hands the other half to the lane across), so that eight reductions cost 22 instructions and not 32, and what
+// follows -- a group's scale and its reciprocal, some 40 instructions -- is done by two lanes for a group, not by all.
+template <bool MAX>
+__device__ __forceinline__ float extreme_of(const float (&v)[8], int m) {
+  auto pick = [](float a, float b) { return MAX ? larger(a, b) : smaller(a, b); };
+  const bool b3 = (m & 8) != 0, b2 = (m & 4) != 0, b1 = (m & 2) != 0;
+  float x[4], y[2];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = pick(b3 ? v[e + 4] : v[e], from_lane<kXor8>(b3 ? v[e] : v[e + 4]));
+#pragma unroll
+  for (int e = 0; e < 2; ++e) y[e] = pick(b2 ? x[e + 2] : x[e], from_lane<kXor7>(b2 ? x[e] : x[e + 2]));
+  float z = pick(b1 ? y[1] : y[0], from_lane<kXor2>(b1 ? y[0] : y[1]));
+  // a move between lanes must not read what one of the two instructions in front of it wrote, and the compiler, which sees to
+  // that for its own instructions, does not look into these
+  asm("s_nop 1" : "+v"(z));
+  return pick(z, from_lane<kXor1>(z));
 }
 
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
@@ -57,48 +81,72 @@ __device__ __forceinline__ void encode_group(const float (&x)[4][8], const bool 
     return;
   }
   constexpr float top = (float)((1 << BITS) - 1);
-  uint32_t code[4][8];
-  uint32_t pair_lo = 0, pair_hi = 0;   // this lane's parameter pair, element m & 7
+  float lo8[8], hi8[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float lo = min16(fminf(fminf(x[0][e], x[1][e]), fminf(x[2][e], x[3][e])));
-    const float hi = max16(fmaxf(fmaxf(x[0][e], x[1][e]), fmaxf(x[2][e], x[3][e])));
-    const float s = group_scale<DT, BITS>(lo, hi);
-    const float d = s > 0.f ? s : 1.f;
+    lo8[e] = smaller(smaller(x[0][e], x[1][e], x[2][e]), x[3][e]);
+    hi8[e] = larger(larger(x[0][e], x[1][e], x[2][e]), x[3][e]);
+  }
+  const float lo = extreme_of<false>(lo8, m), hi = extreme_of<true>(hi8, m), s = group_scale<DT, BITS>(lo, hi);
+  if ((m & 1) == 0) {
+    if constexpr (DT == THK_BF16) *(uint32_t *)(par + m * 2) = (__float_as_uint(s) >> 16) | (__float_as_uint(lo) & 0xffff0000u);
+    else *(uint2 *)(par + m * 4) = make_uint2(__float_as_uint(s), __float_as_uint(lo));
+  }
+  // (x - lo) / s, correctly rounded, by Markstein's corrections of a product with the reciprocal: with r the rounded
+  // 1 / s, y' = y + (t - y s) r is the rounded quotient where y is within one unit of it, which the product itself is for a
+  // scale of 8 bits (no quotient of a 24-bit by an 8-bit number lies within 2^-33 of the middle of two floats, and y' is
+  // within 2^-46 in front of its rounding) and one correction makes it for 24 bits.  The residuals are exact unless s is
+  // near the end of the range, where the division itself is taken.  s = 0 gives r = 0 and codes 0.
+  const float r = s > 0.f ? 1.f / s : 0.f;
+  const bool plain = __any(s != 0.f && !(s >= 0x1p-90f && s <= 0x1p120f));
+  // A quotient below 2^22 plus 1.5 * 2^23 has its nearest whole number (ties to even) in the lowest bits; codes are put
+  // together with the rest of the bits in place, whose sum is taken off at the end.
+  constexpr float kMagic = 0x1.8p23f;
+  constexpr uint32_t kRest = 0x4b400000u;
+  uint32_t word[4][BITS / 4];   // a unit per j
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int w = 0; w < BITS / 4; ++w) word[j][w] = 0;
+  constexpr auto place = [](int e) { return BITS == 4 ? 4 * (e >> 1) + 16 * (e & 1) : 8 * (e & 3); };
+  auto one = [&](auto divide, auto lane) {
+    constexpr int e = decltype(lane)::value;
+    const float le = from_lane<kLane0 + 2 * e>(lo), se = from_lane<kLane0 + 2 * e>(s), re = from_lane<kLane0 + 2 * e>(r);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float c = fminf(rintf((x[j][e] - lo) / d), top);
-      code[j][e] = s > 0.f && ok[j] ? (uint32_t)c : 0u;
+      const float t = x[j][e] - le;
+      float y;
+      if constexpr (!decltype(divide)::value) {
+        y = t * re;
+        y = fmaf(fmaf(-y, se, t), re, y);
+        if constexpr (DT == THK_F32) y = fmaf(fmaf(-y, se, t), re, y);
+      } else {
+        y = se > 0.f ? t / se : 0.f;
+      }
+      if constexpr (BITS == 8 || DT == THK_F32) y = fminf(y, top);   // (a scale of 8 bits is at most 2^-8 off: 15.06)
+      word[j][e / (32 / BITS)] += __float_as_uint(y + kMagic) << place(e);
     }
-    if ((m & 7) == e) {
-      pair_lo = __float_as_uint(s);
-      pair_hi = __float_as_uint(lo);
-    }
-  }
-  if (m < 8) {
-    if constexpr (DT == THK_BF16) *(uint32_t *)(par + m * 4) = (pair_lo >> 16) | (pair_hi & 0xffff0000u);
-    else *(uint2 *)(par + m * 8) = make_uint2(pair_lo, pair_hi);
-  }
+  };
+  auto all = [&](auto divide) {
+    one(divide, std::integral_constant<int, 0>()); one(divide, std::integral_constant<int, 1>());
+    one(divide, std::integral_constant<int, 2>()); one(divide, std::integral_constant<int, 3>());
+    one(divide, std::integral_constant<int, 4>()); one(divide, std::integral_constant<int, 5>());
+    one(divide, std::integral_constant<int, 6>()); one(divide, std::integral_constant<int, 7>());
+  };
+  if (plain) all(std::true_type());
+  else all(std::false_type());
+  uint32_t rest = 0;
+  for (int e = 0; e < 32 / BITS; ++e) rest += kRest << place(e);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int w = 0; w < BITS / 4; ++w) word[j][w] = ok[j] ? word[j][w] - rest : 0u;
   if constexpr (BITS == 4) {
-    u32x4 u;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      u[j] = 0;
-#pragma unroll
-      for (int p = 0; p < 4; ++p) u[j] |= (code[j][2 * p] << (4 * p)) | (code[j][2 * p + 1] << (16 + 4 * p));
-    }
-    st_stream((u32x4 *)(dst + m * 16), u);
+    st_stream((u32x4 *)(dst + m * 16), u32x4{word[0][0], word[1][0], word[2][0], word[3][0]});
   } else {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      u32x4 u;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int j = 2 * k + (w >> 1), e = 4 * (w & 1);
-        u[w] = code[j][e] | (code[j][e + 1] << 8) | (code[j][e + 2] << 16) | (code[j][e + 3] << 24);
-      }
-      st_stream((u32x4 *)(dst + (k * 16 + m) * 16), u);
-    }
+    for (int k = 0; k < 2; ++k)
+      st_stream((u32x4 *)(dst + (k * 16 + m) * 16), u32x4{word[2 * k][0], word[2 * k][1], word[2 * k + 1][0], word[2 * k + 1][1]});
   }
 }
 
@@ -109,7 +157,7 @@ __global__ __launch_bounds__(256) void k_paged_write(PagedWriteArgs a) {
   using E = Elem<DT>;
   constexpr int EB = E::EB, PITCH = kD * EB + 16;
   __shared__ __align__(16) char rows_lds[kTile * PITCH];
-  __shared__ int16_t idx_lds[kD];
+  __shared__ __align__(16) int16_t idx_lds[kD];
   const int tid = threadIdx.x, m = tid & 15, grp = tid >> 4;
   const int64_t u = blockIdx.x / (uint32_t)a.tiles;
   const int t = blockIdx.x % (uint32_t)a.tiles;
@@ -156,15 +204,19 @@ __global__ __launch_bounds__(256) void k_paged_write(PagedWriteArgs a) {
   if (grp >= a.p.lay.chunks) return;
   float xk[4][8];
   bool ok[4];
+  int channel[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) channel[e] = idx_lds[8 * grp + e];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int r = 16 * j + m;
     ok[j] = r < rows;
     const char *const src = rows_lds + min(r, rows - 1) * PITCH;   // a row outside repeats one inside: the extremes stay
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int c = 8 * grp + e;
-      xk[j][e] = c < a.T ? E::load1(src, idx_lds[c]) : 0.f;
+    for (int e = 0; e < 8; ++e) xk[j][e] = E::load1(src, channel[e]);
+    if (8 * grp + 8 > a.T) {   // past the last kept channel: zeros
+#pragma unroll
+      for (int e = 0; e < 8; ++e) xk[j][e] = 8 * grp + e < a.T ? xk[j][e] : 0.f;
     }
   }
   encode_group<DT, BITS>(xk, ok, dst + grp * 64 * a.p.lay.unit_bytes, dst + a.p.lay.k_params + grp * 8 * 2 * EB, m);
