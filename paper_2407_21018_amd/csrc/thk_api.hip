@@ -721,6 +721,8 @@ PagedPool paged_pool(const thk_shape *s, const thk_pages *p, const void *pool, c
   a.tpp_shift = __builtin_ctz((unsigned)p->page_rows / kTile);
   a.N_kv = s->N_kv;
   a.B = s->B;
+  a.by_N_kv = Divisor(s->N_kv);
+  a.by_B = Divisor(s->B);
   a.lay = paged_layout(s->dtype, p->bits, s->T);
   return a;
 }
@@ -1265,6 +1267,7 @@ thk_status thk_paged_write(const thk_shape *s, const thk_pages *p, const void *k
   a.units = units_of(s);
   a.T = s->T;
   a.tiles = (int32_t)ceil_div(a.most, kTile);
+  a.by_tiles = Divisor(a.tiles);
   if ((uint64_t)a.units * a.tiles * 256 > kMaxThreads) return THK_ERR_SHAPE;
   return failed(launch_paged_write(s->dtype, p->bits, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
 }
@@ -1286,6 +1289,7 @@ thk_status thk_paged_read(const thk_shape *s, const thk_pages *p, const void *po
   a.units = units_of(s);
   a.T = s->T; a.ld = ld_of(s);
   a.tiles = (int32_t)ceil_div(a.most + (row0 != nullptr ? kTile - 1 : 0), kTile);   // rows that begin inside a tile
+  a.by_tiles = Divisor(a.tiles);
   if ((uint64_t)a.units * a.tiles * 256 > kMaxThreads) return THK_ERR_SHAPE;
   return failed(launch_paged_read(s->dtype, p->bits, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
 }
@@ -1335,6 +1339,9 @@ thk_status thk_decode_attn_paged(const thk_shape *s, const thk_pages *p, const v
   a.n_split = sp.n;
   a.tiles_per_split = (int32_t)(sp.rows / kTile);
   a.groups = (int32_t)paged_groups(s);
+  a.by_split = Divisor(sp.n);
+  a.by_groups = Divisor(a.groups);
+  a.step = std::min(paged_decode_step(p->bits, a.G, a.T), (a.tiles_per_split + 3) / 4);   // no wave idle while another has two
   a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)s->D));
   if ((uint64_t)a.units * a.groups > kMaxThreads / 256 / sp.n || (uint64_t)a.units * a.G > kMaxThreads / 256) return THK_ERR_SHAPE;
   return failed(launch_paged_decode(s->dtype, p->bits, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;

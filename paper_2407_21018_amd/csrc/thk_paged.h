@@ -44,24 +44,65 @@ inline PagedLayout paged_layout(int dtype, int bits, int T) {
   return p;
 }
 
+// An element that is the same for all lanes and that no kernel of the call writes, through the scalar cache: it does not wait
+// for vector loads that are under way.
+__device__ __forceinline__ int scalar_load(const int32_t *p, int64_t i) {
+  return ((__attribute__((address_space(4))) const int32_t *)(uintptr_t)p)[i];
+}
+
+// Division by a number that is known when the call is planned, as a product: n * ceil(2^s / d) >> s is n / d for n < 2^24,
+// with s = 40 for d < 2^16 (the rounding up adds less than n / 2^40 < 2^-16 < 1 / d) and 48 from there on (the product stays
+// below 2^64 in both).  A division costs a wave some 30 instructions in front of its first load.
+struct Divisor {
+  uint64_t inv;
+  int32_t shift;
+  explicit Divisor(int64_t d = 1) : inv((((uint64_t)1 << (d < 65536 ? 40 : 48)) + d - 1) / d), shift(d < 65536 ? 40 : 48) {}
+  __device__ __forceinline__ uint32_t of(uint32_t n) const { return (uint32_t)((n * inv) >> shift); }
+};
+
+// A block's place among layers, sequences and KV heads.
+struct UnitPlace { uint32_t l; int b, h; };
+
+// One unit's pages: the same for all lanes.
+struct UnitPages {
+  char *base;             // of the unit's part of page 0
+  int64_t stride;         // from page to page
+  const int32_t *row;     // the sequence's row of the table
+  uint32_t n_pages;
+  int32_t max_pages, tpp_shift, tile_bytes;
+
+  // The table's entry for tile t of the sequence (for tiles past the table's end the last one), and the tile in that page;
+  // nullptr where the page is none of the pool's.  t < 2^31 / 64 + a step.
+  __device__ __forceinline__ int page_of(int t) const { return scalar_load(row, min(t >> tpp_shift, max_pages - 1)); }
+  __device__ __forceinline__ char *in_page(int page, int t) const {
+    if ((uint32_t)page >= n_pages) return nullptr;   // (negative ones among them)
+    return base + page * stride + (uint32_t)(t & ((1 << tpp_shift) - 1)) * (uint32_t)tile_bytes;
+  }
+  __device__ __forceinline__ char *tile(int64_t t) const {
+    if (t >> tpp_shift >= max_pages) return nullptr;
+    return in_page(page_of((int)t), (int)t);
+  }
+};
+
 // The pool and the tables of a call.
 struct PagedPool {
   void *pool;
   const int32_t *table;    // [B][max_pages]
-  int64_t n_pages;         // pages of one layer's part of the pool
+  int64_t n_pages;         // pages of one layer's part of the pool, < 2^31
   int32_t max_pages;
   int32_t tpp_shift;       // log2 of the tiles of a page
   int32_t N_kv, B;
+  Divisor by_N_kv, by_B;
   PagedLayout lay;
 
-  // Tile `tile` of sequence b's KV head h in layer l, the same for all lanes; nullptr where the table has no page of the
-  // pool for it.
-  __device__ __forceinline__ char *tile(int64_t l, int b, int h, int64_t tile) const {
-    const int64_t slot = tile >> tpp_shift;
-    if (slot >= max_pages) return nullptr;
-    const int page = __builtin_amdgcn_readfirstlane(table[(int64_t)b * max_pages + slot]);
-    if (page < 0 || page >= n_pages) return nullptr;
-    return (char *)pool + ((((l * n_pages + page) * N_kv + h) << tpp_shift) + (tile & ((1 << tpp_shift) - 1))) * (int64_t)lay.tile_bytes;
+  __device__ __forceinline__ UnitPlace place(uint32_t u) const {
+    const uint32_t lb = by_N_kv.of(u), l = by_B.of(lb);
+    return {l, (int)(lb - l * (uint32_t)B), (int)(u - lb * (uint32_t)N_kv)};
+  }
+  __device__ __forceinline__ UnitPages unit(const UnitPlace &w) const {
+    const int64_t part = (int64_t)lay.tile_bytes << tpp_shift;   // a KV head's part of a page (at most 1024 tiles of 33 KB)
+    return {(char *)pool + ((int64_t)w.l * n_pages * N_kv + w.h) * part, part * N_kv, table + (int64_t)w.b * max_pages,
+            (uint32_t)n_pages, max_pages, tpp_shift, lay.tile_bytes};
   }
 };
 
@@ -74,6 +115,7 @@ struct PagedWriteArgs {
   int64_t most;                   // most rows of a sequence in this call
   int64_t units;
   int32_t T, tiles;               // tiles: blocks per unit, those of `most` rows
+  Divisor by_tiles;
 };
 hipError_t launch_paged_write(int dtype, int bits, const PagedWriteArgs &a, hipStream_t st);
 
@@ -85,6 +127,7 @@ struct PagedReadArgs {
   int64_t most;                   // most rows of a sequence in this call
   int64_t units;
   int32_t T, ld, tiles;           // tiles: blocks per unit
+  Divisor by_tiles;
 };
 hipError_t launch_paged_read(int dtype, int bits, const PagedReadArgs &a, hipStream_t st);
 
@@ -107,8 +150,15 @@ struct PagedDecodeArgs {
   int64_t S;                         // most rows of a sequence in pages
   int64_t units;
   int32_t T, G, cap, n_split, tiles_per_split, groups;   // groups: blocks of 16 query heads per unit
+  int32_t step;                      // tiles a wave takes at once, at most what its kernel can
+  Divisor by_split, by_groups;
   float scale_log2;
 };
+// Tiles that a wave of the call's kernel can take at once.
+inline int paged_decode_step(int bits, int G, int T) {
+  if (bits == 4) return G <= 4 && T <= 64 ? 4 : G <= 8 && T <= 96 ? 2 : 1;
+  return bits == 8 && G <= 8 && T <= 64 ? 2 : 1;
+}
 hipError_t launch_paged_decode(int dtype, int bits, const PagedDecodeArgs &a, hipStream_t st);
 hipError_t launch_paged_decode_bf16(int bits, const PagedDecodeArgs &a, hipStream_t st);
 hipError_t launch_paged_decode_f32(int bits, const PagedDecodeArgs &a, hipStream_t st);

@@ -157,10 +157,12 @@ struct State {
 __device__ __forceinline__ void softmax_step(f32x4 (&z)[4], int rows, int h, float scale, State &st) {
   if (__any(rows < kTile)) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < 4; ++j) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (16 * j + 4 * h + i >= rows) z[j][i] = -INFINITY;
+      __builtin_amdgcn_sched_barrier(0);   // (sixteen comparisons ahead of their use would take 32 scalar registers)
+    }
   }
   float mx = -INFINITY;
 #pragma unroll
@@ -195,69 +197,83 @@ struct Query {
   float x[8];
   __device__ __forceinline__ float operator[](int e) const { return x[e]; }
   __device__ __forceinline__ void set(int e, float v) { x[e] = v; }
+  __device__ __forceinline__ void keep() {}
 };
 template <>
 struct Query<THK_BF16> {
   bf16x8 x;
   __device__ __forceinline__ float operator[](int e) const { return (float)x[e]; }
   __device__ __forceinline__ void set(int e, float v) { x[e] = (__bf16)v; }   // exact: v is an element
+  // stays as it is from tile to tile: left to itself the compiler widens it once, in front of the loop, into twice the registers
+  __device__ __forceinline__ void keep() {
+    u32x4 w = __builtin_bit_cast(u32x4, x);
+    asm("" : "+v"(w));
+    x = __builtin_bit_cast(bf16x8, w);
+  }
 };
 
-// CL tiles of pages: t[x] is the x-th (any tile again where there is none).  `rows`: rows that count in the lane's own tile,
-// `own`: that tile's first byte, cls: its place x.
+// CL tiles of pages in a wave's registers: t[x] is the x-th (any of the others again where there is none), `own` the lane's
+// own, of which `rows` rows count.  The keys and the two halves of the values (by rows) are loaded on their own, each as soon as
+// what was loaded two parts before has been used: two of the three parts are in registers or on their way at any time.
 template <int DT, int BITS, int NST, int CL>
-__device__ __forceinline__ void page_tiles(const char *const (&t)[CL], const char *own, int cls, int rows, const PagedLayout &lay,
-                                           int m, int h, const Query<DT> (&q)[NST], float scale, const Mantissa &cst, State &st) {
+struct Tiles {
   using F = Format<DT, BITS>;
-  constexpr int NP = DT == THK_BF16 ? 2 : 4;
+  static constexpr int NP = F::kCodes ? (DT == THK_BF16 ? 2 : 4) : 1, EB = Elem<DT>::EB;
   u32x4 kc[CL][NST][F::NC], kp[F::kCodes ? NST : 1][NP];
-#pragma unroll
-  for (int s = 0; s < NST; ++s) {
-    const int c = min(4 * s + h, lay.chunks - 1);   // groups past the last meet zeros of the query
-    if constexpr (F::kCodes) load_pairs<DT>(own + (uint32_t)(lay.k_params + c * 8 * 2 * Elem<DT>::EB), kp[s]);
-    const uint32_t at = (uint32_t)(c * 64 * F::UB + m * 16);   // 32 bits behind a scalar base
-#pragma unroll
-    for (int x = 0; x < CL; ++x)
-#pragma unroll
-      for (int k = 0; k < F::NC; ++k) kc[x][s][k] = ld_stream((const u32x4 *)(t[x] + at + k * 256));
+  u32x4 vc[CL][4][F::NC], vp[F::kCodes ? 4 : 1][NP];
+
+  // 16 bytes of a tile at a lane's offset and a scalar one, through a resource in scalar registers (read once: not to be
+  // cached).  bytes: the tile's, or 0: zeros, and memory is not asked
+  static __device__ __forceinline__ u32x4 load_cell(const char *t, int bytes, int lane_off, int off) {
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)t, (short)0, bytes, 0x00027000);
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane_off, off, 2));
   }
-  // with codes all of the values are asked for here as well
-  // (the parameters after the first product where the registers would not hold them: 128 channels, two tiles)
-  constexpr bool kLate = NST == 4 && CL == 2;
-  u32x4 vc[F::kCodes ? CL : 1][F::kCodes ? 4 : 1][F::NC], vp[F::kCodes ? 4 : 1][NP];
-  const uint32_t pat = (uint32_t)(lay.v_params + h * 2 * 8 * 2 * Elem<DT>::EB);
-  auto load_value_pairs = [&] {
+  __device__ __forceinline__ void load_keys(const char *const (&t)[CL], int bytes, const char *own, const PagedLayout &lay, int m, int h) {
 #pragma unroll
-    for (int gh = 0; gh < 4; ++gh) load_pairs<DT>(own + pat + ((gh >> 1) * 8 + (gh & 1)) * 8 * 2 * Elem<DT>::EB, vp[gh]);
-  };
-  if constexpr (F::kCodes) {
-    if constexpr (!kLate) load_value_pairs();
-    const uint32_t at = (uint32_t)(lay.v_codes + h * 2 * 64 * F::UB + m * 16);
-#pragma unroll
-    for (int gh = 0; gh < 4; ++gh) {
-      const int grp = (gh >> 1) * 8 + (gh & 1);   // the lane's group, less 2 h
+    for (int s = 0; s < NST; ++s) {
+      const int c = min(4 * s + h, lay.chunks - 1);   // groups past the last meet zeros of the query
+      if constexpr (F::kCodes) load_pairs<DT>(own + (uint32_t)(lay.k_params + c * 8 * 2 * EB), kp[s]);
 #pragma unroll
       for (int x = 0; x < CL; ++x)
 #pragma unroll
-        for (int k = 0; k < F::NC; ++k) vc[x][gh][k] = ld_stream((const u32x4 *)(t[x] + at + grp * 64 * F::UB + k * 256));
+        for (int k = 0; k < F::NC; ++k) kc[x][s][k] = load_cell(t[x], bytes, c * 64 * F::UB + m * 16 + k * 256, 0);
     }
   }
-  // the operands are made where they are used, not ahead: they would not fit into the registers
-  __builtin_amdgcn_sched_barrier(0);
-  f32x4 zx[CL][4] = {};
-  float off = 0.f;
+  // (G0, G1: which halves of the rows)
+  template <int G0 = 0, int G1 = 2>
+  __device__ __forceinline__ void load_values(const char *const (&t)[CL], int bytes, const char *own, const PagedLayout &lay, int m, int h) {
+    const uint32_t pat = (uint32_t)(lay.v_params + h * 2 * 8 * 2 * EB);
 #pragma unroll
-  for (int s = 0; s < NST; ++s) {
+    for (int gh = 2 * G0; gh < 2 * G1; ++gh) {
+      const int grp = (gh >> 1) * 8 + (gh & 1);   // the lane's group, less 2 h
+      if constexpr (F::kCodes) load_pairs<DT>(own + pat + grp * 8 * 2 * EB, vp[gh]);
+#pragma unroll
+      for (int x = 0; x < CL; ++x)
+#pragma unroll
+        for (int k = 0; k < F::NC; ++k) vc[x][gh][k] = load_cell(t[x], bytes, h * 2 * 64 * F::UB + m * 16 + k * 256, lay.v_codes + grp * 64 * F::UB);
+    }
+  }
+
+  // z: the logits of the lane's tile (less the scale); cls: its place
+  __device__ __forceinline__ void logits(const Query<DT> (&q)[NST], int cls, const Mantissa &cst, f32x4 (&z)[4]) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) z[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if constexpr (F::kFp32) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float x[8];
+      for (int s = 0; s < NST; ++s)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(kc[0][s][2 * j + (e >> 2)][e & 3]);
-        zx[0][j] = mfma16_f32(x, q[s].x, zx[0][j]);
-      }
-    } else {
-      bf16x8 b[F::NTK];
+        for (int j = 0; j < 4; ++j) {
+          float x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(kc[0][s][2 * j + (e >> 2)][e & 3]);
+          z[j] = mfma16_f32(x, q[s].x, z[j]);
+        }
+      return;
+    }
+    bf16x8 b[NST][F::NTK];
+    float off = 0.f;
+#pragma unroll
+    for (int s = 0; s < NST; ++s) {
       if constexpr (F::kCodes) {
         float qs[8];
 #pragma unroll
@@ -268,97 +284,88 @@ __device__ __forceinline__ void page_tiles(const char *const (&t)[CL], const cha
           qs[e] = q[s][e] * (sc * (1.f / F::kTimes));
           off = fmaf(qs[e], -F::kBias, off);
         }
-        split_terms<F::NTK>(qs, b);
-      } else {
-        b[0] = q[s].x;
+        split_terms<F::NTK>(qs, b[s]);
+      } else if constexpr (DT == THK_BF16) {
+        b[s][0] = q[s].x;
       }
+    }
 #pragma unroll
-      for (int x = 0; x < CL; ++x)
+    for (int x = 0; x < CL; ++x) {
+      // operands are made where they are used, not ahead: they would not fit into the registers
+      if constexpr (F::kCodes) __builtin_amdgcn_sched_barrier(0);
+      f32x4 zx[4] = {};
+#pragma unroll
+      for (int s = 0; s < NST; ++s)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const bf16x8 a = operand<DT, BITS>(kc[x][s], j, cst);
 #pragma unroll
-          for (int n = 0; n < F::NTK; ++n) zx[x][j] = mfma16(a, b[n], zx[x][j]);
+          for (int n = 0; n < F::NTK; ++n) zx[j] = mfma16(a, b[s][n], zx[j]);
         }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[j][i] = x == 0 || cls == x ? zx[j][i] : z[j][i];
+    }
+    if constexpr (F::kCodes) {
+      off = sum_quarters(off);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) z[j] += off;
     }
   }
-  __builtin_amdgcn_sched_barrier(0);
-  if constexpr (F::kCodes && kLate) load_value_pairs();
-  f32x4 z[4];
+
+  // the values of half G of the rows with the weights w
+  template <int G>
+  __device__ __forceinline__ void add_values(const f32x4 (&w)[4], int cls, const Mantissa &cst, State &st) const {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    z[j] = zx[0][j];
+    for (int half = 0; half < 2; ++half) {
+      constexpr int g = G;
+      const int gh = 2 * g + half;
+      if constexpr (F::kCodes) __builtin_amdgcn_sched_barrier(0);
+      float p[8];
 #pragma unroll
-    for (int x = 1; x < CL; ++x)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) z[j][i] = cls == x ? zx[x][j][i] : z[j][i];
-  }
-  if constexpr (F::kCodes) {
-    off = sum_quarters(off);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) z[j] += off;
-  }
-  softmax_step(z, rows, h, scale, st);
-#pragma unroll
-  for (int gh = 0; gh < 4; ++gh) {
-    const int g = gh >> 1, half = gh & 1;
-    if constexpr (F::kCodes) __builtin_amdgcn_sched_barrier(0);
-    float p[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = z[2 * g + (e >> 2)][e & 3];
-    if constexpr (F::kCodes) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float sc, lo;
-        pair_of<DT>(vp[gh], e, sc, lo);
-        st.off[half] = fmaf(p[e], lo, st.off[half]);
-        p[e] *= sc * (1.f / F::kTimes);
-        st.off[half] = fmaf(p[e], -F::kBias, st.off[half]);
-      }
-      bf16x8 b[F::NTV];
-      split_terms<F::NTV>(p, b);
-#pragma unroll
-      for (int x = 0; x < CL; ++x) {
-        bf16x8 bx[F::NTV];
-#pragma unroll
-        for (int n = 0; n < F::NTV; ++n) {
-          u32x4 w = __builtin_bit_cast(u32x4, b[n]);
-          if constexpr (CL > 1) w &= cls == x ? 0xffffffffu : 0u;
-          bx[n] = __builtin_bit_cast(bf16x8, w);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const bf16x8 a = operand<DT, BITS>(vc[x][gh], i, cst);
-#pragma unroll
-          for (int n = 0; n < F::NTV; ++n) st.acc[4 * half + i] = mfma16(a, bx[n], st.acc[4 * half + i]);
-        }
-      }
-    } else {
-      u32x4 vw[F::NC];
-#pragma unroll
-      for (int k = 0; k < F::NC; ++k)
-        vw[k] = ld_stream((const u32x4 *)(t[0] + (uint32_t)(lay.v_codes + ((g * 4 + h) * 2 + half) * 64 * F::UB + m * 16) + k * 256));
+      for (int e = 0; e < 8; ++e) p[e] = w[2 * g + (e >> 2)][e & 3];
       if constexpr (F::kFp32) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float x[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(vw[2 * i + (e >> 2)][e & 3]);
+          for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(vc[0][gh][2 * i + (e >> 2)][e & 3]);
           st.acc[4 * half + i] = mfma16_f32(x, p, st.acc[4 * half + i]);
         }
       } else {
+        if constexpr (F::kCodes) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float sc, lo;
+            pair_of<DT>(vp[gh], e, sc, lo);
+            st.off[half] = fmaf(p[e], lo, st.off[half]);
+            p[e] *= sc * (1.f / F::kTimes);
+            st.off[half] = fmaf(p[e], -F::kBias, st.off[half]);
+          }
+        }
         bf16x8 b[F::NTV];
         split_terms<F::NTV>(p, b);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const bf16x8 a = operand<DT, BITS>(vw, i, cst);
+        for (int x = 0; x < CL; ++x) {
+          bf16x8 bx[F::NTV];
 #pragma unroll
-          for (int n = 0; n < F::NTV; ++n) st.acc[4 * half + i] = mfma16(a, b[n], st.acc[4 * half + i]);
+          for (int n = 0; n < F::NTV; ++n) {
+            u32x4 t = __builtin_bit_cast(u32x4, b[n]);
+            if constexpr (CL > 1) t &= cls == x ? 0xffffffffu : 0u;
+            bx[n] = __builtin_bit_cast(bf16x8, t);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bf16x8 a = operand<DT, BITS>(vc[x][gh], i, cst);
+#pragma unroll
+            for (int n = 0; n < F::NTV; ++n) st.acc[4 * half + i] = mfma16(a, bx[n], st.acc[4 * half + i]);
+          }
         }
       }
     }
   }
-}
+};
 
 // A tile of the tail: rows of 128 elements one after another, `rows` of them in use.  Rows past that are not read, since
 // what lies there may be anything: the last row in use stands in for their keys (their logits are masked) and zeros for
@@ -433,84 +440,152 @@ __device__ __forceinline__ void tail_tile(const char *kt, const char *vt, int ro
 constexpr int kRec = kD + 2;     // floats of a split record: max, sum, acc[128]
 constexpr int kAccPitch = kD + 4;
 
-// One block: up to 16 query heads of one unit, one piece of the sequence's tiles, shared out among its four waves.  The
-// sequence's last piece takes the tail as well.
+// As many zeros as a tile of codes has bytes at most (128 channels, 8 bits, fp32 parameters).
+static __device__ __align__(16) const char no_parameters[32 * 64 * 8 + 256 * 8] = {};
+
+// An address that came out of memory, as one of device memory (and not of whichever memory it may be).
+__device__ __forceinline__ const char *as_global(const void *p) {
+  return (const char *)(__attribute__((address_space(1))) const char *)(uintptr_t)p;
+}
+
+// The lane's number, asked for anew.
+__device__ __forceinline__ int lane_again() {
+  int x;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
+  return x;
+}
+
+// One block: up to 16 query heads of one unit, one piece of the sequence's tiles, which its four waves take in turn, `step`
+// tiles at a time.  The sequence's last piece takes the tail as well.
+// Short calls are a chain of trips to memory; everything that depends on the arguments alone is asked for first: the
+// lengths, the page of the wave's first tiles, the query, the index list.
 template <int DT, int BITS, int NST, int CL>
-__global__ __launch_bounds__(256, DT == THK_F32 && BITS != 0 ? 1 : 2) void k_paged_decode(PagedDecodeArgs a) {
+__global__ __launch_bounds__(256, DT == THK_F32 ? 1 : 2) void k_paged_decode(PagedDecodeArgs a) {
   using E = Elem<DT>;
+  using F = Format<DT, BITS>;
   constexpr int EB = E::EB, QP = kD * EB + 16, HC = 16 / CL;   // HC: heads of a class
-  __shared__ __align__(16) union {
-    struct { char q[HC * QP]; int16_t idx[kD]; } in;
-    struct { float acc[4][16][kAccPitch], ml[4][16][2]; } out;
-  } lds;
+  constexpr int QN = HC * (kD * EB / 16) / 256 > 0 ? HC * (kD * EB / 16) / 256 : 1;   // 16-byte pieces of the query per thread
+  __shared__ __align__(16) char q_lds[HC * QP];
+  __shared__ __align__(16) int16_t idx_lds[kD];
+  __shared__ __align__(16) float acc_lds[4][16][kAccPitch];
+  __shared__ f32x2 ml_lds[4][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, h = lane >> 4;
   const int cls = m / HC, hd = m % HC;
-  const int sp = blockIdx.x % (uint32_t)a.n_split;
-  const int64_t ug = blockIdx.x / (uint32_t)a.n_split;
-  const int hg = (int)(ug % a.groups);
-  const int64_t u = ug / a.groups;
-  const int hk = (int)(u % a.p.N_kv), b = (int)(u / a.p.N_kv % a.p.B);
-  const int64_t l = u / a.p.N_kv / a.p.B;
-  const int heads = min(16, a.G - 16 * hg);
-  const int64_t head0 = u * a.G + 16 * hg;   // of all query heads of the call: a unit's are neighbours
-  const int np = (int)min((int64_t)max(a.s_pages[b], 0), a.S);
-  const int nt = a.s_tail != nullptr ? min(max(a.s_tail[b], 0), a.cap) : 0;
+  // (a grid has fewer than 2^24 blocks)
+  const uint32_t ug = a.by_split.of(blockIdx.x), sp = blockIdx.x - ug * (uint32_t)a.n_split;
+  const uint32_t u = a.by_groups.of(ug), hg = ug - u * (uint32_t)a.groups;
+  const UnitPlace place = a.p.place(u);
+  const int b = place.b;
+  const UnitPages pages = a.p.unit(place);
+  // the wave's tiles: t0 + wave * step + x, x < step, then 4 * step on
+  const int t0 = (int)min((int64_t)sp * a.tiles_per_split, (int64_t)INT32_MAX / kTile);
+  int it = t0 + wave * a.step;
+  int page[CL];   // the next tiles' table entries
+#pragma unroll
+  for (int x = 0; x < CL; ++x) page[x] = pages.page_of(it + x);
+  const int s_pages = scalar_load(a.s_pages, b), s_tail = a.s_tail != nullptr ? scalar_load(a.s_tail, b) : 0;
+  const int heads = min(16, a.G - 16 * (int)hg);
+  const int64_t head0 = (int64_t)u * a.G + 16 * hg;   // of all query heads of the call: a unit's are neighbours
+  const int64_t most = a.S;
+
+  u32x4 qr[QN];   // (heads that are not there: the last one again, zeros later)
+#pragma unroll
+  for (int i = 0; i < QN; ++i) {
+    const int n = (tid + 256 * i) / (kD * EB / 16), c = (tid + 256 * i) % (kD * EB / 16);
+    qr[i] = *(const u32x4 *)((const char *)a.q + (head0 + min(n, heads - 1)) * kD * EB + c * 16);
+  }
+  const int channel = a.idx[(size_t)u * a.T + min(tid, a.T - 1)];
+
+  // (a place without a tile has another one's address; where there is none at all, nothing is read but parameters, and these
+  // from the zeros: they meet weights of zero, which must not meet what else memory holds)
+  struct Where { const char *t[CL], *own; int rows, bytes; };
+  auto where = [&](int it, int end, int np) {
+    Where w;
+    const char *any = nullptr;
+#pragma unroll
+    for (int x = 0; x < CL; ++x) {
+      w.t[x] = x < a.step && it + x < end ? pages.in_page(page[x], it + x) : nullptr;
+      if (w.t[x] != nullptr) any = w.t[x];
+    }
+    w.bytes = any != nullptr ? pages.tile_bytes : 0;
+    if (any == nullptr) any = no_parameters;
+    w.rows = 0;
+    w.own = any;
+#pragma unroll
+    for (int x = 0; x < CL; ++x) {
+      if (cls == x && w.t[x] != nullptr) {
+        w.rows = np - (it + x) * kTile;
+        w.own = w.t[x];
+      }
+      if (w.t[x] == nullptr) w.t[x] = any;
+    }
+    return w;
+  };
+  const int np = (int)min((int64_t)max(s_pages, 0), most), nt = min(max(s_tail, 0), a.cap);
   const int tiles = (np + kTile - 1) / kTile;
   const int last = max(0, (tiles - 1) / a.tiles_per_split);   // the piece that also takes the tail
-  if (sp > last) return;
-  const int t0 = sp * a.tiles_per_split, t1 = min(tiles, t0 + a.tiles_per_split);
+  if ((int)sp > last) return;
+  const int t1 = min(tiles, t0 + a.tiles_per_split);
 
-  for (int i = tid; i < HC * (kD * EB / 16); i += 256) {
-    const int n = i / (kD * EB / 16), c = i % (kD * EB / 16);
-    u32x4 x = {0, 0, 0, 0};
-    if (n < heads) x = *(const u32x4 *)((const char *)a.q + (head0 + n) * kD * EB + c * 16);
-    *(u32x4 *)(lds.in.q + n * QP + c * 16) = x;
+  auto ask_pages = [&](int t) {
+#pragma unroll
+    for (int x = 0; x < CL; ++x) page[x] = pages.page_of(t + x);
+  };
+  Where cur = where(it, t1, np);
+  ask_pages(it + 4 * a.step);
+  Tiles<DT, BITS, NST, CL> tl;
+  tl.load_keys(cur.t, cur.bytes, cur.own, a.p.lay, m, h);
+  tl.template load_values<0, 1>(cur.t, cur.bytes, cur.own, a.p.lay, m, h);
+#pragma unroll
+  for (int i = 0; i < QN; ++i) {
+    const int n = (tid + 256 * i) / (kD * EB / 16), c = (tid + 256 * i) % (kD * EB / 16);
+    if (n < HC) *(u32x4 *)(q_lds + n * QP + c * 16) = n < heads ? qr[i] : u32x4{0, 0, 0, 0};
   }
-  if (tid < kD) lds.in.idx[tid] = tid < a.T ? a.idx[u * a.T + tid] & (kD - 1) : -1;
+  // kept channels past the last one are the row's padding, which holds zeros
+  if (tid < kD) idx_lds[tid] = (int16_t)(tid < a.T ? channel & (kD - 1) : kD);
+  if (tid < HC) *(u32x4 *)(q_lds + tid * QP + kD * EB) = u32x4{0, 0, 0, 0};
   __syncthreads();
-  const char *const q_row = lds.in.q + hd * QP;
+  const char *const q_row = q_lds + hd * QP;
   Query<DT> q[NST];
 #pragma unroll
-  for (int s = 0; s < NST; ++s)
+  for (int s = 0; s < NST; ++s) {
+    int16_t c[8];
+    *(u32x4 *)c = *(const u32x4 *)(idx_lds + 32 * s + 8 * h);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int c = lds.in.idx[32 * s + 8 * h + e];
-      q[s].set(e, c >= 0 ? E::load1(q_row, c) : 0.f);
-    }
+    for (int e = 0; e < 8; ++e) q[s].set(e, E::load1(q_row, c[e]));
+  }
   const Mantissa cst;
   State st;
 #pragma unroll
   for (int i = 0; i < 8; ++i) st.acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   st.off[0] = st.off[1] = st.l = 0.f;
   st.m = -INFINITY;
-  const int each = (t1 - t0 + 3) / 4, w0 = t0 + wave * each, w1 = min(t1, w0 + each);   // this wave's tiles
-  for (int it = w0; it < w1; it += CL) {
-    const char *t[CL], *any = nullptr;
+  for (; it < t1; it += 4 * a.step) {
+    const Where next = where(it + 4 * a.step, t1, np);
+    ask_pages(it + 8 * a.step);
+    f32x4 z[4];
 #pragma unroll
-    for (int x = 0; x < CL; ++x) {
-      t[x] = it + x < w1 ? a.p.tile(l, b, hk, it + x) : nullptr;
-      if (t[x] != nullptr) any = t[x];
-    }
-    if (any == nullptr) continue;
-    int rows = 0;
-    const char *own = any;
-#pragma unroll
-    for (int x = 0; x < CL; ++x) {
-      if (cls == x && t[x] != nullptr) {
-        rows = np - (it + x) * kTile;
-        own = t[x];
-      }
-      if (t[x] == nullptr) t[x] = any;
-    }
-    page_tiles<DT, BITS, NST, CL>(t, own, cls, rows, a.p.lay, m, h, q, a.scale_log2, cst, st);
+    for (int s = 0; s < NST; ++s) q[s].keep();
+    tl.logits(q, cls, cst, z);
+    tl.template load_values<1, 2>(cur.t, cur.bytes, cur.own, a.p.lay, m, h);
+    softmax_step(z, cur.rows, h, a.scale_log2, st);
+    tl.template add_values<0>(z, cls, cst, st);
+    tl.load_keys(next.t, next.bytes, next.own, a.p.lay, m, h);
+    tl.template add_values<1>(z, cls, cst, st);
+    tl.template load_values<0, 1>(next.t, next.bytes, next.own, a.p.lay, m, h);
+    cur = next;
   }
-  if (sp == last)
-    for (int r0 = wave * kTile; r0 < nt; r0 += 4 * kTile) {
-      const size_t at = ((size_t)u * a.cap + r0) * kD * EB;
-      tail_tile<DT>((const char *)a.kt + at, (const char *)a.vt + at, min(kTile, nt - r0), cls == 0, m, h, q_row, a.scale_log2, st);
+  // The arguments that are needed from here on are asked for here: kept through the loop they cost it registers.
+  const PagedDecodeArgs *late = (const PagedDecodeArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(late));
+  const PagedDecodeArgs &z = *late;
+  if ((int)sp == last)
+    for (int r0 = (3 - wave) * kTile; r0 < nt; r0 += 4 * kTile) {   // (the last wave has the fewest pages)
+      const size_t at = ((size_t)u * z.cap + r0) * kD * EB;
+      tail_tile<DT>(as_global(z.kt) + at, as_global(z.vt) + at, min(kTile, nt - r0), cls == 0, m, h, q_row, z.scale_log2, st);
     }
   st.l = sum_quarters(st.l);
-  if constexpr (BITS != 0) {
+  if constexpr (F::kCodes) {
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const float off = sum_quarters(st.off[half]);
@@ -518,102 +593,125 @@ __global__ __launch_bounds__(256, DT == THK_F32 && BITS != 0 ? 1 : 2) void k_pag
       for (int i = 0; i < 4; ++i) st.acc[4 * half + i] += off;
     }
   }
-  __syncthreads();   // the query's part of LDS is not needed any more
-  if (h == 0) {
-    lds.out.ml[wave][m][0] = st.m;
-    lds.out.ml[wave][m][1] = st.l;
+  const int lane2 = lane_again(), m2 = lane2 & 15, h2 = lane2 >> 4;   // (not kept through the loops: registers)
+  if (m2 % HC < heads) {
+    if (h2 == 0) ml_lds[wave][m2] = f32x2{st.m, st.l};
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *(f32x4 *)&acc_lds[wave][m2][64 * half + 16 * h2 + 4 * r] =
+            f32x4{st.acc[4 * half][r], st.acc[4 * half + 1][r], st.acc[4 * half + 2][r], st.acc[4 * half + 3][r]};
   }
-#pragma unroll
-  for (int half = 0; half < 2; ++half)
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      *(f32x4 *)&lds.out.acc[wave][m][64 * half + 16 * h + 4 * r] =
-          f32x4{st.acc[4 * half][r], st.acc[4 * half + 1][r], st.acc[4 * half + 2][r], st.acc[4 * half + 3][r]};
   __syncthreads();
-  // the states of a head, joined: four waves, CL columns of each
-  const int n = tid >> 4, c0 = (tid & 15) * 8;
-  if (n >= heads) return;
-  float M = -INFINITY, L = 0.f, o[8] = {};
+  // the states of a head, joined by a wave, two channels a lane: four waves, CL columns of each
+  for (int n = wave; n < heads; n += 4) {
+    f32x2 ml[4][CL], x[4][CL];
+    float M = -INFINITY, L = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; ++w)
+    for (int w = 0; w < 4; ++w)
 #pragma unroll
-    for (int x = 0; x < CL; ++x) M = fmaxf(M, lds.out.ml[w][x * HC + n][0]);
+      for (int c = 0; c < CL; ++c) {
+        ml[w][c] = ml_lds[w][c * HC + n];
+        x[w][c] = *(const f32x2 *)&acc_lds[w][c * HC + n][2 * lane2];
+        M = fmaxf(M, ml[w][c][0]);
+      }
+    f32x2 o = {0.f, 0.f};
 #pragma unroll
-  for (int w = 0; w < 4; ++w)
+    for (int w = 0; w < 4; ++w)
 #pragma unroll
-    for (int x = 0; x < CL; ++x) {
-      const int col = x * HC + n;
-      const float mw = lds.out.ml[w][col][0], wgt = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - M);
-      L = fmaf(lds.out.ml[w][col][1], wgt, L);
-#pragma unroll
-      for (int c = 0; c < 8; ++c) o[c] = fmaf(lds.out.acc[w][col][c0 + c], wgt, o[c]);
+      for (int c = 0; c < CL; ++c) {
+        const float wgt = ml[w][c][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w][c][0] - M);
+        L = fmaf(ml[w][c][1], wgt, L);
+        o += x[w][c] * wgt;
+      }
+    if (last == 0) {
+      const float inv = L > 0.f ? 1.f / L : 0.f;   // no rows at all: zeros
+      E::store2((void *)as_global(z.out), (head0 + n) * kD + 2 * lane2, o[0] * inv, o[1] * inv);
+    } else {
+      float *const rec = (float *)as_global(z.ws) + ((head0 + n) * z.n_split + sp) * kRec;
+      *(f32x2 *)(rec + 2 + 2 * lane2) = o;
+      if (lane2 == 0) *(f32x2 *)rec = f32x2{M, L};
     }
-  if (last > 0) {
-    float *const rec = a.ws + ((head0 + n) * a.n_split + sp) * kRec;
-    if (c0 == 0) *(f32x2 *)rec = f32x2{M, L};
-#pragma unroll
-    for (int c = 0; c < 8; c += 2) *(f32x2 *)(rec + 2 + c0 + c) = f32x2{o[c], o[c + 1]};
-    return;
   }
-  const float inv = L > 0.f ? 1.f / L : 0.f;   // no rows at all: zeros
-#pragma unroll
-  for (int c = 0; c < 8; c += 2) E::store2(a.out, (head0 + n) * kD + c0 + c, o[c] * inv, o[c + 1] * inv);
 }
 
-// The pieces of one query head, joined: a block per head, its four waves take the records in turn, a lane two channels.
-template <int DT>
-__global__ __launch_bounds__(256) void k_paged_merge(PagedDecodeArgs a) {
-  __shared__ f32x2 part[4][kWave], part_ml[4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t head = blockIdx.x;
-  const int b = (int)(head / a.G / a.p.N_kv % a.p.B);
-  const int np = (int)min((int64_t)max(a.s_pages[b], 0), a.S);
+// The pieces of one query head, joined: a block per head, its NW waves take eight records at a time, a lane two channels.
+template <int DT, int NW>
+__global__ __launch_bounds__(64 * NW) void k_paged_merge(PagedDecodeArgs a) {
+  constexpr int P = 8;
+  __shared__ f32x2 part[NW][kWave], part_ml[NW];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t head = blockIdx.x, lb = head / ((uint32_t)a.G * (uint32_t)a.p.N_kv);
+  const int b = (int)(lb - a.p.by_B.of(lb) * (uint32_t)a.p.B);
+  const int np = (int)min((int64_t)max(scalar_load(a.s_pages, b), 0), a.S);
   const int pieces = max(0, ((np + kTile - 1) / kTile - 1) / a.tiles_per_split) + 1;
   if (pieces == 1) return;   // written by the piece itself
-  const float *const rec = a.ws + head * a.n_split * kRec;
+  const float *const rec = a.ws + (int64_t)head * a.n_split * kRec;
   float M = -INFINITY, L = 0.f;
   f32x2 o = {0.f, 0.f};
-  for (int i = wave; i < pieces; i += 4) {
-    const f32x2 ml = *(const f32x2 *)(rec + i * kRec), x = *(const f32x2 *)(rec + i * kRec + 2 + 2 * lane);
-    const float M_new = fmaxf(M, ml[0]);
-    const float keep = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - M_new), wgt = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - M_new);
+  for (int i0 = wave * P; i0 < pieces; i0 += NW * P) {
+    f32x2 ml[P], x[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) {   // (records past the last: the last one again, without weight)
+      const float *const r = rec + (int64_t)min(i0 + i, pieces - 1) * kRec;
+      ml[i] = *(const f32x2 *)r;
+      x[i] = *(const f32x2 *)(r + 2 + 2 * lane);
+    }
+    float M_new = M;
+#pragma unroll
+    for (int i = 0; i < P; ++i) M_new = fmaxf(M_new, ml[i][0]);
+    const float keep = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - M_new);
     M = M_new;
-    L = L * keep + ml[1] * wgt;
-    o = o * keep + x * wgt;
+    L *= keep;
+    o *= keep;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const float wgt = i0 + i >= pieces || ml[i][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[i][0] - M);
+      L = fmaf(ml[i][1], wgt, L);
+      o += x[i] * wgt;
+    }
   }
   part[wave][lane] = o;
   if (lane == 0) part_ml[wave] = f32x2{M, L};
   __syncthreads();
   if (wave != 0) return;
-  for (int w = 0; w < 4; ++w) M = fmaxf(M, part_ml[w][0]);
+#pragma unroll
+  for (int w = 0; w < NW; ++w) M = fmaxf(M, part_ml[w][0]);
   L = 0.f;
   o = f32x2{0.f, 0.f};
-  for (int w = 0; w < 4; ++w) {
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
     const f32x2 ml = part_ml[w];
     const float wgt = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - M);
-    L += ml[1] * wgt;
+    L = fmaf(ml[1], wgt, L);
     o += part[w][lane] * wgt;
   }
   const float inv = L > 0.f ? 1.f / L : 0.f;
-  Elem<DT>::store2(a.out, head * kD + 2 * lane, o[0] * inv, o[1] * inv);
+  Elem<DT>::store2(a.out, (int64_t)head * kD + 2 * lane, o[0] * inv, o[1] * inv);
 }
 
-template <int DT, int BITS, int CL>
+template <int DT, int BITS>
 void (*kernel_of(int T))(PagedDecodeArgs) {
-  return T <= 64 ? k_paged_decode<DT, BITS, 2, CL> : T <= 96 ? k_paged_decode<DT, BITS, 3, CL> : k_paged_decode<DT, BITS, 4, CL>;
+  return T <= 64 ? k_paged_decode<DT, BITS, 2, 1> : T <= 96 ? k_paged_decode<DT, BITS, 3, 1> : k_paged_decode<DT, BITS, 4, 1>;
 }
 
 template <int DT, int BITS>
 hipError_t launch(const PagedDecodeArgs &a, hipStream_t st) {
   clear_stale_hip_error();
   void (*k)(PagedDecodeArgs);
-  if constexpr (BITS == 4) k = a.G <= 8 ? kernel_of<DT, BITS, 2>(a.T) : kernel_of<DT, BITS, 1>(a.T);
-  else k = kernel_of<DT, BITS, 1>(a.T);
+  const int CL = a.step > 2 ? 4 : a.step;   // (tiles past a.step are columns without weight: no more of them than needed)
+  if constexpr (BITS == 4) k = CL == 4 ? k_paged_decode<DT, BITS, 2, 4> : CL == 2 ? (a.T <= 64 ? k_paged_decode<DT, BITS, 2, 2> : k_paged_decode<DT, BITS, 3, 2>) : kernel_of<DT, BITS>(a.T);
+  else if constexpr (BITS == 8) k = CL == 2 ? k_paged_decode<DT, BITS, 2, 2> : kernel_of<DT, BITS>(a.T);
+  else k = kernel_of<DT, BITS>(a.T);
   PagedDecodeArgs copy = a;
   void *args[] = {&copy};
   hipError_t e = launch_main_kernel((const void *)k, dim3((unsigned)(a.units * a.groups * a.n_split)), dim3(256), args, 0, st);
   if (e != hipSuccess || a.n_split == 1) return e;
-  hipLaunchKernelGGL(k_paged_merge<DT>, dim3((unsigned)(a.units * a.G)), dim3(256), 0, st, a);
+  const dim3 heads((unsigned)(a.units * a.G));
+  if (a.n_split <= 8) hipLaunchKernelGGL((k_paged_merge<DT, 1>), heads, dim3(64), 0, st, a);
+  else if (a.n_split <= 32) hipLaunchKernelGGL((k_paged_merge<DT, 4>), heads, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_paged_merge<DT, 8>), heads, dim3(512), 0, st, a);
   return hipGetLastError();
 }
 

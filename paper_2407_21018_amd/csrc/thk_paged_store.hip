@@ -159,15 +159,14 @@ __global__ __launch_bounds__(256) void k_paged_write(PagedWriteArgs a) {
   __shared__ __align__(16) char rows_lds[kTile * PITCH];
   __shared__ __align__(16) int16_t idx_lds[kD];
   const int tid = threadIdx.x, m = tid & 15, grp = tid >> 4;
-  const int64_t u = blockIdx.x / (uint32_t)a.tiles;
-  const int t = blockIdx.x % (uint32_t)a.tiles;
-  const int h = (int)(u % a.p.N_kv), b = (int)(u / a.p.N_kv % a.p.B);
-  const int64_t l = u / a.p.N_kv / a.p.B;
-  const int64_t n = min((int64_t)a.n_rows[b], a.most);
-  const int64_t row0 = a.row0 != nullptr ? a.row0[b] : 0;
+  const uint32_t u = a.by_tiles.of(blockIdx.x), t = blockIdx.x - u * (uint32_t)a.tiles;   // (a grid has fewer than 2^24 blocks)
+  const UnitPlace place = a.p.place(u);
+  const int b = place.b;
+  const int64_t n = min((int64_t)scalar_load(a.n_rows, b), a.most);
+  const int64_t row0 = a.row0 != nullptr ? scalar_load(a.row0, b) : 0;
   const int64_t r0 = (int64_t)t * kTile;
   if (r0 >= n || row0 < 0 || (row0 & (kTile - 1)) != 0) return;
-  char *const dst = a.p.tile(l, b, h, row0 / kTile + t);
+  char *const dst = a.p.unit(place).tile(row0 / kTile + t);
   if (dst == nullptr) return;
   const int rows = (int)min(n - r0, (int64_t)kTile);
   const size_t base = ((size_t)u * a.src_rows + r0) * kD;   // first element of the tile's rows
@@ -272,16 +271,16 @@ __global__ __launch_bounds__(256) void k_paged_read(PagedReadArgs a) {
   constexpr int EB = E::EB;
   __shared__ __align__(16) char rows_lds[16 + kTile * kD * EB];
   const int tid = threadIdx.x, m = tid & 15, grp = tid >> 4;
-  const int64_t u = blockIdx.x / (uint32_t)a.tiles;
-  const int h = (int)(u % a.p.N_kv), b = (int)(u / a.p.N_kv % a.p.B);
-  const int64_t l = u / a.p.N_kv / a.p.B;
-  const int64_t row0 = a.row0 != nullptr ? a.row0[b] : 0;
+  const uint32_t u = a.by_tiles.of(blockIdx.x);
+  const UnitPlace place = a.p.place(u);
+  const int b = place.b;
+  const int64_t row0 = a.row0 != nullptr ? scalar_load(a.row0, b) : 0;
   if (row0 < 0) return;
-  const int64_t end = row0 + min((int64_t)a.n_rows[b], a.most);
-  const int64_t t = row0 / kTile + blockIdx.x % (uint32_t)a.tiles;
+  const int64_t end = row0 + min((int64_t)scalar_load(a.n_rows, b), a.most);
+  const int64_t t = row0 / kTile + (blockIdx.x - u * (uint32_t)a.tiles);
   const int64_t lo = max(row0, t * kTile), hi = min(end, (t + 1) * kTile);   // rows of this block
   if (lo >= hi) return;
-  const char *const src = a.p.tile(l, b, h, t);
+  const char *const src = a.p.unit(place).tile(t);
   if (src == nullptr) return;
   const size_t out_row = (size_t)u * a.out_rows + (lo - row0);
   const int first = (int)(lo - t * kTile), rows = (int)(hi - lo);
