@@ -729,14 +729,52 @@ PagedPool paged_pool(const thk_shape *s, const thk_pages *p, const void *pool, c
 
 int64_t paged_groups(const thk_shape *s) { return ceil_div(s->N_q / s->N_kv, 16); }
 
-// Pieces of whole tiles; by the length's bound, since the lengths are on the device.
-Split paged_split(const thk_shape *s) {
+// Pieces of whole tiles; by the length's bound, since the lengths are on the device.  Unless the caller says how many, the
+// count with the least estimated time of a few.  With k = tiles of a piece, R = 2 blocks resident on a compute unit (fp32: 1) and
+// L = blocks on the fullest one, in us:
+//     sum over rounds of l = R (in the last round what is left) blocks of
+//         max(l k t_tile, steps t_step) + t_block (l + 1) / 2                     steps: of a wave through its piece
+//     + [more than one piece] t_merge + t_record * records / 1000
+// t_tile = t0 + t1 T / 64, with (1 + f) or (1 + 2 f) of it where a wave takes two tiles or one at once: codes are bound by the
+// vector unit.  Fitted to 820 random shapes (all formats, 1 to 64 sequences, 65 to 131072 rows, up to 18 counts each): the
+// chosen count takes 0.5 % (element pages) to 2.5 % (4 bits) longer than the best one on average, 1.5x at worst; as many
+// blocks as are resident at once, 9 to 10 % longer.
+struct PagedTimes { double t0, t1, f, t_step, t_block, t_merge, t_record; };
+constexpr PagedTimes kPagedTimes[2][3] = {   // [fp32, bf16][elements, 4 bits, 8 bits]
+    {{0.831, 0.615, 0, 4.292, 6.566, 2.971, 0.084}, {0.288, 0.239, 0.074, 1.163, 8.175, 2.675, 0.574}, {0.274, 0.268, 0.129, 1.970, 9.844, 1.678, 0.044}},
+    {{0.286, 0.344, 0, 0.097, 3.799, 2.940, 0.429}, {0.124, 0.069, 0.827, 3.527, 3.235, 3.238, 0.042}, {0.121, 0.265, 0.088, 3.521, 3.777, 2.944, 0.332}}};
+
+Split paged_split(const thk_shape *s, int bits) {
   const int64_t tiles = ceil_div(s->S, kTile), blocks = units_of(s) * paged_groups(s);
-  int64_t n = s->n_split;
-  if (n == 0) n = std::min(ceil_div(4 * kCUs, blocks), ceil_div(tiles, 4));
-  const int64_t per = ceil_div(tiles, std::max<int64_t>(n, 1));
-  return {(int)ceil_div(tiles, per), per * kTile};
+  auto pieces = [&](int64_t n) {
+    const int64_t per = ceil_div(tiles, n);
+    return Split{(int)ceil_div(tiles, per), per * kTile};
+  };
+  if (s->n_split != 0) return pieces(s->n_split);
+  const PagedTimes &t = kPagedTimes[s->dtype == THK_BF16][bits == 0 ? 0 : bits == 4 ? 1 : 2];
+  const int resident = s->dtype == THK_BF16 ? 2 : 1, most_step = paged_decode_step(bits, s->N_q / s->N_kv, s->T);
+  const double t_tile = t.t0 + t.t1 * s->T / 64;
+  Split best = pieces(1);
+  double least = 0;
+  for (const int n : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128}) {
+    if (n > 1 && (n > tiles || blocks * n > 16 * kCUs)) break;
+    const Split sp = pieces(n);
+    const int64_t per = sp.rows / kTile, step = std::min<int64_t>(most_step, ceil_div(per, 4)), steps = ceil_div(per, 4 * step);
+    const int64_t on_cu = ceil_div(blocks * sp.n, kCUs), rounds = on_cu / resident;
+    const double tile = t_tile * (step >= 3 ? 1 : step == 2 ? 1 + t.f : 1 + 2 * t.f);
+    auto round = [&](int64_t l) { return std::max((double)(l * per) * tile, (double)steps * t.t_step) + t.t_block * 0.5 * (double)(l + 1); };
+    double time = (double)rounds * round(resident);
+    if (on_cu > rounds * resident) time += round(on_cu - rounds * resident);
+    if (sp.n > 1) time += t.t_merge + t.t_record * 1e-3 * (double)((int64_t)s->L * s->B * s->N_q * sp.n);
+    if (n == 1 || time < least) {
+      best = sp;
+      least = time;
+    }
+  }
+  return best;
 }
+// The most pieces that a call of the shape may have, whatever its pages hold.
+int paged_most_pieces(const thk_shape *s) { return std::max({paged_split(s, 0).n, paged_split(s, 4).n, paged_split(s, 8).n}); }
 size_t paged_ws_bytes(const thk_shape *s, int n_split) {
   return n_split == 1 ? 16 : (size_t)s->L * s->B * s->N_q * n_split * (kD + 2) * sizeof(float);
 }
@@ -800,7 +838,7 @@ int32_t thk_default_split(const thk_shape *s, int32_t op) {
   if (op == THK_OP_DECODE) return decode_split(&t).n;
   if (op == THK_OP_SCORE) return score_split(&t, units_of(&t)).n;
   if (op == THK_OP_PRUNE) return score_split(&t, prune_group_units(&t)).n;
-  if (op == THK_OP_DECODE_PAGED) return t.S <= INT32_MAX ? paged_split(&t).n : 0;
+  if (op == THK_OP_DECODE_PAGED) return t.S <= INT32_MAX ? paged_most_pieces(&t) : 0;
   if (op == THK_OP_SCORE_VALUE || op == THK_OP_PRUNE_VALUE) return (t.S_obs >= 1 && t.S_obs <= t.S) ? value_split(&t).n : 0;
   return 0;
 }
@@ -837,7 +875,7 @@ size_t thk_workspace_bytes(const thk_shape *s, int32_t op) {
       return sp.n == 1 ? 16 : decode_ws_bytes(s, sp.n);
     }
     case THK_OP_DECODE_PAGED:
-      return s->S <= INT32_MAX ? paged_ws_bytes(s, paged_split(s).n) : 0;
+      return s->S <= INT32_MAX ? paged_ws_bytes(s, paged_most_pieces(s)) : 0;
     case THK_OP_SCORE_VALUE:
       if (s->S_obs < 1 || (int64_t)s->S_obs > s->S) return 0;
       return value_ws_bytes(s, value_split(s).n);
@@ -1327,7 +1365,7 @@ thk_status thk_decode_attn_paged(const thk_shape *s, const thk_pages *p, const v
   if (!aligned16(q) || !aligned16(pool) || !aligned16(idx) || !aligned16(out) || !aligned4(table) || !aligned4(s_pages) ||
       (tail && (!aligned16(k_tail) || !aligned16(v_tail) || !aligned4(s_tail))))
     return THK_ERR_ALIGN;
-  const Split sp = paged_split(s);
+  const Split sp = paged_split(s, p->bits);
   if (sp.n > 1 && (ws == nullptr || !aligned16(ws) || ws_bytes < paged_ws_bytes(s, sp.n))) return THK_ERR_WORKSPACE;
   PagedDecodeArgs a;
   a.p = paged_pool(s, p, pool, table);
