@@ -745,27 +745,27 @@ constexpr PagedTimes kPagedTimes[2][3] = {   // [fp32, bf16][elements, 4 bits, 8
     {{0.286, 0.344, 0, 0.097, 3.799, 2.940, 0.429}, {0.124, 0.069, 0.827, 3.527, 3.235, 3.238, 0.042}, {0.121, 0.265, 0.088, 3.521, 3.777, 2.944, 0.332}}};
 
 Split paged_split(const thk_shape *s, int bits) {
-  const int64_t tiles = ceil_div(s->S, kTile), blocks = units_of(s) * paged_groups(s);
-  auto pieces = [&](int64_t n) {
-    const int64_t per = ceil_div(tiles, n);
-    return Split{(int)ceil_div(tiles, per), per * kTile};
+  const int64_t tiles64 = ceil_div(s->S, kTile), blocks = units_of(s) * paged_groups(s);   // S < 2^31
+  const uint32_t tiles = (uint32_t)tiles64;
+  auto pieces = [&](uint32_t n) {
+    const uint32_t per = (tiles + n - 1) / n;
+    return Split{(int)((tiles + per - 1) / per), (int64_t)per * kTile};
   };
-  if (s->n_split != 0) return pieces(s->n_split);
+  if (s->n_split != 0) return pieces((uint32_t)s->n_split);
+  if (tiles == 1 || blocks > 8 * kCUs) return pieces(1);
   const PagedTimes &t = kPagedTimes[s->dtype == THK_BF16][bits == 0 ? 0 : bits == 4 ? 1 : 2];
-  const int resident = s->dtype == THK_BF16 ? 2 : 1, most_step = paged_decode_step(bits, s->N_q / s->N_kv, s->T);
-  const double t_tile = t.t0 + t.t1 * s->T / 64;
+  const uint32_t resident = s->dtype == THK_BF16 ? 2 : 1, most_step = (uint32_t)paged_decode_step(bits, s->N_q / s->N_kv, s->T);
+  const double t_tile = t.t0 + t.t1 * s->T / 64, t_records = t.t_record * 1e-3 * (double)((int64_t)s->L * s->B * s->N_q);
   Split best = pieces(1);
   double least = 0;
-  for (const int n : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128}) {
+  for (const uint32_t n : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 40, 48, 64, 96, 128}) {
     if (n > 1 && (n > tiles || blocks * n > 16 * kCUs)) break;
     const Split sp = pieces(n);
-    const int64_t per = sp.rows / kTile, step = std::min<int64_t>(most_step, ceil_div(per, 4)), steps = ceil_div(per, 4 * step);
-    const int64_t on_cu = ceil_div(blocks * sp.n, kCUs), rounds = on_cu / resident;
+    const uint32_t per = (uint32_t)(sp.rows / kTile), step = std::min(most_step, (per + 3) / 4), steps = (per + 4 * step - 1) / (4 * step);
+    const uint32_t on_cu = ((uint32_t)blocks * (uint32_t)sp.n + kCUs - 1) / kCUs, rounds = on_cu / resident, rest = on_cu % resident;
     const double tile = t_tile * (step >= 3 ? 1 : step == 2 ? 1 + t.f : 1 + 2 * t.f);
-    auto round = [&](int64_t l) { return std::max((double)(l * per) * tile, (double)steps * t.t_step) + t.t_block * 0.5 * (double)(l + 1); };
-    double time = (double)rounds * round(resident);
-    if (on_cu > rounds * resident) time += round(on_cu - rounds * resident);
-    if (sp.n > 1) time += t.t_merge + t.t_record * 1e-3 * (double)((int64_t)s->L * s->B * s->N_q * sp.n);
+    auto round = [&](uint32_t l) { return std::max((double)l * per * tile, steps * t.t_step) + t.t_block * 0.5 * (l + 1); };
+    const double time = rounds * round(resident) + (rest != 0 ? round(rest) : 0) + (sp.n > 1 ? t.t_merge + t_records * sp.n : 0);
     if (n == 1 || time < least) {
       best = sp;
       least = time;
