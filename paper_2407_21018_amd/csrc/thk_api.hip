@@ -707,7 +707,7 @@ thk_status check_pages(const thk_shape *s, const thk_pages *p) {
   if (p->bits != 0 && p->bits != 4 && p->bits != 8) return THK_ERR_UNSUPPORTED;
   if (p->page_rows < kTile || p->page_rows > 65536 || (p->page_rows & (p->page_rows - 1)) != 0) return THK_ERR_SHAPE;
   if (p->max_pages < 1 || (int64_t)p->max_pages * p->page_rows > INT32_MAX) return THK_ERR_SHAPE;
-  if (p->n_pages < 1 || p->n_pages > INT32_MAX || s->S > INT32_MAX) return THK_ERR_SHAPE;
+  if (p->n_pages < 1 || p->n_pages > INT32_MAX || s->S > INT32_MAX - kTile) return THK_ERR_SHAPE;
   return THK_OK;
 }
 int64_t paged_rows(const thk_shape *s, const thk_pages *p) { return std::min<int64_t>(s->S, (int64_t)p->max_pages * p->page_rows); }
@@ -775,8 +775,9 @@ Split paged_split(const thk_shape *s, int bits) {
 }
 // The most pieces that a call of the shape may have, whatever its pages hold.
 int paged_most_pieces(const thk_shape *s) { return std::max({paged_split(s, 0).n, paged_split(s, 4).n, paged_split(s, 8).n}); }
-size_t paged_ws_bytes(const thk_shape *s, int n_split) {
-  return n_split == 1 ? 16 : (size_t)s->L * s->B * s->N_q * n_split * (kD + 2) * sizeof(float);
+int64_t paged_blocks(const thk_shape *s, int n_split) { return units_of(s) * paged_groups(s) * (n_split == 1 ? 1 : n_split + 1); }
+size_t paged_ws_bytes(const thk_shape *s, int n_split) {   // a record per block and head of it
+  return n_split == 1 ? 16 : (size_t)paged_blocks(s, n_split) * std::min(s->N_q / s->N_kv, 16) * (kD + 2) * sizeof(float);
 }
 
 size_t score_ws_bytes(const thk_shape *s, int64_t units) {
@@ -838,7 +839,7 @@ int32_t thk_default_split(const thk_shape *s, int32_t op) {
   if (op == THK_OP_DECODE) return decode_split(&t).n;
   if (op == THK_OP_SCORE) return score_split(&t, units_of(&t)).n;
   if (op == THK_OP_PRUNE) return score_split(&t, prune_group_units(&t)).n;
-  if (op == THK_OP_DECODE_PAGED) return t.S <= INT32_MAX ? paged_most_pieces(&t) : 0;
+  if (op == THK_OP_DECODE_PAGED) return t.S <= INT32_MAX - kTile ? paged_most_pieces(&t) : 0;
   if (op == THK_OP_SCORE_VALUE || op == THK_OP_PRUNE_VALUE) return (t.S_obs >= 1 && t.S_obs <= t.S) ? value_split(&t).n : 0;
   return 0;
 }
@@ -875,7 +876,7 @@ size_t thk_workspace_bytes(const thk_shape *s, int32_t op) {
       return sp.n == 1 ? 16 : decode_ws_bytes(s, sp.n);
     }
     case THK_OP_DECODE_PAGED:
-      return s->S <= INT32_MAX ? paged_ws_bytes(s, paged_most_pieces(s)) : 0;
+      return s->S <= INT32_MAX - kTile ? paged_ws_bytes(s, paged_most_pieces(s)) : 0;
     case THK_OP_SCORE_VALUE:
       if (s->S_obs < 1 || (int64_t)s->S_obs > s->S) return 0;
       return value_ws_bytes(s, value_split(s).n);
@@ -1375,13 +1376,18 @@ thk_status thk_decode_attn_paged(const thk_shape *s, const thk_pages *p, const v
   a.units = units_of(s);
   a.T = s->T; a.G = s->N_q / s->N_kv; a.cap = s_tail_cap;
   a.n_split = sp.n;
-  a.tiles_per_split = (int32_t)(sp.rows / kTile);
+  // Cut by the lengths where the call is long enough for it not to matter: the work of a batch of the longest ones, spread
+  // over the card, is 32 tiles a compute unit (some 10 us) or more.
+  const bool by_lengths = sp.n > 1 && (s->B > 1 || sp.rows >= 64 * kTile) && a.units * ceil_div(s->S, kTile) >= 32 * kCUs;
+  a.per = by_lengths ? 0 : (int32_t)(sp.rows / kTile);
   a.groups = (int32_t)paged_groups(s);
-  a.by_split = Divisor(sp.n);
+  a.cols = (int32_t)(a.units / s->B * a.groups);
+  a.by_cols = Divisor(a.cols);
   a.by_groups = Divisor(a.groups);
-  a.step = std::min(paged_decode_step(p->bits, a.G, a.T), (a.tiles_per_split + 3) / 4);   // no wave idle while another has two
+  a.by_split = Divisor(sp.n);
+  a.step = std::min(paged_decode_step(p->bits, a.G, a.T), (int32_t)((sp.rows / kTile + 3) / 4));   // no wave idle while another has two
   a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)s->D));
-  if ((uint64_t)a.units * a.groups > kMaxThreads / 256 / sp.n || (uint64_t)a.units * a.G > kMaxThreads / 256) return THK_ERR_SHAPE;
+  if ((uint64_t)paged_blocks(s, sp.n) > kMaxThreads / 256 || (uint64_t)a.units * a.G > kMaxThreads / 256) return THK_ERR_SHAPE;
   return failed(launch_paged_decode(s->dtype, p->bits, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
 }
 

@@ -146,14 +146,18 @@ struct PagedDecodeArgs {
   const int16_t *idx;
   const int32_t *s_pages, *s_tail;   // [B]; s_tail may be nullptr (no tail)
   void *out;
-  float *ws;                         // split records [head][n_split]: (max, sum, acc[128])
+  float *ws;                         // a record per block and head of it: (max, sum, acc[128])
   int64_t S;                         // most rows of a sequence in pages
   int64_t units;
-  int32_t T, G, cap, n_split, tiles_per_split, groups;   // groups: blocks of 16 query heads per unit
+  int32_t T, G, cap, groups;         // groups: blocks of 16 query heads per unit
+  int32_t n_split;                   // pieces per unit: at most, or where they go by the lengths on average
+  int32_t per;                       // tiles of a piece; 0: by the lengths
+  int32_t cols;                      // units and groups of one sequence: L * N_kv * groups
   int32_t step;                      // tiles a wave takes at once, at most what its kernel can
-  Divisor by_split, by_groups;
   float scale_log2;
+  Divisor by_cols, by_groups, by_split;
 };
+
 // Tiles that a wave of the call's kernel can take at once.
 inline int paged_decode_step(int bits, int G, int T) {
   if (bits == 4) return G <= 4 && T <= 64 ? 4 : G <= 8 && T <= 96 ? 2 : 1;

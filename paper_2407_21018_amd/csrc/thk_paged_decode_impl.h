@@ -156,11 +156,13 @@ struct State {
 // the state is brought to the new m.
 __device__ __forceinline__ void softmax_step(f32x4 (&z)[4], int rows, int h, float scale, State &st) {
   if (__any(rows < kTile)) {
+    int left = rows - 4 * h;
+    asm("" : "+v"(left));   // (else the sixteen rows' numbers are kept in registers through the loop)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (16 * j + 4 * h + i >= rows) z[j][i] = -INFINITY;
+        if (16 * j + i >= left) z[j][i] = -INFINITY;
       __builtin_amdgcn_sched_barrier(0);   // (sixteen comparisons ahead of their use would take 32 scalar registers)
     }
   }
@@ -455,6 +457,63 @@ __device__ __forceinline__ int lane_again() {
   return x;
 }
 
+// Inclusive sums over the wave's lanes.
+__device__ __forceinline__ uint32_t wave_sums(uint32_t x) {
+  x += __builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false);   // 1, 2, 4, 8 lanes up within a row of 16
+  x += __builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false);   // the row below's last lane
+  x += __builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false);   // the lower half's last lane
+  return x;
+}
+
+// How the sequences are cut into pieces: a sequence of t tiles (at least one: an empty one has an output too) into
+// ceil(t / per) of them.  Blocks are numbered by sequence, unit and group, piece.
+// With per given, every unit has n_split blocks, and those past its last piece have nothing to do.  A block knows its place
+// without the lengths.
+// Otherwise the cutting is done here, where the lengths are: per = all sequences' tiles over (sequences * n_split), pieces of
+// one sequence of equal size up to a tile; there are at most n_split + 1 per unit and group on average.  The block's place
+// takes a trip to memory and some 100 instructions (0.8 us), but the pieces do not depend on how far the host's bound of the
+// lengths is from the lengths, and one long sequence among short ones is cut into as many as it takes.
+struct Cutting {
+  const PagedDecodeArgs &a;
+  uint32_t per;   // tiles
+
+  __device__ __forceinline__ uint32_t tiles_of(int rows) const {
+    return (uint32_t)max((min(max(rows, 0), (int)a.S) + (kTile - 1)) / kTile, 1);   // S < 2^31 - 63
+  }
+  // of sequence b; 0 past the last
+  __device__ __forceinline__ uint32_t tiles_at(int b) const { return b < a.p.B ? tiles_of(a.s_pages[b]) : 0u; }
+  __device__ __forceinline__ uint32_t pieces_of(uint32_t tiles) const { return (tiles + per - 1) / per; }
+
+  __device__ __forceinline__ Cutting(const PagedDecodeArgs &args, int lane) : a(args), per((uint32_t)args.per) {
+    if (a.per != 0) return;
+    double total = 0;   // exact
+    for (int b0 = 0; b0 < a.p.B; b0 += kWave) total += (double)(uint32_t)__builtin_amdgcn_readlane((int)wave_sums(tiles_at(b0 + lane)), 63);
+    const double n = (double)a.p.B * (double)a.n_split;
+    per = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)ceil(total / n));
+  }
+  // The sequence in which the x-th of all sequences' pieces lies (b = B: none), and the number of pieces in front of it; or,
+  // with x < 0, the number of pieces in front of sequence b.  (Not with per given.)
+  __device__ __forceinline__ void find(int x, int &b, uint32_t &before, int lane) const {
+    before = 0;
+    for (int b0 = 0; b0 < a.p.B; b0 += kWave) {
+      const uint32_t n = pieces_of(tiles_at(b0 + lane)), sums = wave_sums(n);
+      // (lanes past the last sequence have no tiles and no pieces)
+      const unsigned long long past = x >= 0 ? __ballot(before + sums > (uint32_t)x) : (b < b0 + kWave ? ~0ull << (b - b0) : 0ull);
+      if (past != 0) {
+        const int i = __builtin_ctzll(past);
+        b = b0 + i;
+        before += (uint32_t)__builtin_amdgcn_readlane((int)(sums - n), i);
+        return;
+      }
+      before += (uint32_t)__builtin_amdgcn_readlane((int)sums, 63);
+    }
+    b = a.p.B;
+  }
+};
+
 // One block: up to 16 query heads of one unit, one piece of the sequence's tiles, which its four waves take in turn, `step`
 // tiles at a time.  The sequence's last piece takes the tail as well.
 // Short calls are a chain of trips to memory; everything that depends on the arguments alone is asked for first: the
@@ -472,22 +531,39 @@ __global__ __launch_bounds__(256, DT == THK_F32 ? 1 : 2) void k_paged_decode(Pag
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, h = lane >> 4;
   const int cls = m / HC, hd = m % HC;
   // (a grid has fewer than 2^24 blocks)
-  const uint32_t ug = a.by_split.of(blockIdx.x), sp = blockIdx.x - ug * (uint32_t)a.n_split;
-  const uint32_t u = a.by_groups.of(ug), hg = ug - u * (uint32_t)a.groups;
-  const UnitPlace place = a.p.place(u);
-  const int b = place.b;
-  const UnitPages pages = a.p.unit(place);
+  const Cutting cut(a, lane);
+  int b;
+  uint32_t col, sp, share, n;   // n: pieces of the unit, once its length is known
+  if (a.per != 0) {
+    const uint32_t x = a.by_split.of(blockIdx.x);
+    sp = blockIdx.x - x * (uint32_t)a.n_split;
+    b = (int)a.by_cols.of(x);
+    col = x - (uint32_t)b * (uint32_t)a.cols;
+    share = (uint32_t)a.per;
+    n = 0;
+  } else {
+    uint32_t before;
+    cut.find((int)a.by_cols.of(blockIdx.x), b, before, lane);
+    if (b >= a.p.B) return;   // more blocks than pieces
+    const uint32_t all = cut.tiles_of(scalar_load(a.s_pages, b)), at = blockIdx.x - before * (uint32_t)a.cols;
+    n = cut.pieces_of(all);
+    col = at / n;
+    sp = at - col * n;
+    share = (all + n - 1) / n;
+  }
+  const int s_pages = scalar_load(a.s_pages, b), s_tail = a.s_tail != nullptr ? scalar_load(a.s_tail, b) : 0;
+  const uint32_t lh = a.by_groups.of(col), hg = col - lh * (uint32_t)a.groups;
+  const uint32_t l = a.p.by_N_kv.of(lh), hk = lh - l * (uint32_t)a.p.N_kv;
+  const uint32_t u = (l * (uint32_t)a.p.B + (uint32_t)b) * (uint32_t)a.p.N_kv + hk;
+  const UnitPages pages = a.p.unit({l, b, (int)hk});
   // the wave's tiles: t0 + wave * step + x, x < step, then 4 * step on
-  const int t0 = (int)min((int64_t)sp * a.tiles_per_split, (int64_t)INT32_MAX / kTile);
+  const int t0 = (int)min(sp * (uint64_t)share, (uint64_t)(INT32_MAX / kTile));   // (past the sequence's end: none)
   int it = t0 + wave * a.step;
   int page[CL];   // the next tiles' table entries
 #pragma unroll
   for (int x = 0; x < CL; ++x) page[x] = pages.page_of(it + x);
-  const int s_pages = scalar_load(a.s_pages, b), s_tail = a.s_tail != nullptr ? scalar_load(a.s_tail, b) : 0;
   const int heads = min(16, a.G - 16 * (int)hg);
   const int64_t head0 = (int64_t)u * a.G + 16 * hg;   // of all query heads of the call: a unit's are neighbours
-  const int64_t most = a.S;
-
   u32x4 qr[QN];   // (heads that are not there: the last one again, zeros later)
 #pragma unroll
   for (int i = 0; i < QN; ++i) {
@@ -521,11 +597,11 @@ __global__ __launch_bounds__(256, DT == THK_F32 ? 1 : 2) void k_paged_decode(Pag
     }
     return w;
   };
-  const int np = (int)min((int64_t)max(s_pages, 0), most), nt = min(max(s_tail, 0), a.cap);
-  const int tiles = (np + kTile - 1) / kTile;
-  const int last = max(0, (tiles - 1) / a.tiles_per_split);   // the piece that also takes the tail
-  if ((int)sp > last) return;
-  const int t1 = min(tiles, t0 + a.tiles_per_split);
+  const int np = min(max(s_pages, 0), (int)a.S), nt = min(max(s_tail, 0), a.cap);
+  const int t1 = min((np + kTile - 1) / kTile, t0 + (int)share);
+  if (n == 0) n = cut.pieces_of(cut.tiles_of(s_pages));
+  if (sp >= n) return;
+  const bool joined = n > 1, with_tail = sp + 1 == n;   // the last piece takes the tail
 
   auto ask_pages = [&](int t) {
 #pragma unroll
@@ -579,7 +655,9 @@ __global__ __launch_bounds__(256, DT == THK_F32 ? 1 : 2) void k_paged_decode(Pag
   const PagedDecodeArgs *late = (const PagedDecodeArgs *)__builtin_amdgcn_kernarg_segment_ptr();
   asm volatile("" : "+s"(late));
   const PagedDecodeArgs &z = *late;
-  if ((int)sp == last)
+  const int heads2 = min(16, z.G - 16 * (int)hg);
+  const int64_t head2 = (int64_t)u * z.G + 16 * hg;
+  if (with_tail)
     for (int r0 = (3 - wave) * kTile; r0 < nt; r0 += 4 * kTile) {   // (the last wave has the fewest pages)
       const size_t at = ((size_t)u * z.cap + r0) * kD * EB;
       tail_tile<DT>(as_global(z.kt) + at, as_global(z.vt) + at, min(kTile, nt - r0), cls == 0, m, h, q_row, z.scale_log2, st);
@@ -594,7 +672,7 @@ __global__ __launch_bounds__(256, DT == THK_F32 ? 1 : 2) void k_paged_decode(Pag
     }
   }
   const int lane2 = lane_again(), m2 = lane2 & 15, h2 = lane2 >> 4;   // (not kept through the loops: registers)
-  if (m2 % HC < heads) {
+  if (m2 % HC < heads2) {
     if (h2 == 0) ml_lds[wave][m2] = f32x2{st.m, st.l};
 #pragma unroll
     for (int half = 0; half < 2; ++half)
@@ -605,7 +683,7 @@ __global__ __launch_bounds__(256, DT == THK_F32 ? 1 : 2) void k_paged_decode(Pag
   }
   __syncthreads();
   // the states of a head, joined by a wave, two channels a lane: four waves, CL columns of each
-  for (int n = wave; n < heads; n += 4) {
+  for (int n = wave; n < heads2; n += 4) {
     f32x2 ml[4][CL], x[4][CL];
     float M = -INFINITY, L = 0.f;
 #pragma unroll
@@ -625,11 +703,11 @@ __global__ __launch_bounds__(256, DT == THK_F32 ? 1 : 2) void k_paged_decode(Pag
         L = fmaf(ml[w][c][1], wgt, L);
         o += x[w][c] * wgt;
       }
-    if (last == 0) {
+    if (!joined) {
       const float inv = L > 0.f ? 1.f / L : 0.f;   // no rows at all: zeros
-      E::store2((void *)as_global(z.out), (head0 + n) * kD + 2 * lane2, o[0] * inv, o[1] * inv);
+      E::store2((void *)as_global(z.out), (head2 + n) * kD + 2 * lane2, o[0] * inv, o[1] * inv);
     } else {
-      float *const rec = (float *)as_global(z.ws) + ((head0 + n) * z.n_split + sp) * kRec;
+      float *const rec = (float *)as_global(z.ws) + ((int64_t)blockIdx.x * min(z.G, 16) + n) * kRec;
       *(f32x2 *)(rec + 2 + 2 * lane2) = o;
       if (lane2 == 0) *(f32x2 *)rec = f32x2{M, L};
     }
@@ -642,19 +720,27 @@ __global__ __launch_bounds__(64 * NW) void k_paged_merge(PagedDecodeArgs a) {
   constexpr int P = 8;
   __shared__ f32x2 part[NW][kWave], part_ml[NW];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t head = blockIdx.x, lb = head / ((uint32_t)a.G * (uint32_t)a.p.N_kv);
-  const int b = (int)(lb - a.p.by_B.of(lb) * (uint32_t)a.p.B);
-  const int np = (int)min((int64_t)max(scalar_load(a.s_pages, b), 0), a.S);
-  const int pieces = max(0, ((np + kTile - 1) / kTile - 1) / a.tiles_per_split) + 1;
+  const uint32_t head = blockIdx.x, u = head / (uint32_t)a.G, n = head - u * (uint32_t)a.G;
+  const UnitPlace place = a.p.place(u);
+  int b = place.b;
+  const Cutting cut(a, lane);
+  const int pieces = (int)cut.pieces_of(cut.tiles_of(scalar_load(a.s_pages, b)));
   if (pieces == 1) return;   // written by the piece itself
-  const float *const rec = a.ws + (int64_t)head * a.n_split * kRec;
+  uint32_t before = (uint32_t)(b * a.n_split), blocks = (uint32_t)a.n_split;   // blocks of a unit and group
+  if (a.per == 0) {
+    cut.find(-1, b, before, lane);
+    blocks = (uint32_t)pieces;
+  }
+  const uint32_t col = (place.l * (uint32_t)a.p.N_kv + (uint32_t)place.h) * (uint32_t)a.groups + n / 16;
+  const int64_t stride = (int64_t)min(a.G, 16) * kRec;   // from piece to piece
+  const float *const rec = a.ws + (int64_t)(before * (uint32_t)a.cols + col * blocks) * stride + (n & 15) * kRec;
   float M = -INFINITY, L = 0.f;
   f32x2 o = {0.f, 0.f};
   for (int i0 = wave * P; i0 < pieces; i0 += NW * P) {
     f32x2 ml[P], x[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) {   // (records past the last: the last one again, without weight)
-      const float *const r = rec + (int64_t)min(i0 + i, pieces - 1) * kRec;
+      const float *const r = rec + min(i0 + i, pieces - 1) * stride;
       ml[i] = *(const f32x2 *)r;
       x[i] = *(const f32x2 *)(r + 2 + 2 * lane);
     }
@@ -706,7 +792,7 @@ hipError_t launch(const PagedDecodeArgs &a, hipStream_t st) {
   else k = kernel_of<DT, BITS>(a.T);
   PagedDecodeArgs copy = a;
   void *args[] = {&copy};
-  hipError_t e = launch_main_kernel((const void *)k, dim3((unsigned)(a.units * a.groups * a.n_split)), dim3(256), args, 0, st);
+  hipError_t e = launch_main_kernel((const void *)k, dim3((unsigned)(a.units * a.groups * (a.per == 0 ? a.n_split + 1 : a.n_split))), dim3(256), args, 0, st);
   if (e != hipSuccess || a.n_split == 1) return e;
   const dim3 heads((unsigned)(a.units * a.G));
   if (a.n_split <= 8) hipLaunchKernelGGL((k_paged_merge<DT, 1>), heads, dim3(64), 0, st, a);
