@@ -297,13 +297,15 @@ struct Tiles {
       if constexpr (F::kCodes) __builtin_amdgcn_sched_barrier(0);
       f32x4 zx[4] = {};
 #pragma unroll
-      for (int s = 0; s < NST; ++s)
+      for (int s = 0; s < NST; ++s) {
+        bf16x8 a[4];   // (an instruction waits for the one in front of it in its own sum: four sums in turn)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bf16x8 a = operand<DT, BITS>(kc[x][s], j, cst);
+        for (int j = 0; j < 4; ++j) a[j] = operand<DT, BITS>(kc[x][s], j, cst);
 #pragma unroll
-          for (int n = 0; n < F::NTK; ++n) zx[j] = mfma16(a, b[s][n], zx[j]);
-        }
+        for (int n = 0; n < F::NTK; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) zx[j] = mfma16(a[j], b[s][n], zx[j]);
+      }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -357,12 +359,13 @@ struct Tiles {
             if constexpr (CL > 1) t &= cls == x ? 0xffffffffu : 0u;
             bx[n] = __builtin_bit_cast(bf16x8, t);
           }
+          bf16x8 a[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const bf16x8 a = operand<DT, BITS>(vc[x][gh], i, cst);
+          for (int i = 0; i < 4; ++i) a[i] = operand<DT, BITS>(vc[x][gh], i, cst);
 #pragma unroll
-            for (int n = 0; n < F::NTV; ++n) st.acc[4 * half + i] = mfma16(a, bx[n], st.acc[4 * half + i]);
-          }
+          for (int n = 0; n < F::NTV; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st.acc[4 * half + i] = mfma16(a[i], bx[n], st.acc[4 * half + i]);
         }
       }
     }
