@@ -160,8 +160,8 @@ struct PagedDecodeArgs {
 
 // Tiles that a wave of the call's kernel can take at once.
 inline int paged_decode_step(int bits, int G, int T) {
-  if (bits == 4) return G <= 4 && T <= 64 ? 4 : G <= 8 && T <= 96 ? 2 : 1;
-  return bits == 8 && G <= 8 && T <= 64 ? 2 : 1;
+  if (bits == 4) return G <= 4 && T <= 96 ? 4 : G <= 8 ? 2 : 1;
+  return bits == 8 && G <= 8 && T <= 96 ? 2 : 1;
 }
 hipError_t launch_paged_decode(int dtype, int bits, const PagedDecodeArgs &a, hipStream_t st);
 hipError_t launch_paged_decode_bf16(int bits, const PagedDecodeArgs &a, hipStream_t st);

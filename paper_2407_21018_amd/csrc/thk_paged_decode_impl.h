@@ -34,6 +34,12 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// An address of device memory where the compiler does not see that it is one (it would load through the path that may also reach
+// LDS, whose loads are waited for all at once).
+#define THK_GLOBAL __attribute__((address_space(1)))
+typedef THK_GLOBAL char *GlobalPtr;
+__device__ __forceinline__ GlobalPtr as_global(const void *p) { return (GlobalPtr)(uintptr_t)p; }
+
 // Eight floats as NT bf16 terms that add up to them: each term is what the ones in front left over.
 template <int NT>
 __device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8 (&t)[NT]) {
@@ -129,9 +135,9 @@ __device__ __forceinline__ float max_quarters(float x) {
 
 // scale and minimum of the eight pairs at `par`
 template <int DT>
-__device__ __forceinline__ void load_pairs(const char *par, u32x4 (&w)[DT == THK_BF16 ? 2 : 4]) {
+__device__ __forceinline__ void load_pairs(GlobalPtr par, u32x4 (&w)[DT == THK_BF16 ? 2 : 4]) {
 #pragma unroll
-  for (int i = 0; i < (DT == THK_BF16 ? 2 : 4); ++i) w[i] = ((const u32x4 *)par)[i];
+  for (int i = 0; i < (DT == THK_BF16 ? 2 : 4); ++i) w[i] = ((const THK_GLOBAL u32x4 *)par)[i];
 }
 template <int DT>
 __device__ __forceinline__ void pair_of(const u32x4 (&w)[DT == THK_BF16 ? 2 : 4], int e, float &s, float &lo) {
@@ -220,7 +226,10 @@ struct Query<THK_BF16> {
 template <int DT, int BITS, int NST, int CL>
 struct Tiles {
   using F = Format<DT, BITS>;
-  static constexpr int NP = F::kCodes ? (DT == THK_BF16 ? 2 : 4) : 1, EB = Elem<DT>::EB;
+  static constexpr int NP = F::kCodes ? (DT == THK_BF16 ? 2 : 4) : 1;
+  static constexpr int kPairs = 8 * 2 * Elem<DT>::EB;   // bytes of a group's parameters
+  // an instruction waits for the one in front of it in its own sum: so many sums in turn (fewer where the registers are full)
+  static constexpr int kInTurn = F::kCodes && NST == 3 && CL * BITS == 16 ? 2 : 4;
   u32x4 kc[CL][NST][F::NC], kp[F::kCodes ? NST : 1][NP];
   u32x4 vc[CL][4][F::NC], vp[F::kCodes ? 4 : 1][NP];
 
@@ -230,25 +239,25 @@ struct Tiles {
     const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)t, (short)0, bytes, 0x00027000);
     return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane_off, off, 2));
   }
-  __device__ __forceinline__ void load_keys(const char *const (&t)[CL], int bytes, const char *own, const PagedLayout &lay, int m, int h) {
+  __device__ __forceinline__ void load_keys(const char *const (&t)[CL], int bytes, GlobalPtr own, const PagedLayout &lay, int m, int h) {
 #pragma unroll
     for (int s = 0; s < NST; ++s) {
-      const int c = min(4 * s + h, lay.chunks - 1);   // groups past the last meet zeros of the query
-      if constexpr (F::kCodes) load_pairs<DT>(own + (uint32_t)(lay.k_params + c * 8 * 2 * EB), kp[s]);
+      // group 4 s + h; those past the last are what lies behind the keys in the tile, and meet zeros of the query
+      if constexpr (F::kCodes) load_pairs<DT>(own + lay.k_params + s * 4 * kPairs, kp[s]);
 #pragma unroll
       for (int x = 0; x < CL; ++x)
 #pragma unroll
-        for (int k = 0; k < F::NC; ++k) kc[x][s][k] = load_cell(t[x], bytes, c * 64 * F::UB + m * 16 + k * 256, 0);
+        for (int k = 0; k < F::NC; ++k) kc[x][s][k] = load_cell(t[x], bytes, h * 64 * F::UB + m * 16 + k * 256, s * 256 * F::UB);
     }
   }
   // (G0, G1: which halves of the rows)
   template <int G0 = 0, int G1 = 2>
-  __device__ __forceinline__ void load_values(const char *const (&t)[CL], int bytes, const char *own, const PagedLayout &lay, int m, int h) {
-    const uint32_t pat = (uint32_t)(lay.v_params + h * 2 * 8 * 2 * EB);
+  __device__ __forceinline__ void load_values(const char *const (&t)[CL], int bytes, GlobalPtr own, const PagedLayout &lay, int m, int h) {
+    const GlobalPtr par = own + (uint32_t)(h * kPairs) + lay.v_params;   // (own has one h already)
 #pragma unroll
     for (int gh = 2 * G0; gh < 2 * G1; ++gh) {
       const int grp = (gh >> 1) * 8 + (gh & 1);   // the lane's group, less 2 h
-      if constexpr (F::kCodes) load_pairs<DT>(own + pat + grp * 8 * 2 * EB, vp[gh]);
+      if constexpr (F::kCodes) load_pairs<DT>(par + grp * kPairs, vp[gh]);
 #pragma unroll
       for (int x = 0; x < CL; ++x)
 #pragma unroll
@@ -298,13 +307,16 @@ struct Tiles {
       f32x4 zx[4] = {};
 #pragma unroll
       for (int s = 0; s < NST; ++s) {
-        bf16x8 a[4];   // (an instruction waits for the one in front of it in its own sum: four sums in turn)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) a[j] = operand<DT, BITS>(kc[x][s], j, cst);
+        for (int j0 = 0; j0 < 4; j0 += kInTurn) {
+          bf16x8 a[kInTurn];
 #pragma unroll
-        for (int n = 0; n < F::NTK; ++n)
+          for (int j = 0; j < kInTurn; ++j) a[j] = operand<DT, BITS>(kc[x][s], j0 + j, cst);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) zx[j] = mfma16(a[j], b[s][n], zx[j]);
+          for (int n = 0; n < F::NTK; ++n)
+#pragma unroll
+            for (int j = 0; j < kInTurn; ++j) zx[j0 + j] = mfma16(a[j], b[s][n], zx[j0 + j]);
+        }
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -321,6 +333,9 @@ struct Tiles {
   // the values of half G of the rows with the weights w
   template <int G>
   __device__ __forceinline__ void add_values(const f32x4 (&w)[4], int cls, const Mantissa &cst, State &st) const {
+    uint32_t mine[CL];
+#pragma unroll
+    for (int x = 0; x < CL; ++x) mine[x] = cls == x ? 0xffffffffu : 0u;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       constexpr int g = G;
@@ -353,19 +368,26 @@ struct Tiles {
 #pragma unroll
         for (int x = 0; x < CL; ++x) {
           bf16x8 bx[F::NTV];
+          asm("" : "+v"(mine[x]));   // (one register for the mask, not one for each word)
 #pragma unroll
           for (int n = 0; n < F::NTV; ++n) {
             u32x4 t = __builtin_bit_cast(u32x4, b[n]);
-            if constexpr (CL > 1) t &= cls == x ? 0xffffffffu : 0u;
+            if constexpr (CL > 1) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) t[i] &= mine[x];
+            }
             bx[n] = __builtin_bit_cast(bf16x8, t);
           }
-          bf16x8 a[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) a[i] = operand<DT, BITS>(vc[x][gh], i, cst);
+          for (int i0 = 0; i0 < 4; i0 += kInTurn) {
+            bf16x8 a[kInTurn];
 #pragma unroll
-          for (int n = 0; n < F::NTV; ++n)
+            for (int i = 0; i < kInTurn; ++i) a[i] = operand<DT, BITS>(vc[x][gh], i0 + i, cst);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) st.acc[4 * half + i] = mfma16(a[i], bx[n], st.acc[4 * half + i]);
+            for (int n = 0; n < F::NTV; ++n)
+#pragma unroll
+              for (int i = 0; i < kInTurn; ++i) st.acc[4 * half + i0 + i] = mfma16(a[i], bx[n], st.acc[4 * half + i0 + i]);
+          }
         }
       }
     }
@@ -376,7 +398,7 @@ struct Tiles {
 // what lies there may be anything: the last row in use stands in for their keys (their logits are masked) and zeros for
 // their values.  The columns of the first class attend to it; `mine`: this lane's is one of them.
 template <int DT>
-__device__ __forceinline__ void tail_tile(const char *kt, const char *vt, int rows, bool mine, int m, int h, const char *q_lds,
+__device__ __forceinline__ void tail_tile(GlobalPtr kt, GlobalPtr vt, int rows, bool mine, int m, int h, const char *q_lds,
                                           float scale, State &st) {
   using E = Elem<DT>;
   constexpr int EB = E::EB;
@@ -388,16 +410,16 @@ __device__ __forceinline__ void tail_tile(const char *kt, const char *vt, int ro
     for (int e = 0; e < 8; ++e) q[e] = E::load1(q_lds, 32 * s + 8 * h + e);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const char *const row = kt + (size_t)min(16 * j + m, rows - 1) * kD * EB + (32 * s + 8 * h) * EB;
+      const GlobalPtr row = kt + (size_t)min(16 * j + m, rows - 1) * kD * EB + (32 * s + 8 * h) * EB;
       if constexpr (DT == THK_F32) {
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = ((const float *)row)[e];
+        for (int e = 0; e < 8; ++e) x[e] = ((const THK_GLOBAL float *)row)[e];
         z[j] = mfma16_f32(x, q, z[j]);
       } else {
         bf16x8 b[1];
         split_terms<1>(q, b);
-        z[j] = mfma16(__builtin_bit_cast(bf16x8, *(const u32x4 *)row), b[0], z[j]);
+        z[j] = mfma16(__builtin_bit_cast(bf16x8, *(const THK_GLOBAL u32x4 *)row), b[0], z[j]);
       }
     }
   }
@@ -413,9 +435,9 @@ __device__ __forceinline__ void tail_tile(const char *kt, const char *vt, int ro
       for (int e = 0; e < 8; ++e) {
         p[e] = z[2 * g + (e >> 2)][e & 3];
         const int r = 32 * g + 16 * (e >> 2) + 4 * h + (e & 3);
-        const char *const row = vt + (size_t)min(r, rows - 1) * kD * EB + (64 * half + 4 * m) * EB;
+        const GlobalPtr row = vt + (size_t)min(r, rows - 1) * kD * EB + (64 * half + 4 * m) * EB;
 #pragma unroll
-        for (int i = 0; i < (DT == THK_F32 ? 4 : 2); ++i) x[e][i] = r < rows ? ((const uint32_t *)row)[i] : 0u;
+        for (int i = 0; i < (DT == THK_F32 ? 4 : 2); ++i) x[e][i] = r < rows ? ((const THK_GLOBAL uint32_t *)row)[i] : 0u;
       }
       if constexpr (DT == THK_F32) {
 #pragma unroll
@@ -448,10 +470,6 @@ constexpr int kAccPitch = kD + 4;
 // As many zeros as a tile of codes has bytes at most (128 channels, 8 bits, fp32 parameters).
 static __device__ __align__(16) const char no_parameters[32 * 64 * 8 + 256 * 8] = {};
 
-// An address that came out of memory, as one of device memory (and not of whichever memory it may be).
-__device__ __forceinline__ const char *as_global(const void *p) {
-  return (const char *)(__attribute__((address_space(1))) const char *)(uintptr_t)p;
-}
 
 // The lane's number, asked for anew.
 __device__ __forceinline__ int lane_again() {
@@ -577,7 +595,7 @@ __global__ __launch_bounds__(256, DT == THK_F32 ? 1 : 2) void k_paged_decode(Pag
 
   // (a place without a tile has another one's address; where there is none at all, nothing is read but parameters, and these
   // from the zeros: they meet weights of zero, which must not meet what else memory holds)
-  struct Where { const char *t[CL], *own; int rows, bytes; };
+  struct Where { const char *t[CL]; GlobalPtr own; int rows, bytes; };
   auto where = [&](int it, int end, int np) {
     Where w;
     const char *any = nullptr;
@@ -589,12 +607,12 @@ __global__ __launch_bounds__(256, DT == THK_F32 ? 1 : 2) void k_paged_decode(Pag
     w.bytes = any != nullptr ? pages.tile_bytes : 0;
     if (any == nullptr) any = no_parameters;
     w.rows = 0;
-    w.own = any;
+    w.own = as_global(any) + (uint32_t)(h * (8 * 2 * EB));
 #pragma unroll
     for (int x = 0; x < CL; ++x) {
       if (cls == x && w.t[x] != nullptr) {
         w.rows = np - (it + x) * kTile;
-        w.own = w.t[x];
+        w.own = as_global(w.t[x]) + (uint32_t)(h * (8 * 2 * EB));   // the lane's first group of parameters, less where they begin
       }
       if (w.t[x] == nullptr) w.t[x] = any;
     }
@@ -655,9 +673,10 @@ __global__ __launch_bounds__(256, DT == THK_F32 ? 1 : 2) void k_paged_decode(Pag
     cur = next;
   }
   // The arguments that are needed from here on are asked for here: kept through the loop they cost it registers.
-  const PagedDecodeArgs *late = (const PagedDecodeArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+  typedef const __attribute__((address_space(4))) PagedDecodeArgs LateArgs;
+  LateArgs *late = (LateArgs *)__builtin_amdgcn_kernarg_segment_ptr();
   asm volatile("" : "+s"(late));
-  const PagedDecodeArgs &z = *late;
+  LateArgs &z = *late;
   const int heads2 = min(16, z.G - 16 * (int)hg);
   const int64_t head2 = (int64_t)u * z.G + 16 * hg;
   if (with_tail)
@@ -780,19 +799,26 @@ __global__ __launch_bounds__(64 * NW) void k_paged_merge(PagedDecodeArgs a) {
   Elem<DT>::store2(a.out, (int64_t)head * kD + 2 * lane, o[0] * inv, o[1] * inv);
 }
 
-template <int DT, int BITS>
+// CL: tiles a wave takes at once, as paged_decode_step allows them for T channels.
+template <int DT, int BITS, int CL, int MOST_STEPS>
 void (*kernel_of(int T))(PagedDecodeArgs) {
-  return T <= 64 ? k_paged_decode<DT, BITS, 2, 1> : T <= 96 ? k_paged_decode<DT, BITS, 3, 1> : k_paged_decode<DT, BITS, 4, 1>;
+  if constexpr (MOST_STEPS == 4)
+    if (T > 96) return k_paged_decode<DT, BITS, 4, CL>;
+  return T <= 64 ? k_paged_decode<DT, BITS, 2, CL> : k_paged_decode<DT, BITS, 3, CL>;
 }
 
 template <int DT, int BITS>
 hipError_t launch(const PagedDecodeArgs &a, hipStream_t st) {
   clear_stale_hip_error();
-  void (*k)(PagedDecodeArgs);
+  void (*k)(PagedDecodeArgs) = nullptr;
   const int CL = a.step > 2 ? 4 : a.step;   // (tiles past a.step are columns without weight: no more of them than needed)
-  if constexpr (BITS == 4) k = CL == 4 ? k_paged_decode<DT, BITS, 2, 4> : CL == 2 ? (a.T <= 64 ? k_paged_decode<DT, BITS, 2, 2> : k_paged_decode<DT, BITS, 3, 2>) : kernel_of<DT, BITS>(a.T);
-  else if constexpr (BITS == 8) k = CL == 2 ? k_paged_decode<DT, BITS, 2, 2> : kernel_of<DT, BITS>(a.T);
-  else k = kernel_of<DT, BITS>(a.T);
+  if (CL == 1) k = kernel_of<DT, BITS, 1, 4>(a.T);
+  if constexpr (BITS == 4) {
+    if (CL == 2) k = kernel_of<DT, BITS, 2, 4>(a.T);
+    if (CL == 4) k = kernel_of<DT, BITS, 4, 3>(a.T);
+  }
+  if constexpr (BITS == 8)
+    if (CL == 2) k = kernel_of<DT, BITS, 2, 3>(a.T);
   PagedDecodeArgs copy = a;
   void *args[] = {&copy};
   hipError_t e = launch_main_kernel((const void *)k, dim3((unsigned)(a.units * a.groups * (a.per == 0 ? a.n_split + 1 : a.n_split))), dim3(256), args, 0, st);
