@@ -234,7 +234,8 @@ struct Tiles {
   u32x4 vc[CL][4][F::NC], vp[F::kCodes ? 4 : 1][NP];
 
   // 16 bytes of a tile at a lane's offset and a scalar one, through a resource in scalar registers (read once: not to be
-  // cached).  bytes: the tile's, or 0: zeros, and memory is not asked
+  // cached).  bytes: the tile's, or 0: zeros, and memory is not asked (the lane's offset alone is compared with them: with none
+  // every one is past the end, and with the tile's none can be)
   static __device__ __forceinline__ u32x4 load_cell(const char *t, int bytes, int lane_off, int off) {
     const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)t, (short)0, bytes, 0x00027000);
     return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane_off, off, 2));
@@ -394,71 +395,87 @@ struct Tiles {
   }
 };
 
-// A tile of the tail: rows of 128 elements one after another, `rows` of them in use.  Rows past that are not read, since
-// what lies there may be anything: the last row in use stands in for their keys (their logits are masked) and zeros for
-// their values.  The columns of the first class attend to it; `mine`: this lane's is one of them.
+// A tile of the tail: rows of 128 elements one after another, `rows` of them in use.  All of it is asked for at once, through
+// resources that end with the last row in use: what lies behind it may be anything, and is zeros here (the logits are masked).
+// (Whole offsets are the lanes': a scalar part takes no part in the comparison with a resource's end.)
+// The columns of the first class attend to it; `mine`: this lane's is one of them.
 template <int DT>
-__device__ __forceinline__ void tail_tile(GlobalPtr kt, GlobalPtr vt, int rows, bool mine, int m, int h, const char *q_lds,
+__device__ __forceinline__ void tail_tile(const char *kt, const char *vt, int rows, bool mine, int m, int h, const char *q_lds,
                                           float scale, State &st) {
   using E = Elem<DT>;
-  constexpr int EB = E::EB;
+  constexpr int EB = E::EB, RB = kD * EB, W = EB / 2;   // W: 16-byte pieces of eight channels
+  const auto kr = __builtin_amdgcn_make_buffer_rsrc((void *)kt, (short)0, rows * RB, 0x00027000);
+  const auto vr = __builtin_amdgcn_make_buffer_rsrc((void *)vt, (short)0, rows * RB, 0x00027000);
+  u32x4 kx[4][4][W];
+#pragma unroll
+  for (int s = 0; s < 4; ++s)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int w = 0; w < W; ++w)
+        kx[s][j][w] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, m * RB + 8 * h * EB + (s * 32 * EB + w * 16 + 16 * j * RB), 0, 0));
+  uint32_t vx[4][8][2 * W];   // four channels of each of the lane's eight rows, per half of the rows and of the channels
+#pragma unroll
+  for (int gh = 0; gh < 4; ++gh)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int at = 4 * h * RB + 4 * m * EB + ((gh & 1) * 64 * EB + (32 * (gh >> 1) + 16 * (e >> 2) + (e & 3)) * RB);
+      if constexpr (DT == THK_F32) {
+        const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, at, 0, 0));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vx[gh][e][i] = x[i];
+      } else {
+        const uint64_t x = __builtin_bit_cast(uint64_t, __builtin_amdgcn_raw_buffer_load_b64(vr, at, 0, 0));
+        vx[gh][e][0] = (uint32_t)x;
+        vx[gh][e][1] = (uint32_t)(x >> 32);
+      }
+    }
   f32x4 z[4] = {};
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
     float q[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) q[e] = E::load1(q_lds, 32 * s + 8 * h + e);
+    bf16x8 b[1];
+    if constexpr (DT == THK_BF16) split_terms<1>(q, b);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const GlobalPtr row = kt + (size_t)min(16 * j + m, rows - 1) * kD * EB + (32 * s + 8 * h) * EB;
       if constexpr (DT == THK_F32) {
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = ((const THK_GLOBAL float *)row)[e];
+        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(kx[s][j][e >> 2][e & 3]);
         z[j] = mfma16_f32(x, q, z[j]);
       } else {
-        bf16x8 b[1];
-        split_terms<1>(q, b);
-        z[j] = mfma16(__builtin_bit_cast(bf16x8, *(const THK_GLOBAL u32x4 *)row), b[0], z[j]);
+        z[j] = mfma16(__builtin_bit_cast(bf16x8, kx[s][j][0]), b[0], z[j]);
       }
     }
   }
   softmax_step(z, mine ? rows : 0, h, scale, st);
 #pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    if (32 * g >= rows) break;
+  for (int gh = 0; gh < 4; ++gh) {
+    const int g = gh >> 1, half = gh & 1;
+    float p[8];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      float p[8];
-      uint32_t x[8][DT == THK_F32 ? 4 : 2];   // four channels of each of the lane's eight rows
+    for (int e = 0; e < 8; ++e) p[e] = z[2 * g + (e >> 2)][e & 3];
+    if constexpr (DT == THK_F32) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = z[2 * g + (e >> 2)][e & 3];
-        const int r = 32 * g + 16 * (e >> 2) + 4 * h + (e & 3);
-        const GlobalPtr row = vt + (size_t)min(r, rows - 1) * kD * EB + (64 * half + 4 * m) * EB;
+      for (int i = 0; i < 4; ++i) {
+        float x[8];
 #pragma unroll
-        for (int i = 0; i < (DT == THK_F32 ? 4 : 2); ++i) x[e][i] = r < rows ? ((const THK_GLOBAL uint32_t *)row)[i] : 0u;
+        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(vx[gh][e][i]);
+        st.acc[4 * half + i] = mfma16_f32(x, p, st.acc[4 * half + i]);
       }
-      if constexpr (DT == THK_F32) {
+    } else {
+      bf16x8 b[2];
+      split_terms<2>(p, b);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float a[8];
+      for (int i = 0; i < 4; ++i) {
+        u32x4 x;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) a[e] = __uint_as_float(x[e][i]);
-          st.acc[4 * half + i] = mfma16_f32(a, p, st.acc[4 * half + i]);
-        }
-      } else {
-        bf16x8 b[2];
-        split_terms<2>(p, b);
+        for (int w = 0; w < 4; ++w)   // the lower or the upper halves of two rows' words
+          x[w] = __builtin_amdgcn_perm(vx[gh][2 * w + 1][i >> 1], vx[gh][2 * w][i >> 1], i & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          u32x4 a;
-#pragma unroll
-          for (int w = 0; w < 4; ++w)   // the lower or the upper halves of two rows' words
-            a[w] = __builtin_amdgcn_perm(x[2 * w + 1][i >> 1], x[2 * w][i >> 1], i & 1 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-          for (int n = 0; n < 2; ++n) st.acc[4 * half + i] = mfma16(__builtin_bit_cast(bf16x8, a), b[n], st.acc[4 * half + i]);
-        }
+        for (int n = 0; n < 2; ++n) st.acc[4 * half + i] = mfma16(__builtin_bit_cast(bf16x8, x), b[n], st.acc[4 * half + i]);
       }
     }
   }
@@ -682,7 +699,7 @@ __global__ __launch_bounds__(256, DT == THK_F32 ? 1 : 2) void k_paged_decode(Pag
   if (with_tail)
     for (int r0 = (3 - wave) * kTile; r0 < nt; r0 += 4 * kTile) {   // (the last wave has the fewest pages)
       const size_t at = ((size_t)u * z.cap + r0) * kD * EB;
-      tail_tile<DT>(as_global(z.kt) + at, as_global(z.vt) + at, min(kTile, nt - r0), cls == 0, m, h, q_row, z.scale_log2, st);
+      tail_tile<DT>((const char *)z.kt + at, (const char *)z.vt + at, min(kTile, nt - r0), cls == 0, m, h, q_row, z.scale_log2, st);
     }
   st.l = sum_quarters(st.l);
   if constexpr (F::kCodes) {
