@@ -7,6 +7,8 @@
 namespace thk {
 namespace {
 
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
 // A value of another lane of the 16 that share a group (a row of the wave's data paths); the control words of the moves.
 template <int CTRL>
 __device__ __forceinline__ float from_lane(float x) {
@@ -150,8 +152,9 @@ __device__ __forceinline__ void encode_group(const float (&x)[4][8], const bool 
   }
 }
 
-// One block per (unit, tile of the call).  Keys go through LDS, where their kept channels are picked; values go straight
-// from memory to the lane that encodes them.
+// One block per (unit, tile of the call), or in calls that leave the card empty (paged_apart) two: one for the keys, which go
+// through LDS, where their kept channels are picked, and one for the values, which go straight from memory to the lane that
+// encodes them.
 template <int DT, int BITS>
 __global__ __launch_bounds__(256) void k_paged_write(PagedWriteArgs a) {
   using E = Elem<DT>;
@@ -159,7 +162,9 @@ __global__ __launch_bounds__(256) void k_paged_write(PagedWriteArgs a) {
   __shared__ __align__(16) char rows_lds[kTile * PITCH];
   __shared__ __align__(16) int16_t idx_lds[kD];
   const int tid = threadIdx.x, m = tid & 15, grp = tid >> 4;
-  const uint32_t u = a.by_tiles.of(blockIdx.x), t = blockIdx.x - u * (uint32_t)a.tiles;   // (a grid has fewer than 2^24 blocks)
+  const uint32_t blk = a.apart ? blockIdx.x >> 1 : blockIdx.x;   // (a grid has fewer than 2^24 blocks)
+  const bool keys = !a.apart || (blockIdx.x & 1) == 0, values = !a.apart || (blockIdx.x & 1) != 0;
+  const uint32_t u = a.by_tiles.of(blk), t = blk - u * (uint32_t)a.tiles;
   const UnitPlace place = a.p.place(u);
   const int b = place.b;
   const int64_t n = min((int64_t)scalar_load(a.n_rows, b), a.most);
@@ -170,38 +175,41 @@ __global__ __launch_bounds__(256) void k_paged_write(PagedWriteArgs a) {
   if (dst == nullptr) return;
   const int rows = (int)min(n - r0, (int64_t)kTile);
   const size_t base = ((size_t)u * a.src_rows + r0) * kD;   // first element of the tile's rows
-
-  // values: lane m of group (g, q, half) takes channels 64 half + 4 m .. + 3 of its eight rows
-  float xv[4][8];
-  {
+  float xv[4][8], x[4][8];
+  if (values) {   // lane m of group (g, q, half) takes channels 64 half + 4 m .. + 3 of its eight rows
     const int half = grp & 1, q = (grp >> 1) & 3, g = grp >> 3;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int r = 32 * g + 16 * (e >> 2) + 4 * q + (e & 3);
       const size_t at = base + (size_t)min(r, rows - 1) * kD + 64 * half + 4 * m;
       if constexpr (DT == THK_BF16) {
-        const uint2 w = *(const uint2 *)((const uint16_t *)a.v + at);
+        const u32x2 w = __builtin_nontemporal_load((const u32x2 *)((const uint16_t *)a.v + at));
         xv[0][e] = __uint_as_float(w.x << 16); xv[1][e] = __uint_as_float(w.x & 0xffff0000u);
         xv[2][e] = __uint_as_float(w.y << 16); xv[3][e] = __uint_as_float(w.y & 0xffff0000u);
       } else {
-        const float4 w = *(const float4 *)((const float *)a.v + at);
-        xv[0][e] = w.x; xv[1][e] = w.y; xv[2][e] = w.z; xv[3][e] = w.w;
+        const u32x4 w = ld_stream((const u32x4 *)((const float *)a.v + at));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) xv[j][e] = __uint_as_float(w[j]);
       }
       if (r >= rows) xv[0][e] = xv[1][e] = xv[2][e] = xv[3][e] = 0.f;   // a group of zeros: codes and parameters are zero
     }
   }
   constexpr int CPR = kD * EB / 16;   // 16-byte pieces of a row
-  for (int i = tid; i < rows * CPR; i += 256) {
-    const int r = i / CPR, c = i % CPR;
-    *(u32x4 *)(rows_lds + r * PITCH + c * 16) = ld_stream((const u32x4 *)((const char *)a.k + base * EB) + i);
+  if (keys) {
+    for (int i = tid; i < rows * CPR; i += 256) {
+      const int r = i / CPR, c = i % CPR;
+      *(u32x4 *)(rows_lds + r * PITCH + c * 16) = ld_stream((const u32x4 *)((const char *)a.k + base * EB) + i);
+    }
+    if (tid < kD) idx_lds[tid] = tid < a.T ? a.idx[(size_t)u * a.T + tid] & (kD - 1) : 0;
   }
-  if (tid < kD) idx_lds[tid] = tid < a.T ? a.idx[(size_t)u * a.T + tid] & (kD - 1) : 0;
-  const bool all[4] = {true, true, true, true};
-  encode_group<DT, BITS>(xv, all, dst + a.p.lay.v_codes + grp * 64 * a.p.lay.unit_bytes,
-                         dst + a.p.lay.v_params + grp * 8 * 2 * EB, m);
+  if (values) {
+    const bool all[4] = {true, true, true, true};
+    encode_group<DT, BITS>(xv, all, dst + a.p.lay.v_codes + grp * 64 * a.p.lay.unit_bytes,
+                           dst + a.p.lay.v_params + grp * 8 * 2 * EB, m);
+  }
+  if (!keys) return;
   __syncthreads();
   if (grp >= a.p.lay.chunks) return;
-  float xk[4][8];
   bool ok[4];
   int channel[8];
 #pragma unroll
@@ -212,13 +220,13 @@ __global__ __launch_bounds__(256) void k_paged_write(PagedWriteArgs a) {
     ok[j] = r < rows;
     const char *const src = rows_lds + min(r, rows - 1) * PITCH;   // a row outside repeats one inside: the extremes stay
 #pragma unroll
-    for (int e = 0; e < 8; ++e) xk[j][e] = E::load1(src, channel[e]);
+    for (int e = 0; e < 8; ++e) x[j][e] = E::load1(src, channel[e]);
     if (8 * grp + 8 > a.T) {   // past the last kept channel: zeros
 #pragma unroll
-      for (int e = 0; e < 8; ++e) xk[j][e] = 8 * grp + e < a.T ? xk[j][e] : 0.f;
+      for (int e = 0; e < 8; ++e) x[j][e] = 8 * grp + e < a.T ? x[j][e] : 0.f;
     }
   }
-  encode_group<DT, BITS>(xk, ok, dst + grp * 64 * a.p.lay.unit_bytes, dst + a.p.lay.k_params + grp * 8 * 2 * EB, m);
+  encode_group<DT, BITS>(x, ok, dst + grp * 64 * a.p.lay.unit_bytes, dst + a.p.lay.k_params + grp * 8 * 2 * EB, m);
 }
 
 // The inverse of encode_group: what the lane's 32 codes stand for, rounded once to the element type.
@@ -264,20 +272,22 @@ __device__ __forceinline__ void decode_group(const char *src, const char *par, i
     }
 }
 
-// One block per (unit, tile that holds rows of the call).
+// One block per (unit, tile that holds rows of the call), or two as above.
 template <int DT, int BITS>
 __global__ __launch_bounds__(256) void k_paged_read(PagedReadArgs a) {
   using E = Elem<DT>;
   constexpr int EB = E::EB;
   __shared__ __align__(16) char rows_lds[16 + kTile * kD * EB];
   const int tid = threadIdx.x, m = tid & 15, grp = tid >> 4;
-  const uint32_t u = a.by_tiles.of(blockIdx.x);
+  const uint32_t blk = a.apart ? blockIdx.x >> 1 : blockIdx.x;
+  const bool keys = a.k_out != nullptr && (!a.apart || (blockIdx.x & 1) == 0), values = a.v_out != nullptr && (!a.apart || (blockIdx.x & 1) != 0);
+  const uint32_t u = a.by_tiles.of(blk);
   const UnitPlace place = a.p.place(u);
   const int b = place.b;
   const int64_t row0 = a.row0 != nullptr ? scalar_load(a.row0, b) : 0;
   if (row0 < 0) return;
   const int64_t end = row0 + min((int64_t)scalar_load(a.n_rows, b), a.most);
-  const int64_t t = row0 / kTile + (blockIdx.x - u * (uint32_t)a.tiles);
+  const int64_t t = row0 / kTile + (blk - u * (uint32_t)a.tiles);
   const int64_t lo = max(row0, t * kTile), hi = min(end, (t + 1) * kTile);   // rows of this block
   if (lo >= hi) return;
   const char *const src = a.p.unit(place).tile(t);
@@ -285,7 +295,7 @@ __global__ __launch_bounds__(256) void k_paged_read(PagedReadArgs a) {
   const size_t out_row = (size_t)u * a.out_rows + (lo - row0);
   const int first = (int)(lo - t * kTile), rows = (int)(hi - lo);
   float x[4][8];
-  if (a.v_out != nullptr) {
+  if (values) {
     const int half = grp & 1, q = (grp >> 1) & 3, g = grp >> 3;
     decode_group<DT, BITS>(src + a.p.lay.v_codes + grp * 64 * a.p.lay.unit_bytes, src + a.p.lay.v_params + grp * 8 * 2 * EB, m, x);
 #pragma unroll
@@ -297,7 +307,7 @@ __global__ __launch_bounds__(256) void k_paged_read(PagedReadArgs a) {
       else *(float4 *)((float *)a.v_out + at) = make_float4(x[0][e], x[1][e], x[2][e], x[3][e]);
     }
   }
-  if (a.k_out == nullptr) return;
+  if (!keys) return;
   // The block's key rows are one run of the output.  They are put together in LDS at the output's offset from a 16-byte
   // boundary, so that whole aligned 16-byte pieces can be stored; the two ends go element by element.
   char *const dst = (char *)a.k_out + out_row * a.ld * EB;
@@ -363,13 +373,14 @@ hipError_t launch_paged_write(int dtype, int bits, const PagedWriteArgs &a, hipS
   const bool f32 = dtype == THK_F32;
   return launch(bits == 0   ? (f32 ? k_paged_write<THK_F32, 0> : k_paged_write<THK_BF16, 0>)
                 : bits == 4 ? (f32 ? k_paged_write<THK_F32, 4> : k_paged_write<THK_BF16, 4>)
-                            : (f32 ? k_paged_write<THK_F32, 8> : k_paged_write<THK_BF16, 8>), a, a.units * a.tiles, st);
+                            : (f32 ? k_paged_write<THK_F32, 8> : k_paged_write<THK_BF16, 8>), a, a.units * a.tiles * (a.apart ? 2 : 1), st);
 }
 hipError_t launch_paged_read(int dtype, int bits, const PagedReadArgs &a, hipStream_t st) {
   const bool f32 = dtype == THK_F32;
   return launch(bits == 0   ? (f32 ? k_paged_read<THK_F32, 0> : k_paged_read<THK_BF16, 0>)
                 : bits == 4 ? (f32 ? k_paged_read<THK_F32, 4> : k_paged_read<THK_BF16, 4>)
-                            : (f32 ? k_paged_read<THK_F32, 8> : k_paged_read<THK_BF16, 8>), a, a.units * a.tiles, st);
+                            : (f32 ? k_paged_read<THK_F32, 8> : k_paged_read<THK_BF16, 8>), a,
+                a.units * a.tiles * (a.apart ? 2 : 1), st);
 }
 hipError_t launch_paged_decode(int dtype, int bits, const PagedDecodeArgs &a, hipStream_t st) {
   return dtype == THK_F32 ? launch_paged_decode_f32(bits, a, st) : launch_paged_decode_bf16(bits, a, st);
