@@ -337,6 +337,31 @@ def test_every_split_gives_the_same_attention(dtype, bits):
         _check_attention(c, c.decode())
 
 
+# (L, B, N_kv, G, T, rows, page_rows, tails, cap, n_split, S): calls long enough to be cut into pieces by the lengths
+_RAGGED = [int(x) for x in np.random.default_rng(77).integers(0, 700, 150)]
+BY_LENGTHS = [
+    (1, 150, 2, 4, 51, _RAGGED, 64, [b % 3 for b in range(150)], 4, 3, 2000), (1, 3, 4, 2, 64, [20000, 10, 0], 512, [0, 5, 0], 8, 2, 50000),
+    (1, 1, 8, 1, 64, [5000], 256, [40], 64, 2, 70000), (1, 64, 1, 17, 33, [63 + b for b in range(64)], 64, None, 0, 2, 9000),
+    (2, 2, 4, 8, 97, [2000, 1999], 128, [64, 1], 64, 7, 60000), (1, 65, 4, 4, 64, [0] * 64 + [3000], 64, [0] * 64 + [3], 4, 5, 3000),
+]
+
+
+@pytest.mark.parametrize("case", BY_LENGTHS, ids=[str(i) for i in range(len(BY_LENGTHS))])
+@pytest.mark.parametrize("dtype,bits", [("bf16", 4), ("bf16", 0), ("bf16", 8), ("f32", 4)])
+def test_pieces_by_the_lengths(dtype, bits, case):
+    L, B, N_kv, G, T, rows, page_rows, tails, cap, n_split, S = case
+    assert L * B * N_kv * -(-S // 64) >= 8192
+    c = Cache(dtype, bits, L, B, N_kv, G, T, rows, page_rows, tails, cap, seed=len(rows) + G, n_split=n_split)
+    c.write()
+    c.shape.S = S                      # the host's bound; the lengths are what they are
+    out = c.decode()
+    torch.cuda.synchronize()
+    _check_attention(c, out)
+    assert torch.equal(c.decode(), out)
+    c.shape.n_split = 0
+    _check_attention(c, c.decode())
+
+
 def test_offsets_past_32_bits():
     """A pool of more than 4 GiB whose first and last pages are in use, and tails likewise."""
     c = Cache("bf16", 0, 1, 2, 8, 4, 128, [256, 130], 256, tails=[10, 64], cap=64, seed=6, spare=0)
