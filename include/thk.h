@@ -477,9 +477,15 @@ thk_status thk_tail_append_ragged(const thk_shape *shape, const void *k_new, con
  * counts are not used, whatever they hold: rows of the tail are not read, rows of a tile have
  * weight zero.  fp32 arithmetic: codes enter the matrix cores as whole numbers, what multiplies
  * them as two (bf16) or three (fp32) bf16 terms.
- * The pieces of a long sequence (n_split; by shape->S, so that the host need not know the lengths)
- * are joined in an order fixed by the lengths: repeated calls give identical bits.
- *   ws : thk_workspace_bytes(shape, THK_OP_DECODE_PAGED) bytes, 16-byte aligned.
+ * shape->S is below 2^31 - 64.  A unit's rows are cut into pieces that are joined by a second launch: about n_split of
+ * them (0: as many as the estimate says), each of whole tiles, the last with the tail.  Short calls cut by shape->S, so that
+ * the pieces of a sequence depend on nothing but its own length.  Long calls of several sequences cut by the lengths on the
+ * device, a piece of about the same number of tiles for every sequence: there a result may differ in its last bits with the
+ * other sequences' lengths.  Either way the order of every sum is fixed by the arguments and the lengths: repeated calls
+ * give identical bits.
+ *   ws : thk_workspace_bytes(shape, THK_OP_DECODE_PAGED) bytes, 16-byte aligned: enough for any pages.  Calls that may run at
+ *        the same time need one each; calls one after the other, captured ones too, may share it.  Nothing in it outlives
+ *        the call.
  */
 thk_status thk_decode_attn_paged(const thk_shape *shape, const thk_pages *pages, const void *q,
                                  const void *pool, const int32_t *table, const int32_t *s_pages,

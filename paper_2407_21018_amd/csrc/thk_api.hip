@@ -733,16 +733,24 @@ int64_t paged_groups(const thk_shape *s) { return ceil_div(s->N_q / s->N_kv, 16)
 // count with the least estimated time of a few.  With k = tiles of a piece, R = 2 blocks resident on a compute unit (fp32: 1) and
 // L = blocks on the fullest one, in us:
 //     sum over rounds of l = R (in the last round what is left) blocks of
-//         max(l k t_tile, steps t_step) + t_block (l + 1) / 2                     steps: of a wave through its piece
+//         max(l k t_tile (1 + alone if l < R), steps t_step) + t_block (l + 1) / 2     steps: of a wave through its piece
 //     + [more than one piece] t_merge + t_record * records / 1000
 // t_tile = t0 + t1 T / 64, with (1 + f) or (1 + 2 f) of it where a wave takes two tiles or one at once: codes are bound by the
-// vector unit.  Fitted to 820 random shapes (all formats, 1 to 64 sequences, 65 to 131072 rows, up to 18 counts each): the
-// chosen count takes 0.5 % (element pages) to 2.5 % (4 bits) longer than the best one on average, 1.5x at worst; as many
-// blocks as are resident at once, 9 to 10 % longer.
-struct PagedTimes { double t0, t1, f, t_step, t_block, t_merge, t_record; };
+// vector unit.  Fitted to 1000 random shapes (all formats, 1 to 64 sequences, 65 to 131072 rows, up to 18 counts each; 700
+// with equal lengths, 300 with ragged ones): the chosen count takes 0.1 % to 2 % (fp32, 4 bits) longer than the best one on
+// average, 1.39x at worst; as many blocks as are resident at once, 9 to 13 %.  With 2 blocks or more for every compute unit
+// sequences stay whole: in 97 of those shapes (bf16) that takes 0.1 % longer than the best count, 1.08x at worst, and two
+// pieces up to 1.6x.
+struct PagedTimes { double t0, t1, f, alone, t_step, t_block, t_merge, t_record; };
 constexpr PagedTimes kPagedTimes[2][3] = {   // [fp32, bf16][elements, 4 bits, 8 bits]
-    {{0.831, 0.615, 0, 4.292, 6.566, 2.971, 0.084}, {0.288, 0.239, 0.074, 1.163, 8.175, 2.675, 0.574}, {0.274, 0.268, 0.129, 1.970, 9.844, 1.678, 0.044}},
-    {{0.286, 0.344, 0, 0.097, 3.799, 2.940, 0.429}, {0.124, 0.069, 0.827, 3.527, 3.235, 3.238, 0.042}, {0.121, 0.265, 0.088, 3.521, 3.777, 2.944, 0.332}}};
+    {{0.886, 0.338, 0, 0, 2.007, 6.363, 2.511, 1.874}, {0.195, 0.254, 0.180, 0, 1.378, 6.950, 2.389, 0.030}, {0.307, 0.149, 0.139, 0, 2.027, 7.061, 2.857, 0.317}},
+    {{0.468, 0.147, 0, 0.069, 1.007, 3.285, 3.462, 0.254}, {0.225, 0.023, 0.160, 0.232, 0.817, 5.590, 2.090, 0.076}, {0.190, 0.170, 0.105, 0.105, 1.709, 5.360, 1.799, 0.051}}};
+
+// Cut by the lengths on the device where the call is long enough for it not to matter: the work of a batch of the longest ones,
+// spread over the card, is 32 tiles a compute unit (some 10 us) or more.
+bool paged_by_lengths(const thk_shape *s, const Split &sp) {
+  return sp.n > 1 && (s->B > 1 || sp.rows >= 64 * kTile) && units_of(s) * ceil_div(s->S, kTile) >= 32 * kCUs;
+}
 
 Split paged_split(const thk_shape *s, int bits) {
   const int64_t tiles64 = ceil_div(s->S, kTile), blocks = units_of(s) * paged_groups(s);   // S < 2^31
@@ -752,7 +760,7 @@ Split paged_split(const thk_shape *s, int bits) {
     return Split{(int)((tiles + per - 1) / per), (int64_t)per * kTile};
   };
   if (s->n_split != 0) return pieces((uint32_t)s->n_split);
-  if (tiles == 1 || blocks > 8 * kCUs) return pieces(1);
+  if (tiles == 1 || blocks >= 2 * kCUs) return pieces(1);
   const PagedTimes &t = kPagedTimes[s->dtype == THK_BF16][bits == 0 ? 0 : bits == 4 ? 1 : 2];
   const uint32_t resident = s->dtype == THK_BF16 ? 2 : 1, most_step = (uint32_t)paged_decode_step(bits, s->N_q / s->N_kv, s->T);
   const double t_tile = t.t0 + t.t1 * s->T / 64, t_records = t.t_record * 1e-3 * (double)((int64_t)s->L * s->B * s->N_q);
@@ -764,7 +772,7 @@ Split paged_split(const thk_shape *s, int bits) {
     const uint32_t per = (uint32_t)(sp.rows / kTile), step = std::min(most_step, (per + 3) / 4), steps = (per + 4 * step - 1) / (4 * step);
     const uint32_t on_cu = ((uint32_t)blocks * (uint32_t)sp.n + kCUs - 1) / kCUs, rounds = on_cu / resident, rest = on_cu % resident;
     const double tile = t_tile * (step >= 3 ? 1 : step == 2 ? 1 + t.f : 1 + 2 * t.f);
-    auto round = [&](uint32_t l) { return std::max((double)l * per * tile, steps * t.t_step) + t.t_block * 0.5 * (l + 1); };
+    auto round = [&](uint32_t l) { return std::max((double)l * per * tile * (l < resident ? 1 + t.alone : 1), steps * t.t_step) + t.t_block * 0.5 * (l + 1); };
     const double time = rounds * round(resident) + (rest != 0 ? round(rest) : 0) + (sp.n > 1 ? t.t_merge + t_records * sp.n : 0);
     if (n == 1 || time < least) {
       best = sp;
@@ -1378,10 +1386,7 @@ thk_status thk_decode_attn_paged(const thk_shape *s, const thk_pages *p, const v
   a.units = units_of(s);
   a.T = s->T; a.G = s->N_q / s->N_kv; a.cap = s_tail_cap;
   a.n_split = sp.n;
-  // Cut by the lengths where the call is long enough for it not to matter: the work of a batch of the longest ones, spread
-  // over the card, is 32 tiles a compute unit (some 10 us) or more.
-  const bool by_lengths = sp.n > 1 && (s->B > 1 || sp.rows >= 64 * kTile) && a.units * ceil_div(s->S, kTile) >= 32 * kCUs;
-  a.per = by_lengths ? 0 : (int32_t)(sp.rows / kTile);
+  a.per = paged_by_lengths(s, sp) ? 0 : (int32_t)(sp.rows / kTile);
   a.groups = (int32_t)paged_groups(s);
   a.cols = (int32_t)(a.units / s->B * a.groups);
   a.by_cols = Divisor(a.cols);

@@ -510,10 +510,12 @@ __device__ __forceinline__ uint32_t wave_sums(uint32_t x) {
 // ceil(t / per) of them.  Blocks are numbered by sequence, unit and group, piece.
 // With per given, every unit has n_split blocks, and those past its last piece have nothing to do.  A block knows its place
 // without the lengths.
-// Otherwise the cutting is done here, where the lengths are: per = all sequences' tiles over (sequences * n_split), pieces of
-// one sequence of equal size up to a tile; there are at most n_split + 1 per unit and group on average.  The block's place
-// takes a trip to memory and some 100 instructions (0.8 us), but the pieces do not depend on how far the host's bound of the
-// lengths is from the lengths, and one long sequence among short ones is cut into as many as it takes.
+// Otherwise the cutting is done here, where the lengths are: per = all sequences' tiles over (sequences * n_split), or so much
+// more that sequences of different lengths have n_split pieces on average after rounding (300 ragged batches: 9 % longer without
+// that, some compute units having a block more); pieces of one sequence of equal size up to a tile; never more than n_split + 1
+// per unit and group on average.  The block's place takes a trip to memory and some 100 to 200 instructions (0.8 us), but the
+// pieces do not depend on how far the host's bound of the lengths is from the lengths, and one long sequence among short ones is
+// cut into as many as it takes.
 struct Cutting {
   const PagedDecodeArgs &a;
   uint32_t per;   // tiles
@@ -527,10 +529,18 @@ struct Cutting {
 
   __device__ __forceinline__ Cutting(const PagedDecodeArgs &args, int lane) : a(args), per((uint32_t)args.per) {
     if (a.per != 0) return;
+    const double want = (double)a.p.B * (double)a.n_split;
     double total = 0;   // exact
     for (int b0 = 0; b0 < a.p.B; b0 += kWave) total += (double)(uint32_t)__builtin_amdgcn_readlane((int)wave_sums(tiles_at(b0 + lane)), 63);
-    const double n = (double)a.p.B * (double)a.n_split;
-    per = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)ceil(total / n));
+    per = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)ceil(total / want));
+    // Sequences of different lengths now have up to a piece more each than they should; longer pieces, until the sum is met.
+    for (int i = 0; i < 4; ++i) {
+      double have = 0;
+      for (int b0 = 0; b0 < a.p.B; b0 += kWave)
+        have += (double)(uint32_t)__builtin_amdgcn_readlane((int)wave_sums(pieces_of(tiles_at(b0 + lane))), 63);
+      if (have <= want) return;
+      per = max(per + 1, (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(per * have / want)));
+    }
   }
   // The sequence in which the x-th of all sequences' pieces lies (b = B: none), and the number of pieces in front of it; or,
   // with x < 0, the number of pieces in front of sequence b.  (Not with per given.)
