@@ -700,14 +700,23 @@ size_t prune_value_ws_bytes(const thk_shape *s, int n) {
 bool aligned4(const void *p) { return ((uintptr_t)p & 3u) == 0; }
 constexpr uint64_t kMaxThreads = 0xffffffffull;   // of a launch
 
+// check_shape, with the number of units not past 64 bits
+thk_status check_paged_shape(const thk_shape *s) {
+  if (s != nullptr && s->L > 0 && s->B > 0 && s->N_kv > 0 && (int64_t)s->L * s->B > kMaxGrid / s->N_kv) return THK_ERR_SHAPE;
+  return check_shape(s, false);
+}
 thk_status check_pages(const thk_shape *s, const thk_pages *p) {
-  const thk_status st = check_shape(s, false);
+  const thk_status st = check_paged_shape(s);
   if (st != THK_OK) return st;
   if (p == nullptr) return THK_ERR_NULL;
   if (p->bits != 0 && p->bits != 4 && p->bits != 8) return THK_ERR_UNSUPPORTED;
   if (p->page_rows < kTile || p->page_rows > 65536 || (p->page_rows & (p->page_rows - 1)) != 0) return THK_ERR_SHAPE;
   if (p->max_pages < 1 || (int64_t)p->max_pages * p->page_rows > INT32_MAX) return THK_ERR_SHAPE;
   if (p->n_pages < 1 || p->n_pages > INT32_MAX || s->S > INT32_MAX - kTile) return THK_ERR_SHAPE;
+  int64_t bytes = 0;   // of the pool: not past 63 bits either
+  if (__builtin_mul_overflow((int64_t)s->L * s->N_kv, p->n_pages, &bytes) ||
+      __builtin_mul_overflow(bytes, (int64_t)(p->page_rows / kTile) * paged_layout(s->dtype, p->bits, s->T).tile_bytes, &bytes))
+    return THK_ERR_SHAPE;
   return THK_OK;
 }
 int64_t paged_rows(const thk_shape *s, const thk_pages *p) { return std::min<int64_t>(s->S, (int64_t)p->max_pages * p->page_rows); }
@@ -847,7 +856,7 @@ int32_t thk_default_split(const thk_shape *s, int32_t op) {
   if (op == THK_OP_DECODE) return decode_split(&t).n;
   if (op == THK_OP_SCORE) return score_split(&t, units_of(&t)).n;
   if (op == THK_OP_PRUNE) return score_split(&t, prune_group_units(&t)).n;
-  if (op == THK_OP_DECODE_PAGED) return t.S <= INT32_MAX - kTile ? paged_most_pieces(&t) : 0;
+  if (op == THK_OP_DECODE_PAGED) return check_paged_shape(s) == THK_OK && t.S <= INT32_MAX - kTile ? paged_most_pieces(&t) : 0;
   if (op == THK_OP_SCORE_VALUE || op == THK_OP_PRUNE_VALUE) return (t.S_obs >= 1 && t.S_obs <= t.S) ? value_split(&t).n : 0;
   return 0;
 }
@@ -884,7 +893,7 @@ size_t thk_workspace_bytes(const thk_shape *s, int32_t op) {
       return sp.n == 1 ? 16 : decode_ws_bytes(s, sp.n);
     }
     case THK_OP_DECODE_PAGED:
-      return s->S <= INT32_MAX - kTile ? paged_ws_bytes(s, paged_most_pieces(s)) : 0;
+      return check_paged_shape(s) == THK_OK && s->S <= INT32_MAX - kTile ? paged_ws_bytes(s, paged_most_pieces(s)) : 0;
     case THK_OP_SCORE_VALUE:
       if (s->S_obs < 1 || (int64_t)s->S_obs > s->S) return 0;
       return value_ws_bytes(s, value_split(s).n);
@@ -1346,7 +1355,7 @@ thk_status thk_paged_read(const thk_shape *s, const thk_pages *p, const void *po
 thk_status thk_tail_append_ragged(const thk_shape *s, const void *k_new, const void *v_new, int32_t src_rows,
                                   const int32_t *src_row0, const int32_t *n_new, void *k_tail, void *v_tail,
                                   const int32_t *s_tail, int32_t s_tail_cap, void *stream) {
-  const thk_status st = check_shape(s, false);
+  const thk_status st = check_paged_shape(s);
   if (st != THK_OK) return st;
   if (k_new == nullptr || v_new == nullptr || k_tail == nullptr || v_tail == nullptr || s_tail == nullptr) return THK_ERR_NULL;
   if (src_rows < 1 || s_tail_cap < 1) return THK_ERR_SHAPE;

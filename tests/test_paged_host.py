@@ -114,6 +114,25 @@ def test_launches_too_large_for_one_grid_are_refused():
     assert _decode(s, p) == 2
 
 
+@pytest.mark.parametrize("kw", [dict(L=1 << 30, B=1 << 30, N_kv=16, N_q=16), dict(L=1 << 30, B=1 << 30, N_kv=1 << 4, N_q=1 << 8),
+                                dict(L=(1 << 31) - 1, B=(1 << 31) - 1, N_kv=(1 << 31) - 1, N_q=(1 << 31) - 1), dict(L=1 << 16, B=1 << 16)])
+def test_units_past_the_number_range_are_refused(kw):
+    """L * B * N_kv past 64 bits must not pass for a small number, nor for none."""
+    s, p = _shape(**kw), _pages()
+    assert _write(s, p) == 2 and _read(s, p) == 2 and _append(s) == 2 and _decode(s, p) == 2
+    assert thk.thk_paged_pool_bytes(s, p) == 0
+    assert thk.thk_workspace_bytes(s, thk.THK_OP_DECODE_PAGED) == 0 and thk.thk_default_split(s, thk.THK_OP_DECODE_PAGED) == 0
+
+
+def test_pools_past_the_number_range_are_refused():
+    s = _shape(L=64, N_q=64, N_kv=64)
+    for n_pages, want in (((1 << 31) - 1, 2), (1 << 30, 2), (1 << 20, 0)):
+        p = _pages(page_rows=65536, max_pages=1, n_pages=n_pages)
+        assert (thk.thk_paged_pool_bytes(s, p) == 0) == (want == 2)
+        if want:
+            assert _write(s, p) == 2 and _read(s, p) == 2 and _decode(s, p) == 2
+
+
 def test_sizes():
     for dtype, e in ((thk.THK_BF16, 2), (thk.THK_F32, 4)):
         for T in (1, 8, 51, 64, 76, 128):
