@@ -421,7 +421,8 @@ thk_status thk_tail_flush(const thk_shape *shape, const int16_t *idx, void *k_pr
  *     code of x = min(N, rint(fl(fl(x - m) / s))), ties to even; 0 where s == 0
  * and a code c stands for m + c s.  m and s are held in the element type.  An element is off by
  * at most s / 2 (plus, for bf16 caches of 8-bit codes, what rounding s to 8 bits moves the last
- * code: s / 2).  max x - min x must be finite.
+ * code: s / 2).  What is stored as codes must be finite, max x - min x too: of a tile that holds an
+ * infinity or NaN the codes and scales are unspecified.  Rows stored as elements may be anything.
  */
 typedef struct {
   int32_t bits;      /* 0: rows in the element type; 4 or 8: codes                      */
@@ -475,7 +476,7 @@ thk_status thk_tail_append_ragged(const thk_shape *shape, const void *k_new, con
  * the full-width tail (at most s_tail_cap; s_tail_cap = 0: no tail, and k_tail, v_tail, s_tail are
  * not looked at).  One softmax over both; a sequence without any row gets zeros.  Rows past the
  * counts are not used, whatever they hold: rows of the tail are not read, rows of a tile have
- * weight zero.  fp32 arithmetic: codes enter the matrix cores as whole numbers, what multiplies
+ * weight zero, and elements are taken out.  fp32 arithmetic: codes enter the matrix cores as whole numbers, what multiplies
  * them as two (bf16) or three (fp32) bf16 terms.
  * shape->S is below 2^31 - 64.  A unit's rows are cut into pieces that are joined by a second launch: about n_split of
  * them (0: as many as the estimate says), each of whole tiles, the last with the tail.  Short calls cut by shape->S, so that

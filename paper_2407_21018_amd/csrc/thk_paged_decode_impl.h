@@ -243,12 +243,14 @@ struct Tiles {
   __device__ __forceinline__ void load_keys(const char *const (&t)[CL], int bytes, GlobalPtr own, const PagedLayout &lay, int m, int h) {
 #pragma unroll
     for (int s = 0; s < NST; ++s) {
-      // group 4 s + h; those past the last are what lies behind the keys in the tile, and meet zeros of the query
+      // group 4 s + h; those past the last are what lies behind the keys in the tile, and meet zeros of the query.  (Elements: the
+      // last group again, which belongs to the same rows.  What lies behind it need not be finite.)
       if constexpr (F::kCodes) load_pairs<DT>(own + lay.k_params + s * 4 * kPairs, kp[s]);
+      const int at = F::kCodes ? h * 64 * F::UB : min(4 * s + h, lay.chunks - 1) * 64 * F::UB, off = F::kCodes ? s * 256 * F::UB : 0;
 #pragma unroll
       for (int x = 0; x < CL; ++x)
 #pragma unroll
-        for (int k = 0; k < F::NC; ++k) kc[x][s][k] = load_cell(t[x], bytes, h * 64 * F::UB + m * 16 + k * 256, s * 256 * F::UB);
+        for (int k = 0; k < F::NC; ++k) kc[x][s][k] = load_cell(t[x], bytes, at + m * 16 + k * 256, off);
     }
   }
   // (G0, G1: which halves of the rows)
@@ -263,6 +265,38 @@ struct Tiles {
       for (int x = 0; x < CL; ++x)
 #pragma unroll
         for (int k = 0; k < F::NC; ++k) vc[x][gh][k] = load_cell(t[x], bytes, h * 2 * 64 * F::UB + m * 16 + k * 256, lay.v_codes + grp * 64 * F::UB);
+    }
+  }
+
+  // Half G of the values past the last of `rows` rows becomes zeros: a weight of zero does not take an infinity or NaN out of a
+  // sum.  (Elements only: codes are finite.)
+  template <int G>
+  __device__ __forceinline__ void drop_values(int rows, int h) {
+    if constexpr (!F::kCodes) {
+      const int left = rows - 4 * h - 32 * G;
+      if constexpr (DT == THK_BF16) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const int r = 16 * (w >> 1) + 2 * (w & 1);
+          const uint32_t keep = (r < left ? 0xffffu : 0u) | (r + 1 < left ? 0xffff0000u : 0u);
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int k = 0; k < F::NC; ++k) vc[0][2 * G + half][k][w] &= keep;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const bool keep = 16 * (e >> 2) + (e & 3) < left;
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              u32x4 &x = vc[0][2 * G + half][2 * i + (e >> 2)];
+              x[e & 3] = keep ? x[e & 3] : 0u;
+            }
+        }
+      }
     }
   }
 
@@ -693,8 +727,10 @@ __global__ __launch_bounds__(256, DT == THK_F32 ? 1 : 2) void k_paged_decode(Pag
     tl.logits(q, cls, cst, z);
     tl.template load_values<1, 2>(cur.t, cur.bytes, cur.own, a.p.lay, m, h);
     softmax_step(z, cur.rows, h, a.scale_log2, st);
+    if (!F::kCodes && cur.rows < kTile) tl.template drop_values<0>(cur.rows, h);
     tl.template add_values<0>(z, cls, cst, st);
     tl.load_keys(next.t, next.bytes, next.own, a.p.lay, m, h);
+    if (!F::kCodes && cur.rows < kTile) tl.template drop_values<1>(cur.rows, h);
     tl.template add_values<1>(z, cls, cst, st);
     tl.template load_values<0, 1>(next.t, next.bytes, next.own, a.p.lay, m, h);
     cur = next;

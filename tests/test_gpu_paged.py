@@ -303,6 +303,28 @@ def test_rows_of_a_tile_past_the_count_do_not_matter(dtype, bits):
                 assert np.abs(_np(out[0, b, h * 4:(h + 1) * 4]) - want).max() <= tol
 
 
+@pytest.mark.parametrize("T", [1, 33, 64, 72, 97, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_elements_past_the_count_may_be_anything(dtype, T):
+    """Rows of element pages that a shorter count leaves out: infinities and NaN in keys and values, whose tile is still read."""
+    c = Cache(dtype, 0, 1, 3, 2, 3, T, [300, 200, 64], 64, tails=[0, 3, 0], cap=8, seed=80 + T)
+    rows = [295, 193, 1]
+    full = [c.unit(0, b, h) for b in range(3) for h in range(2)]
+    for b, n in enumerate(rows):
+        for i, bad in enumerate((float("nan"), float("inf"), -float("inf"))):
+            c.k[:, b, :, n + i:c.rows[b]:3], c.v[:, b, :, n + i:c.rows[b]:3] = bad, -bad
+    c.write()
+    c.s_pages, c.rows = _ints(rows), rows
+    out = c.decode()
+    torch.cuda.synchronize()
+    for b in range(3):
+        for h in range(2):
+            k, v, kt, vt, idx = full[b * 2 + h]
+            want = P.attend(_np(c.q[0, b, h * 3:(h + 1) * 3]), idx, k[:rows[b]], v[:rows[b]], kt, vt)
+            tol = {"bf16": 2.0 ** -8, "f32": 2e-5}[dtype] * np.abs(want).max() + {"bf16": 1e-3, "f32": 1e-5}[dtype]
+            assert np.abs(_np(out[0, b, h * 3:(h + 1) * 3]) - want).max() <= tol
+
+
 def test_pages_outside_the_pool_take_no_part():
     c = Cache("bf16", 4, 1, 2, 1, 4, 64, [256, 256], 64, tails=[3, 0], cap=64, seed=21)
     c.write()
