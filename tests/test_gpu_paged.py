@@ -496,3 +496,39 @@ def test_other_streams_and_refused_tensors():
         with pytest.raises(ValueError):
             c.decode(out=got, ws=ws_tensor(1 << 16))
         setattr(c, name, keep)
+
+
+@pytest.mark.parametrize("bits", [0, 4, 8])
+def test_shared_pages(bits):
+    """Sequences whose first pages are the same ones, and a sequence that has one page twice."""
+    c = Cache("bf16", bits, 1, 3, 2, 4, 64, [384, 384, 256], 128, tails=[5, 0, 64], cap=64, seed=60)
+    c.idx[:] = c.idx[:, :1]                       # a shared page holds one choice of channels
+    c.k[:, 1, :, :256], c.v[:, 1, :, :256] = c.k[:, 0, :, :256], c.v[:, 0, :, :256]
+    c.k[:, 2, :, :128], c.v[:, 2, :, :128] = c.k[:, 0, :, 128:256], c.v[:, 0, :, 128:256]
+    c.k[:, 2, :, 128:256], c.v[:, 2, :, 128:256] = c.k[:, 0, :, 128:256], c.v[:, 0, :, 128:256]
+    c.write()
+    want = c.decode()
+    torch.cuda.synchronize()
+    _check_attention(c, want)
+    c.table[1, :2] = c.table[0, :2]
+    c.table[2, :2] = c.table[0, 1]
+    assert torch.equal(c.decode(), want)
+
+
+def test_two_calls_at_once():
+    """Calls on two streams, each with a workspace of its own, side by side."""
+    cs = [Cache("bf16", 4, 1, 8, 8, 4, 64, [9000 - 900 * b for b in range(8)], 128, seed=70, S=9000),
+          Cache("bf16", 8, 1, 2, 8, 4, 76, [9000, 3000], 128, tails=[9, 64], cap=64, seed=71)]
+    wants, outs, streams = [], [], [torch.cuda.Stream() for _ in cs]
+    for c in cs:
+        c.write()
+        wants.append(c.decode())
+        outs.append(torch.zeros_like(wants[-1]))
+    spaces = [ws_tensor(thk.thk_workspace_bytes(c.shape, thk.THK_OP_DECODE_PAGED)) for c in cs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, out, ws, s in zip(cs, outs, spaces, streams):
+            c.decode(out=out, ws=ws, stream=s)
+    torch.cuda.synchronize()
+    for out, want in zip(outs, wants):
+        assert torch.equal(out, want)
