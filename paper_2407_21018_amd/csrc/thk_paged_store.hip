@@ -155,6 +155,9 @@ __device__ __forceinline__ void encode_group(const float (&x)[4][8], const bool 
 // One block per (unit, tile of the call), or in calls that leave the card empty (paged_apart) two: one for the keys, which go
 // through LDS, where their kept channels are picked, and one for the values, which go straight from memory to the lane that
 // encodes them.
+// Bound by memory, at the rate of a copy (5.3 to 5.5 TB/s read + write): bf16 elements, 64 units x 8191 rows, 51 channels 86 us;
+// 4 bits, 1024 units x 4096 rows, 76 channels 481 us.  fp32 rows of keys take 34 KB of LDS, four blocks of a compute unit: 32
+// units of up to 2048 rows, 8 bits 18 us, 3.7 TB/s in its single round of blocks.
 template <int DT, int BITS>
 __global__ __launch_bounds__(256) void k_paged_write(PagedWriteArgs a) {
   using E = Elem<DT>;
@@ -272,7 +275,8 @@ __device__ __forceinline__ void decode_group(const char *src, const char *par, i
     }
 }
 
-// One block per (unit, tile that holds rows of the call), or two as above.
+// One block per (unit, tile that holds rows of the call), or two as above.  Bound by memory as the write is: the cases there
+// take 75 us (5.0 TB/s), 400 us (5.5) and 13 us (2.9: one round of blocks).
 template <int DT, int BITS>
 __global__ __launch_bounds__(256) void k_paged_read(PagedReadArgs a) {
   using E = Elem<DT>;
@@ -340,7 +344,8 @@ __global__ __launch_bounds__(256) void k_paged_read(PagedReadArgs a) {
   }
 }
 
-// One thread per 16-byte piece of a row.
+// One thread per 16-byte piece of a row.  4096 units, 63 rows at most of each: 33 us, 5.1 TB/s read + write; one row of each
+// of 8 units 1.9 us, its launch and two trips to memory (lengths, rows).
 template <int DT>
 __global__ __launch_bounds__(256) void k_append_ragged(RaggedAppendArgs a) {
   constexpr int CPR = kD * Elem<DT>::EB / 16;
