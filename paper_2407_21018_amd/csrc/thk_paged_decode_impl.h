@@ -8,8 +8,9 @@
 // the scaled query and the scaled probabilities -- enters as a sum of bf16 terms: two for bf16 tensors (2^-17 of the value),
 // three for fp32 ones (2^-25).  Of a code c an operand holds something more, which is taken out again with the minimum: 4-bit
 // codes of bf16 tensors are used as 16 + c, whose bits are the code in the mantissa of 16 (one shift and one mask for two of
-// them); all others as c less half the range, a signed byte, which keeps the two sums that make up a logit small and with them
-// what their rounding costs (fp32, 8 bits, 2048 rows: 1.5e-6 of the result with plain codes).
+// them); those of fp32 tensors as c less half the range, a signed byte, which keeps the two sums that make up a logit small and
+// with them what their rounding costs (8 bits, 2048 rows: 1.5e-6 of the result with plain codes, 2.4e-7 so).  8-bit codes of bf16
+// tensors are plain.
 //
 // A wave takes a tile of 64 rows at a time.  S^T = K q^T: A = 16 rows x 32 channels of keys, B = 32 channels x 16 query
 // heads, so lane (m, h) = (lane % 16, lane / 16) ends up with the logits of head m for rows 16 j + 4 h + i.  out^T = V^T P^T:
@@ -73,14 +74,21 @@ struct Format {
   static constexpr int NTV = DT == THK_F32 ? 3 : 2;                 // terms of the (scaled) probabilities
   // an operand is kTimes * code + kBias
   static constexpr bool kMantissa = BITS == 4 && DT == THK_BF16;
+  static constexpr bool kPlain = BITS == 8 && DT == THK_BF16;
   static constexpr float kTimes = BITS == 4 && !kMantissa ? 16.f : 1.f;
-  static constexpr float kBias = kMantissa ? 16.f : -128.f;
+  static constexpr float kBias = kMantissa ? 16.f : kPlain ? 0.f : -128.f;
 };
 
 // Signed bytes A and B of x as two bf16 numbers: whole numbers below 256 in size have all their bits in a float's upper half.
 template <int A, int B>
 __device__ __forceinline__ uint32_t byte_pair(uint32_t x) {
   return __builtin_amdgcn_perm(__float_as_uint((float)(int8_t)(x >> (8 * B))), __float_as_uint((float)(int8_t)(x >> (8 * A))), 0x07060302u);
+}
+
+// ... unsigned ones.
+template <int A, int B>
+__device__ __forceinline__ uint32_t code_pair(uint32_t x) {
+  return __builtin_amdgcn_perm(__float_as_uint((float)((x >> (8 * B)) & 255u)), __float_as_uint((float)((x >> (8 * A)) & 255u)), 0x07060302u);
 }
 
 // Constants of the 4-bit form, in vector registers: an instruction takes one scalar operand only.
@@ -95,16 +103,22 @@ __device__ __forceinline__ bf16x8 operand(const u32x4 (&w)[Format<DT, BITS>::NC]
   u32x4 u;
   if constexpr (Format<DT, BITS>::kMantissa) {
     const uint32_t x = w[0][j];
-    u[0] = ((x << 3) & c.mask) | c.one;
-    u[1] = ((x >> 1) & c.mask) | c.one;
-    u[2] = ((x >> 5) & c.mask) | c.one;
-    u[3] = ((x >> 9) & c.mask) | c.one;
+    u[0] = (x & c.mask) | c.one;
+    u[1] = ((x >> 4) & c.mask) | c.one;
+    u[2] = ((x >> 8) & c.mask) | c.one;
+    u[3] = (rotate_right(x, 12) & c.mask) | c.one;
   } else if constexpr (BITS == 4) {   // a code in the upper half of a byte: 16 c - 128 as a signed byte
-    const uint32_t even = ((w[0][j] << 4) & 0xf0f0f0f0u) ^ 0x80808080u, odd = (w[0][j] & 0xf0f0f0f0u) ^ 0x80808080u;
+    const uint32_t even = (rotate_right(w[0][j], 31) & 0xf0f0f0f0u) ^ 0x80808080u, odd = (rotate_right(w[0][j], 3) & 0xf0f0f0f0u) ^ 0x80808080u;
     u[0] = byte_pair<0, 2>(even);
     u[1] = byte_pair<0, 2>(odd);
     u[2] = byte_pair<1, 3>(even);
     u[3] = byte_pair<1, 3>(odd);
+  } else if constexpr (Format<DT, BITS>::kPlain) {
+    const uint32_t lo = w[j >> 1][2 * (j & 1)], hi = w[j >> 1][2 * (j & 1) + 1];
+    u[0] = code_pair<0, 1>(lo);
+    u[1] = code_pair<2, 3>(lo);
+    u[2] = code_pair<0, 1>(hi);
+    u[3] = code_pair<2, 3>(hi);
   } else if constexpr (BITS == 8) {
     const uint32_t lo = w[j >> 1][2 * (j & 1)] ^ 0x80808080u, hi = w[j >> 1][2 * (j & 1) + 1] ^ 0x80808080u;
     u[0] = byte_pair<0, 1>(lo);
@@ -334,7 +348,7 @@ struct Tiles {
           pair_of<DT>(kp[s], e, sc, lo);
           off = fmaf(q[s][e], lo, off);
           qs[e] = q[s][e] * (sc * (1.f / F::kTimes));
-          off = fmaf(qs[e], -F::kBias, off);
+          if constexpr (!F::kPlain) off = fmaf(qs[e], -F::kBias, off);
         }
         split_terms<F::NTK>(qs, b[s]);
       } else if constexpr (DT == THK_BF16) {
@@ -401,7 +415,7 @@ struct Tiles {
             pair_of<DT>(vp[gh], e, sc, lo);
             st.off[half] = fmaf(p[e], lo, st.off[half]);
             p[e] *= sc * (1.f / F::kTimes);
-            st.off[half] = fmaf(p[e], -F::kBias, st.off[half]);
+            if constexpr (!F::kPlain) st.off[half] = fmaf(p[e], -F::kBias, st.off[half]);
           }
         }
         bf16x8 b[F::NTV];
