@@ -13,8 +13,8 @@
 //   unit of 8 bytes (8-bit codes):  cell k = j 2 k, 2 k + 1
 //   unit of 16 bytes (bf16):        cell k = j k
 //   unit of 32 bytes (fp32):        cells 2 j, 2 j + 1
-// 4-bit units hold code 2 p at bits 4 p and code 2 p + 1 at bits 16 + 4 p of a word that is stored rotated by three to the left:
-// two neighbours are one shift (the first two: none) and one mask away from the upper bits of two bf16 mantissas.
+// 4-bit units hold code 2 p at bits 4 p and code 2 p + 1 at bits 16 + 4 p: two neighbours are one shift and one mask away
+// from the two halves of a word.
 // A parameter is a pair (scale, minimum) of the element type; the pairs of a group's eight channels (keys) or rows (values)
 // lie together, groups in order.
 #pragma once
@@ -49,8 +49,6 @@ inline PagedLayout paged_layout(int dtype, int bits, int T) {
 __device__ __forceinline__ int scalar_load(const int32_t *p, int64_t i) {
   return ((__attribute__((address_space(4))) const int32_t *)(uintptr_t)p)[i];
 }
-
-__device__ __forceinline__ uint32_t rotate_right(uint32_t x, int n) { return __builtin_amdgcn_alignbit(x, x, n); }
 
 // Division by a number that is known when the call is planned, as a product: n * ceil(2^s / d) >> s is n / d for n < 2^24,
 // with s = 40 for d < 2^16 (the rounding up adds less than n / 2^40 < 2^-16 < 1 / d) and 48 from there on (the product stays

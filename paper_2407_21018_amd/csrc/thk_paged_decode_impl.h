@@ -103,12 +103,12 @@ __device__ __forceinline__ bf16x8 operand(const u32x4 (&w)[Format<DT, BITS>::NC]
   u32x4 u;
   if constexpr (Format<DT, BITS>::kMantissa) {
     const uint32_t x = w[0][j];
-    u[0] = (x & c.mask) | c.one;
-    u[1] = ((x >> 4) & c.mask) | c.one;
-    u[2] = ((x >> 8) & c.mask) | c.one;
-    u[3] = (rotate_right(x, 12) & c.mask) | c.one;
+    u[0] = ((x << 3) & c.mask) | c.one;
+    u[1] = ((x >> 1) & c.mask) | c.one;
+    u[2] = ((x >> 5) & c.mask) | c.one;
+    u[3] = ((x >> 9) & c.mask) | c.one;
   } else if constexpr (BITS == 4) {   // a code in the upper half of a byte: 16 c - 128 as a signed byte
-    const uint32_t even = (rotate_right(w[0][j], 31) & 0xf0f0f0f0u) ^ 0x80808080u, odd = (rotate_right(w[0][j], 3) & 0xf0f0f0f0u) ^ 0x80808080u;
+    const uint32_t even = ((w[0][j] << 4) & 0xf0f0f0f0u) ^ 0x80808080u, odd = (w[0][j] & 0xf0f0f0f0u) ^ 0x80808080u;
     u[0] = byte_pair<0, 2>(even);
     u[1] = byte_pair<0, 2>(odd);
     u[2] = byte_pair<1, 3>(even);

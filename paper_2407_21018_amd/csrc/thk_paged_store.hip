@@ -142,10 +142,7 @@ __device__ __forceinline__ void encode_group(const float (&x)[4][8], const bool 
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int w = 0; w < BITS / 4; ++w) {
-      word[j][w] = ok[j] ? word[j][w] - rest : 0u;
-      if constexpr (BITS == 4) word[j][w] = rotate_right(word[j][w], 29);
-    }
+    for (int w = 0; w < BITS / 4; ++w) word[j][w] = ok[j] ? word[j][w] - rest : 0u;
   if constexpr (BITS == 4) {
     st_stream((u32x4 *)(dst + m * 16), u32x4{word[0][0], word[1][0], word[2][0], word[3][0]});
   } else {
@@ -272,7 +269,7 @@ __device__ __forceinline__ void decode_group(const char *src, const char *par, i
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       uint32_t c;
-      if constexpr (BITS == 4) c = (rotate_right(w[0][j], 3) >> (4 * (e >> 1) + 16 * (e & 1))) & 15u;
+      if constexpr (BITS == 4) c = (w[0][j] >> (4 * (e >> 1) + 16 * (e & 1))) & 15u;
       else c = (w[j >> 1][2 * (j & 1) + (e >> 2)] >> (8 * (e & 3))) & 255u;
       x[j][e] = fmaf((float)c, s[e], lo[e]);
     }
