@@ -3,6 +3,8 @@
 Everything a call must not use holds NaN: the pool before it is written, source rows past a sequence's count, tail rows
 past theirs, outputs before the call.
 """
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -532,3 +534,32 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for out, want in zip(outs, wants):
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("bits", [0, 4, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_pools_laid_out_by_others(dtype, bits, monkeypatch):
+    """The pools of the measured cases are laid out there, from the description of a tile: rows in them are read as what they are."""
+    monkeypatch.syspath_prepend(os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    from perf import operators as O
+    for T, N_q, tail in ((51, 2, 20), (76, 16, 0)):
+        case = O._case("x", "decode", dtype=dtype, bits=bits, B=3, N_q=N_q, N_kv=2, S=333, T=T, page_rows=64, cap=64, tail=tail, ragged=True)
+        st = O.prepare(case, 5)
+        O._setup(st)
+        got = O._run_own(st)["out"].double()
+        want = O.exact(case, 5)["out"]
+        # outputs are rounded once; terms and sums as in _check_attention: twice c_z times the sizes of a logit's products, which are
+        # below 16, and the largest value, which is below 8
+        tol = {"bf16": 2.0 ** -8, "f32": 2.0 ** -23}[dtype] * want.abs() + {"bf16": 2.0 ** -16, "f32": 2.0 ** -20}[dtype] * 256
+        assert ((got - want).abs() <= tol).all()
+        ko = torch.zeros(1, 3, 2, 333, T, dtype=st["q"].dtype, device="cuda")
+        thk.thk_paged_read(st["shape"], st["pages"], st["pool"], st["table"], None, st["rows"], ko, None, 333)
+        again = torch.full_like(st["pool"], 255)
+        v = torch.zeros(1, 3, 2, 333, D, dtype=st["q"].dtype, device="cuda")
+        thk.thk_paged_read(st["shape"], st["pages"], st["pool"], st["table"], None, st["rows"], None, v, 333)
+        k = torch.zeros_like(v).scatter_(4, st["idx"].long()[..., None, :].expand(1, 3, 2, 333, T), ko)
+        if bits == 0:   # elements go back to where they came from
+            thk.thk_paged_write(st["shape"], st["pages"], k, v, 333, st["rows"], None, st["idx"], st["table"], again)
+            for b, n in enumerate(st["rows"].tolist()):
+                pages = st["table"][b, :n // 64].long()
+                assert torch.equal(again[:, pages], st["pool"][:, pages])
