@@ -756,9 +756,10 @@ constexpr PagedTimes kPagedTimes[2][3] = {   // [fp32, bf16][elements, 4 bits, 8
     {{0.468, 0.147, 0, 0.069, 1.007, 3.285, 3.462, 0.254}, {0.225, 0.023, 0.160, 0.232, 0.817, 5.590, 2.090, 0.076}, {0.190, 0.170, 0.105, 0.105, 1.709, 5.360, 1.799, 0.051}}};
 
 // Cut by the lengths on the device where the call is long enough for it not to matter: the work of a batch of the longest ones,
-// spread over the card, is 32 tiles a compute unit (some 10 us) or more.
+// spread over the card, is 32 tiles a compute unit (some 10 us) or more.  (Every block looks at all lengths, up to six times:
+// more sequences than the estimate would cut at all, where the caller gives a count for them, are cut by the bound.)
 bool paged_by_lengths(const thk_shape *s, const Split &sp) {
-  return sp.n > 1 && (s->B > 1 || sp.rows >= 64 * kTile) && units_of(s) * ceil_div(s->S, kTile) >= 32 * kCUs;
+  return sp.n > 1 && s->B <= 2 * kCUs && (s->B > 1 || sp.rows >= 64 * kTile) && units_of(s) * ceil_div(s->S, kTile) >= 32 * kCUs;
 }
 
 Split paged_split(const thk_shape *s, int bits) {

@@ -1,4 +1,5 @@
-// The paged cache: where a tile's codes and parameters lie, and the launchers' arguments.
+// The paged cache: where a tile's codes and parameters lie, and the launchers' arguments.  (perf/operators.py lays pools out by
+// this description; a change of it is a change there.)
 //
 // A tile is 64 rows of one unit.  Its bytes, in this order: key codes, value codes, key parameters, value parameters (the
 // last two only with codes).  Codes come in units of eight -- eight kept channels of one row for keys, eight rows of one

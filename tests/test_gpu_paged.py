@@ -386,6 +386,15 @@ def test_pieces_by_the_lengths(dtype, bits, case):
     _check_attention(c, c.decode())
 
 
+def test_many_sequences_in_pieces():
+    """More sequences than are cut by their lengths."""
+    rows = [int(x) for x in np.random.default_rng(78).integers(0, 300, 600)]
+    c = Cache("bf16", 4, 1, 600, 1, 2, 64, rows, 64, [b % 5 for b in range(600)], 4, seed=90, n_split=3)
+    c.write()
+    c.shape.S = 2000
+    _check_attention(c, c.decode())
+
+
 def test_offsets_past_32_bits():
     """A pool of more than 4 GiB whose first and last pages are in use, and tails likewise."""
     c = Cache("bf16", 0, 1, 2, 8, 4, 128, [256, 130], 256, tails=[10, 64], cap=64, seed=6, spare=0)
