@@ -572,3 +572,35 @@ def test_pools_laid_out_by_others(dtype, bits, monkeypatch):
             for b, n in enumerate(st["rows"].tolist()):
                 pages = st["table"][b, :n // 64].long()
                 assert torch.equal(again[:, pages], st["pool"][:, pages])
+
+
+@pytest.mark.parametrize("seed", range(48))
+def test_random_shapes(seed):
+    """Shapes drawn from a seeded generator: stored, read back, attended over."""
+    r = np.random.default_rng(4000 + seed)
+    pick = lambda *x: x[r.integers(len(x))]   # noqa: E731
+    dtype, bits = pick("bf16", "bf16", "f32"), pick(0, 4, 8)
+    L, B, N_kv, G, T = int(r.integers(1, 3)), int(r.integers(1, 7)), int(r.integers(1, 4)), pick(1, 2, 3, 4, 5, 7, 8, 12, 16, 17), int(r.integers(1, 129))
+    most = int(np.exp(r.uniform(0, np.log(3000))))
+    rows = [int(x) for x in r.integers(0, most + 1, B)]
+    cap = pick(0, 1, 37, 64, 100, 130)
+    tails = [int(x) for x in r.integers(0, cap + 1, B)] if cap else None
+    page_rows, n_split = pick(64, 128, 512), pick(0, 0, 1, 2, 3, 9)
+    print("random", seed, dtype, bits, L, B, N_kv, G, T, rows, page_rows, tails, cap, n_split, flush=True)
+    c = Cache(dtype, bits, L, B, N_kv, G, T, rows, page_rows, tails, cap, seed=100 + seed, n_split=n_split)
+    c.write()
+    out_rows = c.S + int(r.integers(0, 5))
+    ko = torch.full((L, B, N_kv, out_rows, T), 7.0, dtype=TDT[dtype], device="cuda")
+    vo = torch.full((L, B, N_kv, out_rows, D), 7.0, dtype=TDT[dtype], device="cuda")
+    thk.thk_paged_read(c.shape, c.pages, c.pool, c.table, None, c.s_pages, ko, vo, out_rows)
+    out = c.decode()
+    torch.cuda.synchronize()
+    for b, n in enumerate(rows):
+        for l in range(L):
+            for h in range(N_kv):
+                k, v, _, _, _ = c.unit(l, b, h)
+                for got, want in ((_np(ko[l, b, h]), k), (_np(vo[l, b, h]), v)):
+                    assert np.all(np.abs(got[:n] - want) <= (0 if bits == 0 else HALF_STEP[dtype]) * np.abs(want))
+                    assert np.all(got[n:] == 7)
+    _check_attention(c, out)
+    assert torch.equal(c.decode(), out)
