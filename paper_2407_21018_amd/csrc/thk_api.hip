@@ -1325,7 +1325,7 @@ thk_status thk_paged_write(const thk_shape *s, const thk_pages *p, const void *k
   a.T = s->T;
   a.tiles = (int32_t)ceil_div(a.most, kTile);
   a.by_tiles = Divisor(a.tiles);
-  a.apart = paged_apart(a.units * a.tiles);
+  a.apart = paged_apart(s->dtype, a.units * a.tiles);
   if ((uint64_t)a.units * a.tiles > kMaxThreads / 256) return THK_ERR_SHAPE;
   return failed(launch_paged_write(s->dtype, p->bits, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
 }
@@ -1348,7 +1348,7 @@ thk_status thk_paged_read(const thk_shape *s, const thk_pages *p, const void *po
   a.T = s->T; a.ld = ld_of(s);
   a.tiles = (int32_t)ceil_div(a.most + (row0 != nullptr ? kTile - 1 : 0), kTile);   // rows that begin inside a tile
   a.by_tiles = Divisor(a.tiles);
-  a.apart = paged_apart(a.units * a.tiles);
+  a.apart = paged_apart(s->dtype, a.units * a.tiles);
   if ((uint64_t)a.units * a.tiles > kMaxThreads / 256) return THK_ERR_SHAPE;
   return failed(launch_paged_read(s->dtype, p->bits, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
 }

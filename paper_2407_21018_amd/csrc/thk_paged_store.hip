@@ -152,7 +152,7 @@ __device__ __forceinline__ void encode_group(const float (&x)[4][8], const bool 
   }
 }
 
-// One block per (unit, tile of the call), or in calls that leave the card empty (paged_apart) two: one for the keys, which go
+// One block per (unit, tile of the call), or in calls that leave room for it (paged_apart) two: one for the keys, which go
 // through LDS, where their kept channels are picked, and one for the values, which go straight from memory to the lane that
 // encodes them.
 // Bound by memory, at the rate of a copy (5.3 to 5.5 TB/s read + write): bf16 elements, 64 units x 8191 rows, 51 channels 86 us;
