@@ -27,8 +27,9 @@
 //
 // Measured (kernel alone; a kernel that only reads the bytes reaches 7.1 TB/s): bf16 elements, 8 units of four heads x 131072 rows
 // 62 us, 6.5 TB/s; 4-bit codes, 640 units of one head, up to 8192 rows 79 us, 4.5 TB/s (vector unit busy half of the time, matrix
-// cores a fifth), 256 units of four heads x 32768 rows 147 to 185 us by the card's clock, 5.0 to 6.2 TB/s; 8-bit codes, 64 units of
-// eight heads, up to 8191 rows 23 us, 3.4 TB/s: pieces of 32 tiles, four steps of a wave, whose ramp is as long as they are.
+// cores a fifth), 256 units of four heads x 32768 rows 146 us, 6.3 TB/s, and up to 216 when such calls follow one another for some
+// ms and the card lowers its clock; 8-bit codes, 64 units of eight heads, up to 8191 rows 22 us, 3.5 TB/s: pieces of some 24 tiles,
+// three steps of a wave, whose ramp is as long as they are.
 // 8 units x 1000 rows 5.4 us: launch, three trips to memory one after another (lengths, table, tiles), the states' exchange.
 #pragma once
 #include "thk_paged.h"

@@ -157,7 +157,7 @@ __device__ __forceinline__ void encode_group(const float (&x)[4][8], const bool 
 // encodes them.
 // Bound by memory, at the rate of a copy (5.3 to 5.5 TB/s read + write): bf16 elements, 64 units x 8191 rows, 51 channels 86 us;
 // 4 bits, 1024 units x 4096 rows, 76 channels 481 us.  fp32 rows of keys take 34 KB of LDS, four blocks of a compute unit: 32
-// units of up to 2048 rows, 8 bits 18 us, 3.7 TB/s in its single round of blocks.
+// units of up to 2048 rows, 8 bits 17 us, 3.7 TB/s in its single round of blocks.
 template <int DT, int BITS>
 __global__ __launch_bounds__(256) void k_paged_write(PagedWriteArgs a) {
   using E = Elem<DT>;
@@ -276,7 +276,7 @@ __device__ __forceinline__ void decode_group(const char *src, const char *par, i
 }
 
 // One block per (unit, tile that holds rows of the call), or two as above.  Bound by memory as the write is: the cases there
-// take 75 us (5.0 TB/s), 400 us (5.5) and 13 us (2.9: one round of blocks).
+// take 75 us (5.0 TB/s), 400 us (5.5) and 14 us (2.9: one round of blocks).
 template <int DT, int BITS>
 __global__ __launch_bounds__(256) void k_paged_read(PagedReadArgs a) {
   using E = Elem<DT>;
