@@ -421,8 +421,10 @@ thk_status thk_tail_flush(const thk_shape *shape, const int16_t *idx, void *k_pr
  *     code of x = min(N, rint(fl(fl(x - m) / s))), ties to even; 0 where s == 0
  * and a code c stands for m + c s.  m and s are held in the element type.  An element is off by
  * at most s / 2 (plus, for bf16 caches of 8-bit codes, what rounding s to 8 bits moves the last
- * code: s / 2).  What is stored as codes must be finite, max x - min x too: of a tile that holds an
- * infinity or NaN the codes and scales are unspecified.  Rows stored as elements may be anything.
+ * code: s / 2).  A scale below the type's normal numbers (2^-126) has fewer bits: there an element
+ * may also be off by the group's range less N s, the whole range where s rounds to 0.  What is
+ * stored as codes must be finite, max x - min x too: of a tile that holds an infinity or NaN the
+ * codes and scales are unspecified.  Rows stored as elements may be anything.
  */
 typedef struct {
   int32_t bits;      /* 0: rows in the element type; 4 or 8: codes                      */

@@ -125,7 +125,9 @@ __device__ __forceinline__ void encode_group(const float (&x)[4][8], const bool 
       } else {
         y = se > 0.f ? t / se : 0.f;
       }
-      if constexpr (BITS == 8 || DT == THK_F32) y = fminf(y, top);   // (a scale of 8 bits is at most 2^-8 off: 15.06)
+      // A normal scale of 8 bits is at most 2^-8 off, and the last quotient 15.06 at most: with 4 bits it needs no bound.  A scale
+      // below the normal numbers has fewer bits and may be a third off; it takes the division, and the bound.
+      if constexpr (BITS == 8 || DT == THK_F32 || decltype(divide)::value) y = fminf(y, top);
       word[j][e / (32 / BITS)] += __float_as_uint(y + kMagic) << place(e);
     }
   };

@@ -165,6 +165,42 @@ def test_groups_without_range_and_with_extreme_ones(dtype, bits):
         assert np.all(np.abs(got - want) <= HALF_STEP[dtype] * np.abs(want) + least / 2)
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scales_below_the_normal_numbers_beside_ordinary_ones(dtype, bits):
+    """Groups whose range is 8 to 300 of the type's least number: their scales have few bits, quotients go up to half as far again as
+    the last code.  What an ordinary group beside them holds is its own."""
+    c = Cache(dtype, bits, 1, 1, 4, 1, 128, [320], 64, seed=17)
+    least = 2.0 ** (-149 if dtype == "f32" else -133)
+    r = np.random.default_rng(170)
+
+    def tiny(groups, n):
+        """[groups, n]: whole multiples of the least number, from 0 (or from below it) over a range of 8 .. 300."""
+        span = (8 + np.arange(groups) % 293)[:, None]
+        x = r.integers(0, span + 1, (groups, n))
+        x[:, 0], x[:, 1] = 0, span[:, 0]
+        return (x - r.integers(0, 2, (groups, 1)) * 40) * least
+
+    for h in range(4):
+        k, v = _np(c.k[0, 0, h]), _np(c.v[0, 0, h])
+        for t in range(5):
+            some = r.random(D) < 0.5
+            k[64 * t:64 * t + 64, some] = tiny(some.sum(), 64).T
+        halves = v.reshape(-1, 64)
+        some = r.random(len(halves)) < 0.5
+        halves[some] = tiny(some.sum(), 64)
+        c.k[0, 0, h], c.v[0, 0, h] = (torch.from_numpy(x).to(TDT[dtype]).cuda() for x in (k, v))
+    c.write()
+    ko, vo = (torch.empty(1, 1, 4, 320, D, dtype=TDT[dtype], device="cuda") for _ in range(2))
+    thk.thk_paged_read(c.shape, c.pages, c.pool, c.table, None, c.s_pages, ko, vo, 320)
+    torch.cuda.synchronize()
+    for h in range(4):
+        k, v, _, _, _ = c.unit(0, 0, h)
+        for name, got, want in (("keys", _np(ko[0, 0, h]), k), ("values", _np(vo[0, 0, h]), v)):
+            bad = np.abs(got - want) > HALF_STEP[dtype] * np.abs(want) + least / 2
+            assert not bad.any(), (name, h, int(bad.sum()), np.abs(got - want).max())
+
+
 @pytest.mark.parametrize("dtype,bits", [("bf16", 4), ("bf16", 0), ("f32", 8)])
 def test_a_chunk_after_a_chunk(dtype, bits):
     """A prompt stored in two calls is the prompt stored in one; sequences whose first row is not a tile's are left alone."""
