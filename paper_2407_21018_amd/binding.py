@@ -479,6 +479,13 @@ class _Tensors:
             return x
         return self.address(x, -(-nbytes // x.element_size()), name, None)
 
+    def workspace(self, ws):
+        """(address, bytes), as _ws."""
+        if ws is None:
+            return None, 0
+        x, nbytes = ws if isinstance(ws, tuple) else (ws, ws.numel() * ws.element_size())
+        return self.raw(x, nbytes, "ws"), nbytes
+
 
 def thk_paged_write(shape, pages, k, v, src_rows, n_rows, row0, idx, table, pool, stream=None):
     w = "thk_paged_write"
@@ -533,7 +540,7 @@ def thk_decode_attn_paged(shape, pages, q, pool, table, s_pages, idx, k_tail, v_
                                         t.raw(pool, thk_paged_pool_bytes(shape, pages), "pool"),
                                         t.ints(table, shape.B * pages.max_pages, "table"), t.ints(s_pages, shape.B, "s_pages"),
                                         t.idx(idx, U * T), t.rows(k_tail, m, "k_tail"), t.rows(v_tail, m, "v_tail"),
-                                        t.ints(s_tail, shape.B, "s_tail"), s_tail_cap, t.rows(out, H * D, "out"), *_ws(ws),
+                                        t.ints(s_tail, shape.B, "s_tail"), s_tail_cap, t.rows(out, H * D, "out"), *t.workspace(ws),
                                         _stream(stream)), w)
 
 

@@ -91,6 +91,14 @@ struct Args {
   int16_t *kept(PyObject *x, int64_t n) { return (int16_t *)here(x, n, at::kShort); }
   void *pool(PyObject *x) { return here(x, ok ? (int64_t)f_pool_bytes(shape, pages) : 0, at::kByte); }
   int32_t *table(PyObject *x) { return ints(x, ok ? count(shape->B, pages->max_pages) : 0); }
+  void *workspace_here(PyObject *x, size_t &bytes) {
+    bytes = 0;
+    if (x == Py_None) return nullptr;
+    if (!ok || !plain(x)) return ok = false, nullptr;
+    void *const p = here(x, 0, THPVariable_Unpack(x).scalar_type());
+    if (ok) bytes = THPVariable_Unpack(x).nbytes();
+    return p;
+  }
 
   static bool plain(PyObject *x) { return THPVariable_CheckExact(x); }
   // address of a tensor of at least n elements
@@ -281,7 +289,7 @@ PyObject *decode_attn_paged(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }
     void *out = x.rows_here(a[11], hn);
     size_t bytes = 0;
-    void *ws = x.workspace(a[12], bytes), *st = x.stream(a[13]);
+    void *ws = x.workspace_here(a[12], bytes), *st = x.stream(a[13]);
     if (!x.ok) return not_taken();
     return issue([&] { return f_decode_paged(s, x.pages, q, pool, table, s_pages, idx, kt, vt, s_tail, cap, out, ws, bytes, st); });
   });

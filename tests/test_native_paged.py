@@ -161,6 +161,29 @@ def test_other_forms_are_left_to_the_python_code(name, make):
 
 
 @pytest.mark.gpu
+def test_workspaces_are_checked_by_both():
+    native, public, args = _calls("cuda")["decode_attn_paged"]
+    args["shape"].n_split = 3
+    n = thk.thk_workspace_bytes(args["shape"], thk.THK_OP_DECODE_PAGED)
+    for bad in (torch.empty(n, dtype=torch.uint8), torch.empty(1, dtype=torch.uint8, device="cuda").expand(n),
+                torch.empty(2 * n, dtype=torch.uint8, device="cuda")[::2], (torch.empty(n, dtype=torch.uint8), n),
+                (torch.empty(n - 1, dtype=torch.uint8, device="cuda"), n)):
+        assert native(*{**args, "ws": bad}.values()) == -1
+        with pytest.raises(ValueError, match="ws "):
+            public(*{**args, "ws": bad}.values())
+    for short in (None, torch.empty(n - 1, dtype=torch.uint8, device="cuda")):
+        with pytest.raises(thk.ThkError) as e:
+            public(*{**args, "ws": short}.values())
+        assert e.value.status == 5
+    outs = []
+    for ws in (torch.empty(n, dtype=torch.uint8, device="cuda"), torch.empty(-(-n // 4), device="cuda"), (torch.empty(n, dtype=torch.uint8, device="cuda"), n)):
+        outs.append(torch.zeros_like(args["out"]))
+        public(*{**args, "ws": ws, "out": outs[-1]}.values())
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@pytest.mark.gpu
 def test_two_graphs_share_a_workspace():
     """Two captured calls of different sizes with one workspace, replayed in turn on one stream: each has its own answer, every time."""
     torch.manual_seed(3)

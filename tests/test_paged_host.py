@@ -176,6 +176,14 @@ def test_tensors_are_checked_before_the_library_sees_them():
         thk.thk_paged_read(s, p, torch.zeros(16, dtype=torch.uint8), A, None, A, A, A, 1000, stream=0)
 
 
+@pytest.mark.parametrize("ws", [torch.empty(1 << 20, dtype=torch.uint8), (torch.empty(1 << 20, dtype=torch.uint8), 1 << 20), torch.empty(4).expand(1 << 18, 4)])
+def test_a_workspace_on_the_host_is_refused(ws):
+    """... and so is one whose elements are fewer than they look."""
+    s, p = _shape(n_split=3), _pages()
+    with pytest.raises(ValueError, match="ws must be"):
+        thk.thk_decode_attn_paged(s, p, A, A, A, A, A, A, A, A, 64, A, ws, stream=0)
+
+
 # ---- the oracle ------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("bits", [4, 8])
