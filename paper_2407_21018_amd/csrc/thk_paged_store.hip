@@ -38,11 +38,13 @@ __device__ __forceinline__ float extreme_of(const float (&v)[8], int m) {
   for (int e = 0; e < 4; ++e) x[e] = pick(b3 ? v[e + 4] : v[e], from_lane<kXor8>(b3 ? v[e] : v[e + 4]));
 #pragma unroll
   for (int e = 0; e < 2; ++e) y[e] = pick(b2 ? x[e + 2] : x[e], from_lane<kXor7>(b2 ? x[e] : x[e + 2]));
+  // A move between lanes must not read what one of the two instructions in front of it wrote, and the compiler, which sees to
+  // that for its own instructions, does not look into these: neither the result of the next step may be, nor the function's.
   float z = pick(b1 ? y[1] : y[0], from_lane<kXor2>(b1 ? y[0] : y[1]));
-  // a move between lanes must not read what one of the two instructions in front of it wrote, and the compiler, which sees to
-  // that for its own instructions, does not look into these
   asm("s_nop 1" : "+v"(z));
-  return pick(z, from_lane<kXor1>(z));
+  z = pick(z, from_lane<kXor1>(z));
+  asm("s_nop 1" : "+v"(z));
+  return z;
 }
 
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
