@@ -424,7 +424,7 @@ thk_status thk_tail_flush(const thk_shape *shape, const int16_t *idx, void *k_pr
  * code: s / 2).  A scale below the type's normal numbers (2^-126) has fewer bits: there an element
  * may also be off by the group's range less N s, the whole range where s rounds to 0.  What is
  * stored as codes must be finite, max x - min x too: of a tile that holds an infinity or NaN the
- * codes and scales are unspecified.  Rows stored as elements may be anything.
+ * codes and scales are unspecified.  Elements may be anything, and are read back as they are.
  */
 typedef struct {
   int32_t bits;      /* 0: rows in the element type; 4 or 8: codes                      */
@@ -478,8 +478,10 @@ thk_status thk_tail_append_ragged(const thk_shape *shape, const void *k_new, con
  * the full-width tail (at most s_tail_cap; s_tail_cap = 0: no tail, and k_tail, v_tail, s_tail are
  * not looked at).  One softmax over both; a sequence without any row gets zeros.  Rows past the
  * counts are not used, whatever they hold: rows of the tail are not read, rows of a tile have
- * weight zero, and elements are taken out.  fp32 arithmetic: codes enter the matrix cores as whole numbers, what multiplies
- * them as two (bf16) or three (fp32) bf16 terms.
+ * weight zero, and elements are taken out.  Of the rows that are used the values must be finite (an infinity or NaN makes its channel
+ * NaN or infinite), and keys too, but that a key whose infinities make its logit -inf has weight zero (in all rows: zeros), as
+ * the formula has it.  fp32 arithmetic: codes enter the matrix cores as whole numbers, what multiplies them as two (bf16) or
+ * three (fp32) bf16 terms.
  * shape->S is below 2^31 - 64.  A unit's rows are cut into pieces that are joined by a second launch: about n_split of
  * them (0: as many as the estimate says), each of whole tiles, the last with the tail.  Short calls cut by shape->S, so that
  * the pieces of a sequence depend on nothing but its own length.  Long calls of several sequences cut by the lengths on the

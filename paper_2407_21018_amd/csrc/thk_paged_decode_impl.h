@@ -251,6 +251,7 @@ struct Tiles {
   static constexpr int kPairs = 8 * 2 * Elem<DT>::EB;   // bytes of a group's parameters
   // an instruction waits for the one in front of it in its own sum: so many sums in turn (fewer where the registers are full)
   static constexpr int kInTurn = F::kCodes && NST == 3 && CL * BITS == 16 ? 2 : 4;
+  static constexpr int kPastEnd = 1 << 20;   // (a tile has at most 64 KB)
   u32x4 kc[CL][NST][F::NC], kp[F::kCodes ? NST : 1][NP];
   u32x4 vc[CL][4][F::NC], vp[F::kCodes ? 4 : 1][NP];
 
@@ -264,10 +265,10 @@ struct Tiles {
   __device__ __forceinline__ void load_keys(const char *const (&t)[CL], int bytes, GlobalPtr own, const PagedLayout &lay, int m, int h) {
 #pragma unroll
     for (int s = 0; s < NST; ++s) {
-      // group 4 s + h; those past the last are what lies behind the keys in the tile, and meet zeros of the query.  (Elements: the
-      // last group again, which belongs to the same rows.  What lies behind it need not be finite.)
+      // group 4 s + h; of codes those past the last are what lies behind the keys in the tile, which is finite and meets zeros of the
+      // query.  (Elements there need not be finite, nor those of a group that is there: an offset past the tile's end loads zeros.)
       if constexpr (F::kCodes) load_pairs<DT>(own + lay.k_params + s * 4 * kPairs, kp[s]);
-      const int at = F::kCodes ? h * 64 * F::UB : min(4 * s + h, lay.chunks - 1) * 64 * F::UB, off = F::kCodes ? s * 256 * F::UB : 0;
+      const int at = F::kCodes ? h * 64 * F::UB : 4 * s + h < lay.chunks ? (4 * s + h) * 64 * F::UB : kPastEnd, off = F::kCodes ? s * 256 * F::UB : 0;
 #pragma unroll
       for (int x = 0; x < CL; ++x)
 #pragma unroll

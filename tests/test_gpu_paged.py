@@ -363,6 +363,39 @@ def test_elements_past_the_count_may_be_anything(dtype, T):
             assert np.abs(_np(out[0, b, h * 3:(h + 1) * 3]) - want).max() <= tol
 
 
+@pytest.mark.parametrize("T", [1, 8, 33, 51, 64, 72, 97, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_infinite_keys_of_element_pages_have_no_weight(dtype, T):
+    """Rows in use with an infinity in one kept channel, of the sign that makes the logit -inf, in each of the channels; likewise in the
+    tail; a sequence that has no other rows."""
+    c = Cache(dtype, 0, 1, 3, 2, 1, T, [300, 129, 70], 64, tails=[40, 64, 3], cap=64, seed=180 + T)
+    live = {}
+    for b in range(3):
+        for h in range(2):
+            idx, sign = c.idx[0, b, h].long(), torch.sign(c.q[0, b, h]).float()
+            assert (sign != 0).all()
+            for name, rows, channels in (("k", c.rows[b], idx), ("kt", c.tails[b], torch.arange(D, device="cuda"))):
+                hit = np.arange(1, rows, 2) if b < 2 else np.arange(rows)
+                at = channels[torch.from_numpy(hit).cuda() // 2 % len(channels)]
+                getattr(c, name)[0, b, h, torch.from_numpy(hit).cuda(), at] = (-float("inf") * sign[at]).to(TDT[dtype])
+                live[name, b, h] = np.setdiff1d(np.arange(rows), hit)
+    c.write()
+    out = c.decode()
+    torch.cuda.synchronize()
+    c_z = {"bf16": 2.0 ** -16, "f32": 2.0 ** -20}[dtype]   # as in _check_attention
+    for b in range(3):
+        for h in range(2):
+            k, v, kt, vt, idx = c.unit(0, b, h)
+            ks, ts = live["k", b, h], live["kt", b, h]
+            q, got = _np(c.q[0, b, h:h + 1]), _np(out[0, b, h:h + 1])
+            assert np.isfinite(k[ks]).all() and np.isfinite(kt[ts]).all() and (len(ks) > 0) == (b < 2)
+            want = P.attend(q, idx, k[ks], v[ks], kt[ts], vt[ts])
+            top = max(np.abs(v).max(), np.abs(vt).max())
+            size = 5.2 * np.abs(q[:, idx]) @ np.abs(k[ks]).max(0, initial=0) + np.abs(q) @ np.abs(kt[ts]).max(0, initial=0)
+            assert np.all(np.abs(got - want) <= HALF_STEP[dtype] * np.abs(want) + c_z * top * (2 * size[:, None] / np.sqrt(D) + 5.2)), (b, h)
+            assert b < 2 or not got.any()
+
+
 def test_pages_outside_the_pool_take_no_part():
     c = Cache("bf16", 4, 1, 2, 1, 4, 64, [256, 256], 64, tails=[3, 0], cap=64, seed=21)
     c.write()
