@@ -118,6 +118,42 @@ def test_rows_come_back_as_what_they_were_stored_as(dtype, bits, case):
             assert torch.all(ko[:, b, :, rows[b]:] == 7) and torch.all(vo[:, b, :, rows[b]:] == 7)   # the rest as it was
 
 
+# (B, N_kv, T, ld, rows): 1024 tiles of the grid (bf16; fp32: 512), up to which keys and values have blocks of their own, with the most
+# rows of row0 = 0; a tile a unit more; and ragged ones well past it
+LARGE = {"at": {"bf16": (4, 4, 51, 56, [4096, 4033, 1, 2048]), "f32": (2, 4, 51, 56, [4096, 100])},
+         "past": {"bf16": (4, 4, 76, 76, [4097, 64, 0, 4096]), "f32": (2, 4, 76, 76, [4097, 4096])},
+         "far": {"bf16": (3, 8, 33, 48, [6000, 5999, 17]), "f32": (2, 6, 128, 128, [5000, 4936])}}
+
+
+@pytest.mark.parametrize("size", LARGE)
+@pytest.mark.parametrize("bits", [0, 4, 8])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_writes_and_reads(dtype, bits, size):
+    """One block for a tile's keys and values: all rows, any range of them, with both outputs and with one."""
+    B, N_kv, T, ld, rows = LARGE[size][dtype]
+    print("large", dtype, bits, size, flush=True)
+    c = Cache(dtype, bits, 1, B, N_kv, 1, T, rows, 256, seed=300 + T)
+    c.write()
+    c.shape.ld_keep = ld
+    units = [[c.unit(0, b, h)[:2] for h in range(N_kv)] for b in range(B)]
+    inside = [min(37 + 64 * b, n) for b, n in enumerate(rows)]
+    for row0, n in ((None, rows), (inside, [x - y for x, y in zip(rows, inside)]), (inside, [min(x - y, 65) for x, y in zip(rows, inside)])):
+        for with_keys, with_values in ((True, True), (True, False), (False, True)):
+            ko = torch.full((1, B, N_kv, c.S, ld), 7.0, dtype=TDT[dtype], device="cuda") if with_keys else None
+            vo = torch.full((1, B, N_kv, c.S, D), 7.0, dtype=TDT[dtype], device="cuda") if with_values else None
+            thk.thk_paged_read(c.shape, c.pages, c.pool, c.table, None if row0 is None else _ints(row0), _ints(n), ko, vo, c.S)
+            torch.cuda.synchronize()
+            for b in range(B):
+                at = 0 if row0 is None else row0[b]
+                for out, which, width in ((ko, 0, T), (vo, 1, D)):
+                    if out is None:
+                        continue
+                    assert torch.all(out[0, b, :, n[b]:] == 7) and not out[0, b, :, :n[b], width:].any()
+                    got = _np(out[0, b, :, :n[b], :width])
+                    want = np.stack([units[b][h][which][at:at + n[b]] for h in range(N_kv)])
+                    assert np.all(np.abs(got - want) <= (0 if bits == 0 else HALF_STEP[dtype]) * np.abs(want)), (b, row0, which)
+
+
 @pytest.mark.parametrize("bits", [0, 4])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_any_range_of_rows_is_read(dtype, bits):
