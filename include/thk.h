@@ -453,8 +453,8 @@ thk_status thk_paged_write(const thk_shape *shape, const thk_pages *pages, const
 /*
  * Reads rows back: rows row0[b] .. row0[b] + n_rows[b] - 1 of sequence b, any row0 >= 0, to rows
  * 0 .. of k_out [L][B][N_kv][out_rows][ld_keep] (kept channels; columns past T are zeros) and
- * v_out [L][B][N_kv][out_rows][D], in the element type: m + c s rounded once.  Other rows of the
- * outputs stay as they are.  Either output may be NULL.  n_rows is bounded by the smaller of
+ * v_out [L][B][N_kv][out_rows][D], in the element type: m + c s rounded to fp32 and, for bf16, from there
+ * to bf16.  Other rows of the outputs stay as they are.  Either output may be NULL.  n_rows is bounded by the smaller of
  * shape->S and out_rows; what was never written there reads as whatever the pool holds.
  */
 thk_status thk_paged_read(const thk_shape *shape, const thk_pages *pages, const void *pool,

@@ -236,7 +236,7 @@ __global__ __launch_bounds__(256) void k_paged_write(PagedWriteArgs a) {
   encode_group<DT, BITS>(x, ok, dst + grp * 64 * a.p.lay.unit_bytes, dst + a.p.lay.k_params + grp * 8 * 2 * EB, m);
 }
 
-// The inverse of encode_group: what the lane's 32 codes stand for, rounded once to the element type.
+// The inverse of encode_group: what the lane's 32 codes stand for, rounded to fp32 (the store rounds to the element type).
 template <int DT, int BITS>
 __device__ __forceinline__ void decode_group(const char *src, const char *par, int m, float (&x)[4][8]) {
   constexpr int UB = BITS != 0 ? BITS : DT == THK_BF16 ? 16 : 32;

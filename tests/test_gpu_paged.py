@@ -237,6 +237,28 @@ def test_scales_below_the_normal_numbers_beside_ordinary_ones(dtype, bits):
             assert not bad.any(), (name, h, int(bad.sum()), np.abs(got - want).max())
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+def test_bf16_rows_are_rounded_through_fp32(bits):
+    """A minimum far below a step of fp32 decides a tie of m + c s between two bf16 numbers if that is rounded once; what is read is rounded
+    to fp32 first."""
+    c = Cache("bf16", bits, 1, 1, 2, 1, 128, [640], 128, seed=19)
+    g = torch.Generator().manual_seed(190)
+    x = (torch.rand(2, 640, 2, 64, generator=g) * 4 + 0.01) * torch.exp(torch.randn(2, 640, 2, 1, generator=g))
+    x[..., 0] = 2.0 ** -40
+    c.v[0, 0] = x.reshape(2, 640, D).to(torch.bfloat16).cuda()
+    c.k[0, 0] = x.reshape(2, 10, D, 64).transpose(2, 3).reshape(2, 640, D).to(torch.bfloat16).cuda()
+    c.write()
+    ko, vo = (torch.empty(1, 1, 2, 640, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    thk.thk_paged_read(c.shape, c.pages, c.pool, c.table, None, c.s_pages, ko, vo, 640)
+    torch.cuda.synchronize()
+    for h in range(2):
+        k, v, _, _, _ = c.unit(0, 0, h)
+        for got, want in ((_np(ko[0, 0, h]), k), (_np(vo[0, 0, h]), v)):
+            step = 2.0 ** (np.floor(np.log2(want)) - 7)
+            assert (np.rint(want / step) * step != P.round_to(want, "bf16")).sum() > 100   # round_to goes through fp32 too
+            assert np.array_equal(got, P.round_to(want, "bf16"))
+
+
 @pytest.mark.parametrize("dtype,bits", [("bf16", 4), ("bf16", 0), ("f32", 8)])
 def test_a_chunk_after_a_chunk(dtype, bits):
     """A prompt stored in two calls is the prompt stored in one; sequences whose first row is not a tile's are left alone."""
