@@ -710,7 +710,7 @@ thk_status check_pages(const thk_shape *s, const thk_pages *p) {
   if (st != THK_OK) return st;
   if (p == nullptr) return THK_ERR_NULL;
   if (p->bits != 0 && p->bits != 4 && p->bits != 8) return THK_ERR_UNSUPPORTED;
-  if (p->page_rows < kTile || p->page_rows > 65536 || (p->page_rows & (p->page_rows - 1)) != 0) return THK_ERR_SHAPE;
+  if (p->page_rows < kTile || p->page_rows > kMostTilesOfPage * kTile || (p->page_rows & (p->page_rows - 1)) != 0) return THK_ERR_SHAPE;
   if (p->max_pages < 1 || (int64_t)p->max_pages * p->page_rows > INT32_MAX) return THK_ERR_SHAPE;
   if (p->n_pages < 1 || p->n_pages > INT32_MAX || s->S > INT32_MAX - kTile) return THK_ERR_SHAPE;
   int64_t bytes = 0;   // of the pool: not past 63 bits either

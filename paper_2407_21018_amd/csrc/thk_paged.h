@@ -33,9 +33,9 @@ struct PagedLayout {
   int32_t k_params, v_params;
   int32_t tile_bytes;
 };
-inline PagedLayout paged_layout(int dtype, int bits, int T) {
+constexpr PagedLayout paged_layout(int dtype, int bits, int T) {
   const int e = dtype == THK_BF16 ? 2 : 4;
-  PagedLayout p;
+  PagedLayout p{};
   p.chunks = (T + 7) / 8;
   p.unit_bytes = bits != 0 ? bits : 8 * e;
   p.v_codes = p.chunks * 64 * p.unit_bytes;
@@ -44,6 +44,10 @@ inline PagedLayout paged_layout(int dtype, int bits, int T) {
   p.tile_bytes = p.v_params + (bits != 0 ? kValueGroups * 8 * 2 * e : 0);
   return p;
 }
+constexpr int kMostTileBytes = 65536;   // fp32 elements, all channels
+constexpr int kMostTilesOfPage = 65536 / kTile;
+static_assert(paged_layout(THK_F32, 0, kD).tile_bytes == kMostTileBytes && paged_layout(THK_F32, 8, kD).tile_bytes < kMostTileBytes);
+static_assert((int64_t)kMostTileBytes * kMostTilesOfPage <= INT32_MAX);   // offsets inside a head's part of a page are 32-bit numbers
 
 // An element that is the same for all lanes and that no kernel of the call writes, through the scalar cache: it does not wait
 // for vector loads that are under way.
@@ -101,7 +105,7 @@ struct PagedPool {
     return {l, (int)(lb - l * (uint32_t)B), (int)(u - lb * (uint32_t)N_kv)};
   }
   __device__ __forceinline__ UnitPages unit(const UnitPlace &w) const {
-    const int64_t part = (int64_t)lay.tile_bytes << tpp_shift;   // a KV head's part of a page (at most 1024 tiles of 33 KB)
+    const int64_t part = (int64_t)lay.tile_bytes << tpp_shift;   // a KV head's part of a page (at most 64 MB)
     return {(char *)pool + ((int64_t)w.l * n_pages * N_kv + w.h) * part, part * N_kv, table + (int64_t)w.b * max_pages,
             (uint32_t)n_pages, max_pages, tpp_shift, lay.tile_bytes};
   }

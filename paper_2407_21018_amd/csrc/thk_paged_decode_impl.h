@@ -251,7 +251,8 @@ struct Tiles {
   static constexpr int kPairs = 8 * 2 * Elem<DT>::EB;   // bytes of a group's parameters
   // an instruction waits for the one in front of it in its own sum: so many sums in turn (fewer where the registers are full)
   static constexpr int kInTurn = F::kCodes && NST == 3 && CL * BITS == 16 ? 2 : 4;
-  static constexpr int kPastEnd = 1 << 20;   // (a tile has at most 64 KB)
+  static constexpr int kPastEnd = 1 << 20;
+  static_assert(kPastEnd >= kMostTileBytes);
   u32x4 kc[CL][NST][F::NC], kp[F::kCodes ? NST : 1][NP];
   u32x4 vc[CL][4][F::NC], vp[F::kCodes ? 4 : 1][NP];
 
@@ -541,7 +542,7 @@ constexpr int kRec = kD + 2;     // floats of a split record: max, sum, acc[128]
 constexpr int kAccPitch = kD + 4;
 
 // As many zeros as a tile of codes has bytes at most (128 channels, 8 bits, fp32 parameters).
-static __device__ __align__(16) const char no_parameters[32 * 64 * 8 + 256 * 8] = {};
+static __device__ __align__(16) const char no_parameters[paged_layout(THK_F32, 8, kD).tile_bytes] = {};
 
 
 // The lane's number, asked for anew.

@@ -541,6 +541,31 @@ def test_offsets_past_32_bits():
         assert torch.equal(ko[:, b, :, :n], want[:, b, :, :n])
 
 
+@pytest.mark.parametrize("dtype,bits", [("f32", 0), ("bf16", 4)])
+def test_the_largest_pages(dtype, bits):
+    """Pages of 65536 rows, of the widest tiles among others; a sequence's last tile is the last of its page, and takes the weight."""
+    T = 128
+    c = Cache(dtype, bits, 1, 2, 2, 2, T, [65536 + 70, 65530], 65536, seed=6, spare=0)
+    hot = [65530, 65500]
+    for b, r in enumerate(hot):
+        for h in range(2):
+            c.k[0, b, h, r] = (40 * c.q[0, b, 2 * h].float() / c.q[0, b, 2 * h].float().norm()).to(c.k.dtype)
+    c.write()
+    ko, vo = (torch.empty(1, 2, 2, c.S, D, dtype=TDT[dtype], device="cuda") for _ in range(2))
+    thk.thk_paged_read(c.shape, c.pages, c.pool, c.table, None, c.s_pages, ko, vo, c.S)
+    out = c.decode()
+    torch.cuda.synchronize()
+    for b in range(2):
+        for h in range(2):
+            k, v, kt, vt, idx = c.unit(0, b, h)
+            for got, want in ((_np(ko[0, b, h, :c.rows[b]]), k), (_np(vo[0, b, h, :c.rows[b]]), v)):
+                assert np.all(np.abs(got - want) <= (0 if bits == 0 else HALF_STEP[dtype]) * np.abs(want))
+            q = _np(c.q[0, b, 2 * h:2 * h + 1])
+            z = (q[:, idx] @ k.T / np.sqrt(D))[0]
+            assert np.argmax(z) == hot[b] and z[hot[b]] - np.sort(z)[-2] > 2
+    _check_attention(c, out)
+
+
 @pytest.mark.parametrize("dtype,bits", [("bf16", 4), ("bf16", 0), ("f32", 8)])
 def test_a_ragged_batch_grows(dtype, bits):
     """Prompts stored in whole tiles, their rests in the tails; tokens appended one by one; a full tail goes into pages.
