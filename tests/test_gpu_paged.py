@@ -399,6 +399,50 @@ def test_rows_of_a_tile_past_the_count_do_not_matter(dtype, bits):
                 assert np.abs(_np(out[0, b, h * 4:(h + 1) * 4]) - want).max() <= tol
 
 
+@pytest.mark.parametrize("T", [128, 51])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_elements_of_any_bits_are_read_back(dtype, T):
+    """Every bf16 number there is; fp32 numbers of random bits, NaN of both kinds, infinities and subnormal ones among them."""
+    c = Cache(dtype, 0, 1, 1, 2, 1, T, [512], 128, seed=20)
+    bits = torch.int16 if dtype == "bf16" else torch.int32
+    g = torch.Generator().manual_seed(200)
+    if dtype == "bf16":
+        x = torch.arange(1 << 16).to(torch.int16)
+    else:
+        x = torch.randint(-(1 << 31), 1 << 31, (1 << 16,), generator=g).to(torch.int32)
+        x[::4] |= 0x7f800000                        # infinities and NaN
+        x[1::8] &= -0x7f800001                      # subnormal numbers
+        x[:4] = torch.tensor([0x7f800000, -0x800000, 0x7f800001, -1], dtype=torch.int32)
+    c.k.view(bits)[0, 0] = torch.stack([x.view(512, D), x.flip(0).view(512, D)]).cuda()
+    c.v.view(bits)[0, 0] = torch.stack([x.flip(0).view(512, D), x.view(512, D)]).cuda()
+    c.write()
+    ko, vo = (torch.empty(1, 1, 2, 512, n, dtype=TDT[dtype], device="cuda") for n in (T, D))
+    thk.thk_paged_read(c.shape, c.pages, c.pool, c.table, None, c.s_pages, ko, vo, 512)
+    torch.cuda.synchronize()
+    assert torch.equal(vo.view(bits), c.v.view(bits))
+    assert torch.equal(ko.view(bits), c.k.view(bits).gather(4, c.idx.long()[..., None, :].expand(1, 1, 2, 512, T)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_value_that_is_not_finite_spoils_its_channel_only(dtype):
+    c = Cache(dtype, 0, 1, 3, 2, 3, 51, [300, 64, 20], 64, tails=[0, 9, 64], cap=64, seed=23)
+    c.kt[:, 2], c.vt[:, 2] = c.k[:, 2, :, :64].nan_to_num(0, 0, 0), 1.0   # (finite in all rows)
+    spots = [("v", 0, 0, 299, 5, float("inf")), ("v", 0, 1, 0, 127, float("nan")), ("v", 1, 0, 63, 64, -float("inf")),
+             ("vt", 1, 1, 8, 63, float("inf")), ("vt", 2, 0, 63, 0, float("nan")), ("v", 2, 1, 19, 32, float("inf"))]
+    outs = []
+    for finite in (True, False):
+        for name, b, h, r, ch, x in spots:
+            getattr(c, name)[0, b, h, r, ch] = 0.0 if finite else x
+        c.write()
+        outs.append(c.decode().view(1, 3, 2, 3, D))
+    torch.cuda.synchronize()
+    assert torch.isfinite(outs[0]).all()
+    hit = torch.zeros_like(outs[0], dtype=torch.bool)
+    for _, b, h, _, ch, _ in spots:
+        hit[0, b, h, :, ch] = True
+    assert not torch.isfinite(outs[1][hit]).any() and torch.equal(outs[1][~hit], outs[0][~hit])
+
+
 @pytest.mark.parametrize("T", [1, 33, 64, 72, 97, 128])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_elements_past_the_count_may_be_anything(dtype, T):
