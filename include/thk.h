@@ -406,6 +406,7 @@ thk_status thk_tail_flush(const thk_shape *shape, const int16_t *idx, void *k_pr
  *   table   [B][max_pages]  int32, device: page numbers, 0 .. n_pages - 1
  *   pool    thk_paged_pool_bytes() bytes, device, 16-byte aligned; its content is the library's own
  *           (written by thk_paged_write, read by thk_paged_read and thk_decode_attn_paged)
+ * shape->S is below 2^31 - 64.  What a call writes must not overlap what it reads.
  * Row counts are per sequence, on the DEVICE, int32 [B], so that they can change between replays
  * of a captured graph; the host gives upper bounds.  Counts are clamped to those bounds (and to
  * zero from below), and a table entry outside the pool stands for no page: its rows are not
@@ -467,6 +468,7 @@ thk_status thk_paged_read(const thk_shape *shape, const thk_pages *pages, const 
  *     ->  rows s_tail[b] .. of k_tail, v_tail [L][B][N_kv][s_tail_cap][D]
  * src_row0 may be NULL (zeros), n_new may be NULL (one row each).  Rows that the source does not
  * have or the tail has no room for are left out.  s_tail is not changed: the caller adds n_new.
+ * (Source and tails must not overlap: this does not move rows inside a tail.)
  */
 thk_status thk_tail_append_ragged(const thk_shape *shape, const void *k_new, const void *v_new,
                                   int32_t src_rows, const int32_t *src_row0, const int32_t *n_new,
@@ -474,20 +476,32 @@ thk_status thk_tail_append_ragged(const thk_shape *shape, const void *k_new, con
                                   int32_t s_tail_cap, void *stream);
 
 /*
- * thk_decode_attn over a paged cache: s_pages[b] rows in pages (at most shape->S), s_tail[b] rows in
- * the full-width tail (at most s_tail_cap; s_tail_cap = 0: no tail, and k_tail, v_tail, s_tail are
- * not looked at).  One softmax over both; a sequence without any row gets zeros.  Rows past the
- * counts are not used, whatever they hold: rows of the tail are not read, rows of a tile have
- * weight zero, and elements are taken out.  Of the rows that are used the values must be finite (an infinity or NaN makes its channel
- * NaN or infinite), and keys too, but that a key whose infinities make its logit -inf has weight zero (in all rows: zeros), as
- * the formula has it.  fp32 arithmetic: codes enter the matrix cores as whole numbers, what multiplies them as two (bf16) or
- * three (fp32) bf16 terms.
- * shape->S is below 2^31 - 64.  A unit's rows are cut into pieces that are joined by a second launch: about n_split of
- * them (0: as many as the estimate says), each of whole tiles, the last with the tail.  Short calls cut by shape->S, so that
- * the pieces of a sequence depend on nothing but its own length.  Long calls of several sequences cut by the lengths on the
- * device, a piece of about the same number of tiles for every sequence: there a result may differ in its last bits with the
- * other sequences' lengths.  Either way the order of every sum is fixed by the arguments and the lengths: repeated calls
- * give identical bits.
+ * thk_decode_attn over a paged cache: s_pages[b] rows in pages (at most shape->S), s_tail[b] rows
+ * in the full-width tail (at most s_tail_cap; s_tail_cap = 0: no tail, and k_tail, v_tail, s_tail
+ * are not looked at).  One softmax over both; a sequence without any row gets zeros.  Rows past
+ * the counts are not used, whatever they hold: rows of the tail are not read, rows of a tile have
+ * weight zero, and elements are taken out.  Of the rows that are used the values must be finite
+ * (an infinity or NaN makes its channel NaN or infinite), and keys too, but that a key whose
+ * infinities make its logit -inf has weight zero (where all have: zeros), as the formula has it.
+ * fp32 arithmetic: codes enter the matrix cores as whole numbers, what multiplies them as two
+ * (bf16: 2^-17 of it is left out) or three (fp32: 2^-25) bf16 terms.
+ * A unit's rows are cut into pieces that are joined by a second launch: about n_split of them (0:
+ * as many as the estimate says), each of whole tiles, the last with the tail.  Short calls cut by
+ * shape->S, so that the pieces of a sequence depend on nothing but its own length.  Long calls
+ * (of up to 512 sequences; 8192 tiles or more by shape->S over all units, and of one sequence
+ * pieces of 64 tiles or more) cut by the lengths on the device, a piece of about the same number
+ * of tiles for every sequence: there a result may differ in its last bits with the other
+ * sequences' lengths.  Either way the order of every sum is fixed by the arguments and the
+ * lengths: repeated calls give identical bits.
+ * What the estimate cannot see, and n_split can say (bf16, 8 KV heads of four query heads each):
+ *   - how the lengths differ.  From 512 blocks on (units, times blocks of 16 query heads of a KV
+ *     head) it leaves sequences whole.  64 sequences, one of 131072 rows and 63 of 1000: 512
+ *     us (4 bits; elements 835) with n_split = 0, 58 (107) with 2.  64 of 4096 rows: 41 (119)
+ *     with 0, 52 (126) with 2.
+ *   - how far the lengths stay below shape->S.  One sequence at a bound of 131072 rows, elements:
+ *     1000, 4000, 16384, 65536 and 131072 rows take 18, 32, 33, 39 and 64 us with n_split = 0,
+ *     13, 14, 16, 39 and 70 with 256; at a bound that is the length 8, 8, 13, 35 and 64.  A step
+ *     is best captured once for each range of lengths, with a bound of its own.
  *   ws : thk_workspace_bytes(shape, THK_OP_DECODE_PAGED) bytes, 16-byte aligned: enough for any pages.  Calls that may run at
  *        the same time need one each; calls one after the other, captured ones too, may share it.  Nothing in it outlives
  *        the call.

@@ -749,7 +749,9 @@ int64_t paged_groups(const thk_shape *s) { return ceil_div(s->N_q / s->N_kv, 16)
 // with equal lengths, 300 with ragged ones): the chosen count takes 0.1 % to 2 % (fp32, 4 bits) longer than the best one on
 // average, 1.39x at worst; as many blocks as are resident at once, 9 to 13 %.  With 2 blocks or more for every compute unit
 // sequences stay whole: in 97 of those shapes (bf16) that takes 0.1 % longer than the best count, 1.08x at worst, and two
-// pieces up to 1.6x.
+// pieces up to 1.6x.  The ragged shapes among them fall evenly to a quarter of the longest length.  One long sequence among many short
+// ones is another matter, which only the lengths could tell: 64 x 8 units, one sequence of 131072 rows and 63 of 1000, 4 bits:
+// 512 us whole, 58 with n_split = 2 (thk.h says so to the caller).
 struct PagedTimes { double t0, t1, f, alone, t_step, t_block, t_merge, t_record; };
 constexpr PagedTimes kPagedTimes[2][3] = {   // [fp32, bf16][elements, 4 bits, 8 bits]
     {{0.886, 0.338, 0, 0, 2.007, 6.363, 2.511, 1.874}, {0.195, 0.254, 0.180, 0, 1.378, 6.950, 2.389, 0.030}, {0.307, 0.149, 0.139, 0, 2.027, 7.061, 2.857, 0.317}},
@@ -1404,6 +1406,7 @@ thk_status thk_decode_attn_paged(const thk_shape *s, const thk_pages *p, const v
   a.by_split = Divisor(sp.n);
   a.step = std::min(paged_decode_step(p->bits, a.G, a.T), (int32_t)((sp.rows / kTile + 3) / 4));   // no wave idle while another has two
   a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)s->D));
+  // (the merge of more than 32 pieces has 512 threads for a head, and by the first bound at most 16 * 2^24 / 34 heads: below 2^32)
   if ((uint64_t)paged_blocks(s, sp.n) > kMaxThreads / 256 || (uint64_t)a.units * a.G > kMaxThreads / 256) return THK_ERR_SHAPE;
   return failed(launch_paged_decode(s->dtype, p->bits, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
 }

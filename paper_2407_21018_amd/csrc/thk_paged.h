@@ -124,7 +124,8 @@ struct PagedWriteArgs {
   bool apart;                     // keys and values by blocks of their own
 };
 // Keys and values of a tile by blocks of their own: where these are on the card all at once, eight (bf16) or four (fp32, by their
-// LDS) on a compute unit.  Each then takes half the time.  One block or two, in us: bf16 4 bits, 512 tiles written in 7.7 or 6.9,
+// LDS) on a compute unit.  Each then has half the work.  (One rule for writes and reads: bf16 reads of 1024 tiles lose 6 % by it, writes
+// gain 15 %.)  One block or two, in us: bf16 4 bits, 512 tiles written in 7.7 or 6.9,
 // read in 8.0 or 6.8; 1024: 12.2 or 10.4, 11.4 or 12.1; 2048: 21.6 or 21.1, 18.1 or 19.2; 16384: 108 or 138, 92 or 100.  fp32 8 bits,
 // 384: 10.9 or 8.7, 8.7 or 7.6; 512: 11.3 or 10.2, 9.3 both; 640: 13.4 or 15.3, 11.0 or 12.4; 1024: 16.8 or 18.7, 15.7 or 16.4.
 inline bool paged_apart(int dtype, int64_t tiles) { return tiles <= (dtype == THK_BF16 ? 4 : 2) * kCUs; }

@@ -6,11 +6,14 @@
 // the query takes the scales, once per tile, and the codes enter the matrix cores as the whole numbers they are, which
 // bf16 holds exactly.  Values likewise: sum_r p_r v_rc = sum_r p_r m_r + sum_r (p_r s_r) c_rc.  What is not exact in bf16 --
 // the scaled query and the scaled probabilities -- enters as a sum of bf16 terms: two for bf16 tensors (2^-17 of the value),
-// three for fp32 ones (2^-25).  Of a code c an operand holds something more, which is taken out again with the minimum: 4-bit
-// codes of bf16 tensors are used as 16 + c, whose bits are the code in the mantissa of 16 (one shift and one mask for two of
-// them); those of fp32 tensors as c less half the range, a signed byte, which keeps the two sums that make up a logit small and
-// with them what their rounding costs (8 bits, 2048 rows: 1.5e-6 of the result with plain codes, 2.4e-7 so).  8-bit codes of bf16
-// tensors are plain.
+// three for fp32 ones (2^-25).  Two cost a bf16 output nothing but, now and then, the choice between two neighbours: of 4-bit
+// codes, 640 heads over up to 8192 rows, 1.8 % of the outputs are not the nearest bf16 number but the next one (fp32 arithmetic
+// throughout: 0.05 %), of 8-bit codes 0.7 %, of elements 0.2 to 0.4 %; the error against 64 bits, 1.7e-3, is that of the rounding.
+// Of a code c an operand holds something more, which is taken out again with the minimum: 4-bit codes of bf16 tensors are used
+// as 16 + c, whose bits are the code in the mantissa of 16 (one shift and one mask for two of them); those of fp32 tensors as c
+// less half the range, a signed byte, which keeps the two sums that make up a logit small and with them what their rounding
+// costs (8 bits, 2048 rows: 1.5e-6 of the result with plain codes, 2.4e-7 so).  8-bit codes of bf16 tensors are plain, an
+// instruction less for each word: 1.5e-6 is nothing beside the output's rounding.
 //
 // A wave takes a tile of 64 rows at a time.  S^T = K q^T: A = 16 rows x 32 channels of keys, B = 32 channels x 16 query
 // heads, so lane (m, h) = (lane % 16, lane / 16) ends up with the logits of head m for rows 16 j + 4 h + i.  out^T = V^T P^T:
@@ -27,7 +30,7 @@
 //
 // Measured (kernel alone; a kernel that only reads the bytes reaches 7.1 TB/s): bf16 elements, 8 units of four heads x 131072 rows
 // 62 us, 6.5 TB/s; 4-bit codes, 640 units of one head, up to 8192 rows 79 us, 4.5 TB/s (vector unit busy half of the time, matrix
-// cores a fifth), 256 units of four heads x 32768 rows 146 us, 6.3 TB/s, and up to 216 when such calls follow one another for some
+// cores a fifth), 256 units of four heads x 32768 rows 146 us, 6.3 TB/s, and up to 224 when such calls follow one another for some
 // ms and the card lowers its clock; 8-bit codes, 64 units of eight heads, up to 8191 rows 22 us, 3.5 TB/s: pieces of some 24 tiles,
 // three steps of a wave, whose ramp is as long as they are.
 // 8 units x 1000 rows 5.4 us: launch, three trips to memory one after another (lengths, table, tiles), the states' exchange.
@@ -572,7 +575,8 @@ __device__ __forceinline__ uint32_t wave_sums(uint32_t x) {
 // that, some compute units having a block more); pieces of one sequence of equal size up to a tile; never more than n_split + 1
 // per unit and group on average.  The block's place takes a trip to memory and some 100 to 200 instructions (0.8 us), but the
 // pieces do not depend on how far the host's bound of the lengths is from the lengths, and one long sequence among short ones is
-// cut into as many as it takes.
+// cut into as many as it takes.  That is so where the host plans for two pieces or more (paged_by_lengths): a sequence is not cut
+// in calls of so many units that it plans for one.
 struct Cutting {
   const PagedDecodeArgs &a;
   uint32_t per;   // tiles
