@@ -67,7 +67,8 @@ typedef enum {
   THK_OP_PRUNE = 2,  /* thk_prune                       */
   THK_OP_SCORE_VALUE = 3, /* thk_score_value            */
   THK_OP_PRUNE_VALUE = 4, /* thk_prune_value            */
-  THK_OP_DECODE_PAGED = 5 /* thk_decode_attn_paged      */
+  THK_OP_DECODE_PAGED = 5, /* thk_decode_attn_paged     */
+  THK_OP_PAGED_RESERVE = 6 /* thk_paged_reserve         */
 } thk_op;
 
 /* Problem statement in the paper's B x S x L x N x D terms (Sec. 1). */
@@ -511,6 +512,149 @@ thk_status thk_decode_attn_paged(const thk_shape *shape, const thk_pages *pages,
                                  const int16_t *idx, const void *k_tail, const void *v_tail,
                                  const int32_t *s_tail, int32_t s_tail_cap, void *out, void *ws,
                                  size_t ws_bytes, void *stream);
+
+/*
+ * A serving step around the paged cache: the plan of the step (once for all layers), positions (once per layer), and, for
+ * beam search, the selection and the change of places.  As for the paged calls, what changes from step to step is read
+ * from the DEVICE, so that a captured step can be replayed; int32 arrays need 4-byte alignment only, the token map and the moves 16.
+ *   thk_paged_reserve   pages for every sequence's rows        thk_paged_copy     pages that a sequence has to have for itself
+ *   thk_token_map       where each new token belongs           thk_rope_qkv       queries, keys and values to their places
+ *   thk_beam_select     the best continuations                 thk_beam_reorder   caches follow their beams
+ *
+ * Token map: a record of four int32 per token of a packed batch [n_tokens][4],
+ *   { sequence, position, row, query row }
+ * row: among the rows of the sequence in the buffers that take keys and values (-1: none); query row: among those of the buffer that
+ * takes queries (-1: none).  A record whose sequence is outside [0, B) stands for no token: nothing is written for it.  Callers may
+ * write records of their own (a tree of draft tokens, say).  Two tokens with the same place are a race.
+ *
+ * thk_token_map writes the records of n_new[b] tokens of each sequence, one sequence after the other (NULL: one token each):
+ * token i of sequence b has position pos0[b] + i, row row0[b] + i where that is in [0, cap) (row0 NULL: i), and
+ * query row i - (n_new[b] - q_rows) where that is not negative: the last q_rows tokens, in a window's last places.  Records
+ * behind the last token are { -1, 0, -1, -1 }; tokens past n_tokens are left out.  starts [B + 1] (may be NULL for B <= 4096)
+ * receives the tokens in front of each sequence, at most n_tokens.  Only B of the shape is used.  Positions wrap at 32 bits.
+ */
+thk_status thk_token_map(const thk_shape *shape, const int32_t *n_new, const int32_t *pos0,
+                         const int32_t *row0, int32_t cap, int32_t q_rows, int32_t *map,
+                         int64_t n_tokens, int32_t *starts, void *stream);
+
+/*
+ * Rotary positions.  Of a head's channels the first rot are turned, the others stay.  A pair i < rot / 2 is channels (i, i + rot / 2)
+ * (THK_ROPE_HALVES) or (2 i, 2 i + 1) (THK_ROPE_PAIRS); at position p it becomes
+ *   gain * ( x cos(p w_i) - y sin(p w_i),  y cos(p w_i) + x sin(p w_i) ),     w_i = base^(-2 i / rot) radians or, for long contexts,
+ *   THK_ROPE_LINEAR  w_i / factor
+ *   THK_ROPE_BASE    w_i of the base  base * factor^(rot / (rot - 2))
+ *   THK_ROPE_RAMP    w_i (1 - g_i) + w_i / factor g_i,  g_i = (i - lo) / (hi - lo) in [0, 1] (0.001 for hi = lo), with at(t) the index of the pair that
+ *                    turns t times over `trained` positions, rot ln(trained / (2 pi t)) / (2 ln base): lo = floor(at(high)), at least
+ *                    0, hi = ceil(at(low)), at most rot - 1; the gain is 0.1 ln(factor) + 1 unless given  (arXiv 2309.00071)
+ *   THK_ROPE_BANDS   w_i / factor (1 - g_i) + w_i g_i,  g_i = (r_i - low) / (high - low) in [0, 1], r_i = trained w_i / (2 pi)
+ * thk_rope_turns (host only) writes the rot / 2 speeds, as 2^64ths of a turn per position, to HOST memory; the caller keeps them on
+ * the device.  With them an angle is a product of whole numbers in which full turns fall away: as exact at position 2^31 as at 1.
+ * Sines and cosines are within 2^-23 of the true ones; products are fp32, rounded once.
+ * A negative position turns back, by the same gain: the gradient of the inputs from that of the outputs.
+ */
+typedef enum { THK_ROPE_HALVES = 0, THK_ROPE_PAIRS = 1 } thk_rope_layout;
+typedef enum { THK_ROPE_PLAIN = 0, THK_ROPE_LINEAR = 1, THK_ROPE_BASE = 2, THK_ROPE_RAMP = 3, THK_ROPE_BANDS = 4 } thk_rope_scaling;
+typedef struct {
+  int32_t layout;  /* thk_rope_layout                                                        */
+  int32_t rot;     /* channels turned: even, 2 .. D (BASE: from 4 on)                        */
+  int32_t scaling; /* thk_rope_scaling                                                       */
+  int32_t trained; /* RAMP, BANDS: positions the model was trained on, >= 1                  */
+  double base;     /* > 1                                                                    */
+  double factor;   /* > 0; not used by PLAIN                                                 */
+  double low, high;/* RAMP, BANDS: turns over `trained`, 0 < low < high                      */
+  double gain;     /* 0: 1, or RAMP's own                                                    */
+} thk_rope;
+thk_status thk_rope_turns(const thk_rope *rope, uint64_t *turns);
+
+/*
+ * New tokens' projections to where attention and the caches read them:
+ *   q [L][n_tokens][N_q][D], k, v [L][n_tokens][N_kv][D], ld_* elements from token to token (a row of a joint projection's output)
+ *   q_out  turned queries: [L][B][N_q][q_rows][D] at the map's query rows, or, with q_rows = 0, [L][n_tokens][N_q][D] token by token
+ *   k_out, v_out [L][B][N_kv][cap][D] at the map's rows: keys turned, values as they are
+ * with cap = S_tail_cap and q_rows = 1 a decode step (thk_tail_append_ragged and the query's turn), with cap = S and q_rows = S_obs the
+ * end of a prompt as thk_prune reads it.  Each of the three inputs may be NULL, with its output.  What the map does not name
+ * stays as it was.  ld_* are multiples of 16 bytes (THK_ERR_ALIGN).  Outputs must not overlap inputs, but that q_out may be q with
+ * q_rows = 0 and ld_q = N_q D.  turns [rot / 2] device, 8-byte aligned.  Infinities and NaN stay in their pairs.
+ */
+thk_status thk_rope_qkv(const thk_shape *shape, const thk_rope *rope, const uint64_t *turns,
+                        const void *q, int64_t ld_q, const void *k, int64_t ld_k, const void *v,
+                        int64_t ld_v, const int32_t *map, int64_t n_tokens, void *q_out,
+                        int32_t q_rows, void *k_out, void *v_out, int64_t cap, void *stream);
+
+/*
+ * Pages for sequences that grow, shrink, begin and end, without the host: brings the page table to
+ * what the sequences' rows need.
+ *   rows  [B]   rows that each sequence has to have pages for (0: none, its pages are given back)
+ *   held  [B]   in/out: pages that it holds, the first entries of its row of the table
+ *   table [B][max_pages]  in/out: entries given back become -1
+ *   refs  [n_pages]  in/out: users of each page; a page without any (0 or less) is free.  A caller that shares pages counts them
+ *               here, and pages it keeps for itself.
+ *   room  [B]   out: rows that the sequence now has pages for; less than rows[b] where the pool has run out
+ * Pages past ceil(rows / page_rows) are given back first; then pages are given out, the lowest free numbers first, to sequences in
+ * order, entries in order, as many as there are.  The result depends on the arguments' values alone.
+ * now and moves (both or neither NULL): now [B] is the rows that a sequence has in its pages.  One that is to grow (rows > now > 0)
+ * inside a page that holds some of them and that others use as well gets a page in its place, in front of its other new ones; where
+ * all users of the page are such sequences the first of them keeps it.  moves [B][4] receives { from, to, tiles of 64 rows, 0 },
+ * or { -1, -1, 0, 0 }; thk_paged_copy, next in the stream, does what it says.  Where no page is left for that, room[b] is now[b]:
+ * the sequence must not be written to.  (Shared pages behind the rows in use are not looked for: share pages that hold rows.)
+ * Values outside a bound are clamped to it.  A sequence's entries are pages of the pool (others are given back to nobody) and differ.
+ *   ws : thk_workspace_bytes(shape, THK_OP_PAGED_RESERVE) bytes.
+ */
+thk_status thk_paged_reserve(const thk_shape *shape, const thk_pages *pages, const int32_t *rows,
+                             const int32_t *now, int32_t *held, int32_t *table, int32_t *refs,
+                             int32_t *room, int32_t *moves, void *ws, size_t ws_bytes,
+                             void *stream);
+
+/*
+ * The first moves[i][2] tiles of page moves[i][0] to page moves[i][1], i < n_moves, in every layer and for every KV head; a record with a page
+ * outside the pool is left out.  No page may be written by two records, or written by one and read by another.
+ */
+thk_status thk_paged_copy(const thk_shape *shape, const thk_pages *pages, const int32_t *moves,
+                          int64_t n_moves, void *pool, void *stream);
+
+/*
+ * Beam search: of every prompt's W beams and V continuations of each the K best,
+ *   score = scores[b][w] + (x[v] - max x) - ln sum exp(x - max x),   x = logits[b][w], rows of V, ld elements apart (0: V)
+ * in descending order; equal ones by the lower beam and then the lower token.  (Continuations of one beam are in the order of their
+ * logits, where the sums' 64 bits do not tell them apart.)  -inf in the logits rules a token out.  A beam with a score that is not
+ * finite has no continuations, nor has one whose logits hold +inf or NaN, or nothing but -inf.  done (may be NULL): a beam with done != 0 has ended;
+ * it goes on as it is, with token eos, its logits not looked at.
+ *   parent, token [B][K]  the beam and the token of each; -1 where there are fewer than K
+ *   score_out     [B][K]  (there: -inf); may be scores where K = W
+ *   done_out      [B][K]  1 where the token is eos or the parent has ended (there: 0); may be NULL, and done where K = W
+ * With K = 2 W a caller can set those that end aside and go on with the W best that do not.  Sums are fp32 in eights and 64
+ * bits from there on; scores are 64 bits until they are written.
+ *   ws : thk_beam_workspace_bytes() bytes.  Calls that may run at the same time need one each.
+ */
+typedef struct {
+  int32_t B;     /* prompts                                                   */
+  int32_t W;     /* beams of a prompt, 1 .. 32                                */
+  int32_t K;     /* continuations wanted, 1 .. 64                             */
+  int32_t V;     /* vocabulary, 1 .. 2^24                                     */
+  int64_t ld;    /* elements from row to row of the logits, >= V; 0: V        */
+  int32_t dtype; /* thk_dtype of the logits                                   */
+  int32_t eos;   /* the token that ends a sequence, < V; -1: none, and done is NULL */
+} thk_beams;
+size_t thk_beam_workspace_bytes(const thk_beams *beams);   /* 0 if invalid */
+thk_status thk_beam_select(const thk_beams *beams, const void *logits, const float *scores,
+                           const int32_t *done, int32_t *parent, int32_t *token, float *score_out,
+                           int32_t *done_out, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Sequences that go on from other ones: the shape's B sequences are prompts of W beams side by side, and beam j of prompt p goes on
+ * from beam parent[p][j] (rows of ld_parent entries, of which W are used; one outside [0, W): beam j stays as it is).  In place, for
+ * every beam whose parent is another one:
+ *   k_tail, v_tail [L][B][N_kv][s_tail_cap][D]: the parent's s_tail rows (others stay); s_tail_cap = 0: no tails
+ *   s_tail, s_pages [B]: the parent's counts (each may be NULL where nothing below needs it)
+ *   held, table, refs: the parent's pages that hold rows, ceil(s_pages / page_rows) of them, shared; what the beam held before is
+ *                      given back.  pages = NULL: no pages, and these three are NULL
+ * Pages are shared, so thk_paged_reserve (with now) and thk_paged_copy are called before rows are written to them.  Index lists are a
+ * prompt's, the same for its beams, and stay.
+ */
+thk_status thk_beam_reorder(const thk_shape *shape, const thk_pages *pages, int32_t W,
+                            const int32_t *parent, int32_t ld_parent, void *k_tail, void *v_tail,
+                            int32_t *s_tail, int32_t s_tail_cap, int32_t *s_pages, int32_t *held,
+                            int32_t *table, int32_t *refs, void *stream);
 
 /*
  * Timing hook for benchmarks: the main kernel of the NEXT call made by this host

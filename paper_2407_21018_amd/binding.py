@@ -13,7 +13,9 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libthk.so")
 
 THK_F32, THK_BF16 = 0, 1
-THK_OP_SCORE, THK_OP_DECODE, THK_OP_PRUNE, THK_OP_SCORE_VALUE, THK_OP_PRUNE_VALUE, THK_OP_DECODE_PAGED = 0, 1, 2, 3, 4, 5
+THK_OP_SCORE, THK_OP_DECODE, THK_OP_PRUNE, THK_OP_SCORE_VALUE, THK_OP_PRUNE_VALUE, THK_OP_DECODE_PAGED, THK_OP_PAGED_RESERVE = 0, 1, 2, 3, 4, 5, 6
+THK_ROPE_HALVES, THK_ROPE_PAIRS = 0, 1
+THK_ROPE_PLAIN, THK_ROPE_LINEAR, THK_ROPE_BASE, THK_ROPE_RAMP, THK_ROPE_BANDS = 0, 1, 2, 3, 4
 
 
 class ThkError(RuntimeError):
@@ -33,6 +35,17 @@ class thk_shape(ctypes.Structure):
 class thk_pages(ctypes.Structure):
     _fields_ = [("bits", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32),
                 ("n_pages", ctypes.c_int64)]
+
+
+class thk_rope(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rot", ctypes.c_int32), ("scaling", ctypes.c_int32), ("trained", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("gain", ctypes.c_double)]
+
+
+class thk_beams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("W", ctypes.c_int32), ("K", ctypes.c_int32), ("V", ctypes.c_int32), ("ld", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("eos", ctypes.c_int32)]
 
 
 _lib = None
@@ -117,6 +130,23 @@ def load():
     L.thk_tail_append_ragged.argtypes = [sp, vp, vp, i32, vp, vp, vp, vp, vp, i32, vp]
     L.thk_decode_attn_paged.restype = ctypes.c_int
     L.thk_decode_attn_paged.argtypes = [sp, pp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, ctypes.c_size_t, vp]
+    rp, bp = ctypes.POINTER(thk_rope), ctypes.POINTER(thk_beams)
+    L.thk_token_map.restype = ctypes.c_int
+    L.thk_token_map.argtypes = [sp, vp, vp, vp, i32, i32, vp, i64, vp, vp]
+    L.thk_rope_turns.restype = ctypes.c_int
+    L.thk_rope_turns.argtypes = [rp, ctypes.POINTER(ctypes.c_uint64)]
+    L.thk_rope_qkv.restype = ctypes.c_int
+    L.thk_rope_qkv.argtypes = [sp, rp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i32, vp, vp, i64, vp]
+    L.thk_paged_reserve.restype = ctypes.c_int
+    L.thk_paged_reserve.argtypes = [sp, pp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    L.thk_paged_copy.restype = ctypes.c_int
+    L.thk_paged_copy.argtypes = [sp, pp, vp, i64, vp, vp]
+    L.thk_beam_workspace_bytes.restype = ctypes.c_size_t
+    L.thk_beam_workspace_bytes.argtypes = [bp]
+    L.thk_beam_select.restype = ctypes.c_int
+    L.thk_beam_select.argtypes = [bp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    L.thk_beam_reorder.restype = ctypes.c_int
+    L.thk_beam_reorder.argtypes = [sp, pp, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp]
     L.thk_bench_stream.restype = ctypes.c_int
     L.thk_bench_stream.argtypes = [i32, vp, vp, ctypes.c_int64, i32, vp]
     L.thk_profile_next.restype = None
@@ -449,20 +479,26 @@ def thk_paged_pool_bytes(shape, pages):
 
 class _Tensors:
     """Checks of a call's tensors: on the current device (their kernels run there), of the type the call reads them as,
-    contiguous, large enough.  Integers (raw addresses) and None pass through."""
+    contiguous, large enough.  Integers (raw addresses) and None pass through.  (shape: anything with a dtype.)"""
 
     def __init__(self, shape, where):
         import torch
         self.torch, self.where = torch, where
         self.element = {THK_F32: torch.float32, THK_BF16: torch.bfloat16}.get(shape.dtype)
 
-    def address(self, x, n, name, dtype):
-        if x is None or isinstance(x, int):
-            return x
+    def strided(self, x, name, dtype="element"):
+        """Address of a tensor on the current device and of the type, contiguous or not."""
+        dtype = self.element if dtype == "element" else dtype
         if not x.is_cuda or x.get_device() != self.torch.cuda.current_device():
             raise ValueError(f"{self.where}: {name} must be on the current GPU")
         if dtype is not None and x.dtype != dtype:
             raise ValueError(f"{self.where}: {name} must be {dtype}, is {x.dtype}")
+        return x.data_ptr()
+
+    def address(self, x, n, name, dtype):
+        if x is None or isinstance(x, int):
+            return x
+        self.strided(x, name, dtype)
         return _arg(x, n, name, self.where)
 
     def rows(self, x, n, name):
@@ -542,6 +578,103 @@ def thk_decode_attn_paged(shape, pages, q, pool, table, s_pages, idx, k_tail, v_
                                         t.idx(idx, U * T), t.rows(k_tail, m, "k_tail"), t.rows(v_tail, m, "v_tail"),
                                         t.ints(s_tail, shape.B, "s_tail"), s_tail_cap, t.rows(out, H * D, "out"), *t.workspace(ws),
                                         _stream(stream)), w)
+
+
+# ---- a serving step around the paged cache: positions, plan, beam search ----
+
+def make_rope(layout, rot, scaling=THK_ROPE_PLAIN, trained=0, base=10000.0, factor=1.0, low=0.0, high=0.0, gain=0.0):
+    return thk_rope(layout, rot, scaling, trained, base, factor, low, high, gain)
+
+
+def make_beams(B, W, K, V, ld=0, dtype=THK_BF16, eos=-1):
+    return thk_beams(B, W, K, V, ld, dtype, eos)
+
+
+def thk_rope_turns(rope):
+    """The rot / 2 speeds as 64-bit integers, as an int64 tensor holds them: torch.tensor(...) on the device is thk_rope_qkv's `turns`."""
+    n = max(0, rope.rot // 2)
+    out = (ctypes.c_uint64 * max(1, n))()
+    _check(load().thk_rope_turns(ctypes.byref(rope), out), "thk_rope_turns")
+    return [ctypes.c_int64(x).value for x in out]
+
+
+def _tokens(t, x, ld, n, width, name):
+    """Address of n tokens of `width` elements each, ld elements apart: any view whose last elements are neighbours and whose
+    memory holds them."""
+    if x is None or isinstance(x, int):
+        return x
+    if n > 0:
+        left = x.untyped_storage().nbytes() // x.element_size() - x.storage_offset()
+        if x.numel() == 0 or x.stride(-1) != 1 or left < (n - 1) * ld + width:
+            raise ValueError(f"{t.where}: {name} does not hold {n} tokens of {width} elements, {ld} apart")
+    return t.strided(x, name)
+
+
+def thk_token_map(shape, n_new, pos0, row0, cap, q_rows, map, n_tokens, starts=None, stream=None):
+    w = "thk_token_map"
+    t = _Tensors(shape, w)
+    _check(load().thk_token_map(ctypes.byref(shape), t.ints(n_new, shape.B, "n_new"), t.ints(pos0, shape.B, "pos0"),
+                                t.ints(row0, shape.B, "row0"), cap, q_rows, t.ints(map, n_tokens * 4, "map"), n_tokens,
+                                t.ints(starts, shape.B + 1, "starts"), _stream(stream)), w)
+
+
+def thk_rope_qkv(shape, rope, turns, q, ld_q, k, ld_k, v, ld_v, map, n_tokens, q_out, q_rows, k_out, v_out, cap, stream=None):
+    w = "thk_rope_qkv"
+    t = _Tensors(shape, w)
+    U, H, D, _, _, _, _, _, _ = _dims(shape)
+    n, wide = shape.L * n_tokens, shape.N_kv * D
+    _check(load().thk_rope_qkv(ctypes.byref(shape), ctypes.byref(rope), t.address(turns, rope.rot // 2, "turns", t.torch.int64),
+                               _tokens(t, q, ld_q, n, shape.N_q * D, "q"), ld_q, _tokens(t, k, ld_k, n, wide, "k"), ld_k,
+                               _tokens(t, v, ld_v, n, wide, "v"), ld_v, t.ints(map, n_tokens * 4, "map"), n_tokens,
+                               t.rows(q_out, H * q_rows * D if q_rows else n * shape.N_q * D, "q_out"), q_rows,
+                               t.rows(k_out, U * cap * D, "k_out"), t.rows(v_out, U * cap * D, "v_out"), cap, _stream(stream)), w)
+
+
+def thk_paged_reserve(shape, pages, rows, now, held, table, refs, room, moves, ws, stream=None):
+    w = "thk_paged_reserve"
+    t = _Tensors(shape, w)
+    B = shape.B
+    _check(load().thk_paged_reserve(ctypes.byref(shape), ctypes.byref(pages), t.ints(rows, B, "rows"), t.ints(now, B, "now"),
+                                    t.ints(held, B, "held"), t.ints(table, B * pages.max_pages, "table"),
+                                    t.ints(refs, pages.n_pages, "refs"), t.ints(room, B, "room"), t.ints(moves, 4 * B, "moves"),
+                                    *t.workspace(ws), _stream(stream)), w)
+
+
+def thk_paged_copy(shape, pages, moves, n_moves, pool, stream=None):
+    w = "thk_paged_copy"
+    t = _Tensors(shape, w)
+    _check(load().thk_paged_copy(ctypes.byref(shape), ctypes.byref(pages), t.ints(moves, 4 * n_moves, "moves"), n_moves,
+                                 t.raw(pool, thk_paged_pool_bytes(shape, pages), "pool"), _stream(stream)), w)
+
+
+def thk_beam_workspace_bytes(beams):
+    return int(load().thk_beam_workspace_bytes(ctypes.byref(beams)))
+
+
+def thk_beam_select(beams, logits, scores, done, parent, token, score_out, done_out, ws, stream=None):
+    w = "thk_beam_select"
+    t = _Tensors(beams, w)
+    rows, n = beams.B * beams.W, beams.B * beams.K
+    f32 = t.torch.float32
+    _check(load().thk_beam_select(ctypes.byref(beams), t.rows(logits, (rows - 1) * (beams.ld or beams.V) + beams.V, "logits"),
+                                  t.address(scores, rows, "scores", f32), t.ints(done, rows, "done"), t.ints(parent, n, "parent"),
+                                  t.ints(token, n, "token"), t.address(score_out, n, "score_out", f32), t.ints(done_out, n, "done_out"),
+                                  *t.workspace(ws), _stream(stream)), w)
+
+
+def thk_beam_reorder(shape, pages, W, parent, ld_parent, k_tail, v_tail, s_tail, s_tail_cap, s_pages, held, table, refs, stream=None):
+    w = "thk_beam_reorder"
+    t = _Tensors(shape, w)
+    U, _, D, _, _, _, _, _, _ = _dims(shape)
+    B, m = shape.B, U * s_tail_cap * D
+    if s_tail_cap <= 0:
+        k_tail = v_tail = None
+    entries, n_pages = (B * pages.max_pages, pages.n_pages) if pages is not None else (0, 0)
+    _check(load().thk_beam_reorder(ctypes.byref(shape), None if pages is None else ctypes.byref(pages), W,
+                                   t.ints(parent, (B // max(W, 1) - 1) * ld_parent + W, "parent"), ld_parent, t.rows(k_tail, m, "k_tail"),
+                                   t.rows(v_tail, m, "v_tail"), t.ints(s_tail, B, "s_tail"), s_tail_cap, t.ints(s_pages, B, "s_pages"),
+                                   t.ints(held, B, "held"), t.ints(table, entries, "table"), t.ints(refs, n_pages, "refs"),
+                                   _stream(stream)), w)
 
 
 THK_STREAM_READ, THK_STREAM_COPY, THK_STREAM_WRITE = 0, 1, 2

@@ -11,6 +11,7 @@
 
 #include "thk_internal.h"
 #include "thk_paged.h"
+#include "thk_step.h"
 
 using namespace thk;
 
@@ -800,6 +801,34 @@ size_t paged_ws_bytes(const thk_shape *s, int n_split) {   // a record per block
   return n_split == 1 ? 16 : (size_t)paged_blocks(s, n_split) * std::min(s->N_q / s->N_kv, 16) * (kD + 2) * sizeof(float);
 }
 
+// ---- a serving step around the paged cache ------------------------------------------------
+thk_status check_rope(const thk_rope *r) {
+  if (r == nullptr) return THK_ERR_NULL;
+  if (r->layout != THK_ROPE_HALVES && r->layout != THK_ROPE_PAIRS) return THK_ERR_UNSUPPORTED;
+  if (r->scaling < THK_ROPE_PLAIN || r->scaling > THK_ROPE_BANDS) return THK_ERR_UNSUPPORTED;
+  if (r->rot < 2 || r->rot > kD || r->rot % 2 != 0 || !(r->base > 1) || !isfinite(r->base) || !isfinite(r->gain)) return THK_ERR_SHAPE;
+  if (r->scaling == THK_ROPE_PLAIN) return THK_OK;
+  if (!(r->factor > 0) || !isfinite(r->factor) || (r->scaling == THK_ROPE_BASE && r->rot < 4)) return THK_ERR_SHAPE;
+  if (r->scaling >= THK_ROPE_RAMP && (r->trained < 1 || !(r->low > 0) || !(r->high > r->low) || !isfinite(r->high))) return THK_ERR_SHAPE;
+  return THK_OK;
+}
+double rope_gain(const thk_rope *r) { return r->gain != 0 ? r->gain : r->scaling == THK_ROPE_RAMP ? 0.1 * log(r->factor) + 1 : 1; }
+
+thk_status check_beams(const thk_beams *b) {
+  if (b == nullptr) return THK_ERR_NULL;
+  if (b->B < 1 || b->W < 1 || b->W > kMostBeams || b->K < 1 || b->K > kMostContinuations || b->V < 1 || b->V > 1 << 24) return THK_ERR_SHAPE;
+  if (b->ld != 0 && (b->ld < b->V || b->ld > (int64_t)1 << 40)) return THK_ERR_SHAPE;
+  if (b->eos < -1 || b->eos >= b->V) return THK_ERR_SHAPE;
+  if (b->dtype != THK_F32 && b->dtype != THK_BF16) return THK_ERR_UNSUPPORTED;
+  return THK_OK;
+}
+BeamArgs beam_args(const thk_beams *b) {
+  BeamArgs a{};
+  a.ld = b->ld != 0 ? b->ld : b->V;
+  a.B = b->B; a.W = b->W; a.K = b->K; a.V = b->V; a.eos = b->eos;
+  return a;
+}
+
 size_t score_ws_bytes(const thk_shape *s, int64_t units) {
   return (size_t)units * score_split(s, units).n * kD * sizeof(double);
 }
@@ -897,6 +926,8 @@ size_t thk_workspace_bytes(const thk_shape *s, int32_t op) {
     }
     case THK_OP_DECODE_PAGED:
       return check_paged_shape(s) == THK_OK && s->S <= INT32_MAX - kTile ? paged_ws_bytes(s, paged_most_pieces(s)) : 0;
+    case THK_OP_PAGED_RESERVE:
+      return check_paged_shape(s) == THK_OK ? reserve_ws_bytes(s->B) : 0;
     case THK_OP_SCORE_VALUE:
       if (s->S_obs < 1 || (int64_t)s->S_obs > s->S) return 0;
       return value_ws_bytes(s, value_split(s).n);
@@ -1409,6 +1440,154 @@ thk_status thk_decode_attn_paged(const thk_shape *s, const thk_pages *p, const v
   // (the merge of more than 32 pieces has 512 threads for a head, and by the first bound at most 16 * 2^24 / 34 heads: below 2^32)
   if ((uint64_t)paged_blocks(s, sp.n) > kMaxThreads / 256 || (uint64_t)a.units * a.G > kMaxThreads / 256) return THK_ERR_SHAPE;
   return failed(launch_paged_decode(s->dtype, p->bits, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
+}
+
+// ---- a serving step around the paged cache ------------------------------------------------
+thk_status thk_token_map(const thk_shape *s, const int32_t *n_new, const int32_t *pos0, const int32_t *row0, int32_t cap,
+                         int32_t q_rows, int32_t *map, int64_t n_tokens, int32_t *starts, void *stream) {
+  const thk_status st = check_paged_shape(s);
+  if (st != THK_OK) return st;
+  if (pos0 == nullptr || (map == nullptr && n_tokens != 0) || (starts == nullptr && s->B > kMapSequences)) return THK_ERR_NULL;
+  if (cap < 0 || q_rows < 0 || n_tokens < 0 || n_tokens > INT32_MAX) return THK_ERR_SHAPE;
+  if (!aligned16(map) || !aligned4(n_new) || !aligned4(pos0) || !aligned4(row0) || !aligned4(starts)) return THK_ERR_ALIGN;
+  TokenMapArgs a;
+  a.n_new = n_new; a.pos0 = pos0; a.row0 = row0; a.map = map; a.starts = starts;
+  a.n = n_tokens;
+  a.B = s->B; a.cap = cap; a.q_rows = q_rows;
+  return failed(launch_token_map(a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
+}
+
+thk_status thk_rope_turns(const thk_rope *r, uint64_t *turns) {
+  const thk_status st = check_rope(r);
+  if (st != THK_OK) return st;
+  if (turns == nullptr) return THK_ERR_NULL;
+  // In the 64 bits of the x87 format, so that what is rounded to a 2^64th of a turn is not off by more than that.
+  const long double pi = 3.141592653589793238462643383279502884L, rot = r->rot, f = r->factor;
+  const long double base = r->scaling == THK_ROPE_BASE ? r->base * powl(f, rot / (rot - 2)) : (long double)r->base;
+  for (int i = 0; i < r->rot / 2; ++i) {
+    long double w = powl(base, -2.0L * i / rot);
+    if (r->scaling == THK_ROPE_LINEAR) w /= f;
+    if (r->scaling == THK_ROPE_RAMP) {
+      auto at = [&](long double t) { return rot * logl(r->trained / (2 * pi * t)) / (2 * logl(base)); };
+      const long double lo = std::max(floorl(at(r->high)), 0.0L), hi = std::min(ceill(at(r->low)), rot - 1);
+      const long double g = std::min(std::max((i - lo) / std::max(hi - lo, 0.001L), 0.0L), 1.0L);
+      w = w / f * g + w * (1 - g);
+    }
+    if (r->scaling == THK_ROPE_BANDS) {
+      const long double g = std::min(std::max((r->trained * w / (2 * pi) - r->low) / (r->high - r->low), 0.0L), 1.0L);
+      w = w / f * (1 - g) + w * g;
+    }
+    const long double turn = w / (2 * pi);
+    turns[i] = (uint64_t)((turn - floorl(turn)) * 0x1p64L + 0.5L);   // (less than a turn: below 2^64)
+  }
+  return THK_OK;
+}
+
+thk_status thk_rope_qkv(const thk_shape *s, const thk_rope *r, const uint64_t *turns, const void *q, int64_t ld_q, const void *k,
+                        int64_t ld_k, const void *v, int64_t ld_v, const int32_t *map, int64_t n_tokens, void *q_out,
+                        int32_t q_rows, void *k_out, void *v_out, int64_t cap, void *stream) {
+  thk_status st = check_paged_shape(s);
+  if (st != THK_OK || (st = check_rope(r)) != THK_OK) return st;
+  if (turns == nullptr || (q == nullptr && k == nullptr && v == nullptr) || (q == nullptr) != (q_out == nullptr) ||
+      (k == nullptr) != (k_out == nullptr) || (v == nullptr) != (v_out == nullptr) || (map == nullptr && n_tokens != 0))
+    return THK_ERR_NULL;
+  const bool kv = k != nullptr || v != nullptr;
+  if (n_tokens < 0 || n_tokens > INT32_MAX || q_rows < 0 || (kv && (cap < 1 || cap > INT32_MAX))) return THK_ERR_SHAPE;
+  const int64_t wide_q = (int64_t)s->N_q * kD, wide = (int64_t)s->N_kv * kD, most_ld = (int64_t)1 << 40;
+  if ((q != nullptr && (ld_q < wide_q || ld_q > most_ld)) || (k != nullptr && (ld_k < wide || ld_k > most_ld)) ||
+      (v != nullptr && (ld_v < wide || ld_v > most_ld)))
+    return THK_ERR_SHAPE;
+  const int vec = 16 / elem_bytes(s->dtype);
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(map) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(v_out) ||
+      ((uintptr_t)turns & 7u) != 0 || (q != nullptr && ld_q % vec != 0) || (k != nullptr && ld_k % vec != 0) || (v != nullptr && ld_v % vec != 0))
+    return THK_ERR_ALIGN;
+  RopeArgs a;
+  a.q = q; a.k = k; a.v = v; a.q_out = q_out; a.k_out = k_out; a.v_out = v_out;
+  a.map = map; a.turns = turns;
+  a.n = n_tokens; a.ld_q = ld_q; a.ld_k = ld_k; a.ld_v = ld_v; a.cap = cap;
+  a.L = s->L; a.B = s->B; a.N_q = s->N_q; a.N_kv = s->N_kv; a.q_rows = q_rows; a.rot = r->rot; a.layout = r->layout;
+  const int64_t rows = (q != nullptr ? (int64_t)s->N_q : 0) + ((k != nullptr) + (v != nullptr)) * (int64_t)s->N_kv;
+  int64_t all = 0;
+  if (__builtin_mul_overflow((int64_t)s->L * n_tokens, rows, &all) || all > (int64_t)1 << 27 || rows > 1 << 20) return THK_ERR_SHAPE;
+  a.rows = (int32_t)rows;
+  a.gain = (float)rope_gain(r);
+  if (n_tokens == 0) return THK_OK;
+  return failed(launch_rope(s->dtype, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
+}
+
+thk_status thk_paged_reserve(const thk_shape *s, const thk_pages *p, const int32_t *rows, const int32_t *now, int32_t *held,
+                             int32_t *table, int32_t *refs, int32_t *room, int32_t *moves, void *ws, size_t ws_bytes,
+                             void *stream) {
+  const thk_status st = check_pages(s, p);
+  if (st != THK_OK) return st;
+  if (rows == nullptr || held == nullptr || table == nullptr || refs == nullptr || room == nullptr || (now == nullptr) != (moves == nullptr))
+    return THK_ERR_NULL;
+  if (!aligned4(rows) || !aligned4(now) || !aligned4(held) || !aligned4(table) || !aligned4(refs) || !aligned4(room) || !aligned16(moves))
+    return THK_ERR_ALIGN;
+  if (ws == nullptr || !aligned16(ws) || ws_bytes < reserve_ws_bytes(s->B)) return THK_ERR_WORKSPACE;
+  ReserveArgs a;
+  a.rows = rows; a.now = now; a.held = held; a.table = table; a.refs = refs; a.room = room; a.moves = moves; a.ws = ws;
+  a.n_pages = p->n_pages;
+  a.B = s->B; a.max_pages = p->max_pages; a.page_shift = __builtin_ctz((unsigned)p->page_rows);
+  return failed(launch_reserve(a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
+}
+
+thk_status thk_paged_copy(const thk_shape *s, const thk_pages *p, const int32_t *moves, int64_t n_moves, void *pool, void *stream) {
+  const thk_status st = check_pages(s, p);
+  if (st != THK_OK) return st;
+  if (pool == nullptr || (moves == nullptr && n_moves != 0)) return THK_ERR_NULL;
+  if (n_moves < 0 || n_moves > INT32_MAX) return THK_ERR_SHAPE;
+  if (!aligned16(moves) || !aligned16(pool)) return THK_ERR_ALIGN;
+  PagedCopyArgs a;
+  a.p = paged_pool(s, p, pool, nullptr);
+  a.moves = moves; a.n = n_moves; a.units = (int64_t)s->L * s->N_kv;
+  if (n_moves > (int64_t)(kMaxThreads / 256) / a.units) return THK_ERR_SHAPE;
+  if (n_moves == 0) return THK_OK;
+  return failed(launch_paged_copy(a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
+}
+
+size_t thk_beam_workspace_bytes(const thk_beams *b) {
+  return check_beams(b) == THK_OK ? beam_ws_bytes(b->dtype, beam_args(b)) : 0;
+}
+
+thk_status thk_beam_select(const thk_beams *b, const void *logits, const float *scores, const int32_t *done, int32_t *parent,
+                           int32_t *token, float *score_out, int32_t *done_out, void *ws, size_t ws_bytes, void *stream) {
+  const thk_status st = check_beams(b);
+  if (st != THK_OK) return st;
+  if (logits == nullptr || scores == nullptr || parent == nullptr || token == nullptr || score_out == nullptr) return THK_ERR_NULL;
+  if (done != nullptr && b->eos < 0) return THK_ERR_SHAPE;
+  if (!aligned16(logits) || !aligned4(scores) || !aligned4(done) || !aligned4(parent) || !aligned4(token) || !aligned4(score_out) || !aligned4(done_out))
+    return THK_ERR_ALIGN;
+  BeamArgs a = beam_args(b);
+  const size_t need = beam_ws_bytes(b->dtype, a);
+  if (need == 0) return THK_ERR_SHAPE;
+  if (ws == nullptr || !aligned16(ws) || ws_bytes < need) return THK_ERR_WORKSPACE;
+  a.logits = logits; a.scores = scores; a.done = done; a.parent = parent; a.token = token; a.score_out = score_out; a.done_out = done_out; a.ws = ws;
+  return failed(launch_beam_select(b->dtype, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
+}
+
+thk_status thk_beam_reorder(const thk_shape *s, const thk_pages *p, int32_t W, const int32_t *parent, int32_t ld_parent, void *k_tail,
+                            void *v_tail, int32_t *s_tail, int32_t s_tail_cap, int32_t *s_pages, int32_t *held, int32_t *table,
+                            int32_t *refs, void *stream) {
+  const thk_status st = p != nullptr ? check_pages(s, p) : check_paged_shape(s);
+  if (st != THK_OK) return st;
+  const bool tail = s_tail_cap > 0, paged = p != nullptr;
+  if (parent == nullptr || (tail && (k_tail == nullptr || v_tail == nullptr || s_tail == nullptr)) ||
+      (paged && (s_pages == nullptr || held == nullptr || table == nullptr || refs == nullptr)))
+    return THK_ERR_NULL;
+  if (W < 1 || W > kMostBeams || s->B % W != 0 || ld_parent < W || s_tail_cap < 0) return THK_ERR_SHAPE;
+  if (!paged && (held != nullptr || table != nullptr || refs != nullptr)) return THK_ERR_NULL;
+  if (!aligned4(parent) || !aligned4(s_tail) || !aligned4(s_pages) || !aligned4(held) || !aligned4(table) || !aligned4(refs) ||
+      (tail && (!aligned16(k_tail) || !aligned16(v_tail))))
+    return THK_ERR_ALIGN;
+  ReorderArgs a;
+  a.parent = parent; a.k_tail = k_tail; a.v_tail = v_tail; a.s_tail = s_tail; a.s_pages = s_pages; a.held = held; a.table = table; a.refs = refs;
+  a.prompts = s->B / W; a.n_pages = paged ? p->n_pages : 0;
+  a.L = s->L; a.W = W; a.N_kv = s->N_kv; a.ld_parent = ld_parent; a.cap = s_tail_cap;
+  a.max_pages = paged ? p->max_pages : 0; a.page_shift = paged ? __builtin_ctz((unsigned)p->page_rows) : 0;
+  if (tail && (uint64_t)(units_of(s) / W) > kMaxThreads / 32 / (uint64_t)s_tail_cap - 8) return THK_ERR_SHAPE;   // up to 32 threads a row
+  if ((uint64_t)a.prompts > kMaxThreads / 256) return THK_ERR_SHAPE;
+  return failed(launch_reorder(s->dtype, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
 }
 
 }  // extern "C"
