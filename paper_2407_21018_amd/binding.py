@@ -159,6 +159,8 @@ def load():
         _thk_call.bind(addr(L.thk_decode_attn), addr(L.thk_decode_attn_kv), addr(L.thk_tail_append), addr(L.thk_prune), thk_shape)
         _thk_call.bind_paged(addr(L.thk_decode_attn_paged), addr(L.thk_tail_append_ragged), addr(L.thk_paged_write), addr(L.thk_paged_read),
                              addr(L.thk_paged_pool_bytes), thk_pages)
+        _thk_call.bind_step(addr(L.thk_token_map), addr(L.thk_rope_qkv), addr(L.thk_paged_reserve), addr(L.thk_paged_copy),
+                            addr(L.thk_beam_select), addr(L.thk_beam_reorder), thk_rope, thk_beams)
         _call = _thk_call
     except ImportError as e:
         warnings.warn(f"the native issue of the per-token calls cannot be loaded ({e}): calls go through ctypes, 2 us slower "
@@ -612,6 +614,8 @@ def _tokens(t, x, ld, n, width, name):
 
 def thk_token_map(shape, n_new, pos0, row0, cap, q_rows, map, n_tokens, starts=None, stream=None):
     w = "thk_token_map"
+    if _call is not None and _issued(_call.token_map(shape, n_new, pos0, row0, cap, q_rows, map, n_tokens, starts, stream), w):
+        return
     t = _Tensors(shape, w)
     _check(load().thk_token_map(ctypes.byref(shape), t.ints(n_new, shape.B, "n_new"), t.ints(pos0, shape.B, "pos0"),
                                 t.ints(row0, shape.B, "row0"), cap, q_rows, t.ints(map, n_tokens * 4, "map"), n_tokens,
@@ -620,6 +624,8 @@ def thk_token_map(shape, n_new, pos0, row0, cap, q_rows, map, n_tokens, starts=N
 
 def thk_rope_qkv(shape, rope, turns, q, ld_q, k, ld_k, v, ld_v, map, n_tokens, q_out, q_rows, k_out, v_out, cap, stream=None):
     w = "thk_rope_qkv"
+    if _call is not None and _issued(_call.rope_qkv(shape, rope, turns, q, ld_q, k, ld_k, v, ld_v, map, n_tokens, q_out, q_rows, k_out, v_out, cap, stream), w):
+        return
     t = _Tensors(shape, w)
     U, H, D, _, _, _, _, _, _ = _dims(shape)
     n, wide = shape.L * n_tokens, shape.N_kv * D
@@ -632,6 +638,8 @@ def thk_rope_qkv(shape, rope, turns, q, ld_q, k, ld_k, v, ld_v, map, n_tokens, q
 
 def thk_paged_reserve(shape, pages, rows, now, held, table, refs, room, moves, ws, stream=None):
     w = "thk_paged_reserve"
+    if _call is not None and _issued(_call.paged_reserve(shape, pages, rows, now, held, table, refs, room, moves, ws, stream), w):
+        return
     t = _Tensors(shape, w)
     B = shape.B
     _check(load().thk_paged_reserve(ctypes.byref(shape), ctypes.byref(pages), t.ints(rows, B, "rows"), t.ints(now, B, "now"),
@@ -642,6 +650,8 @@ def thk_paged_reserve(shape, pages, rows, now, held, table, refs, room, moves, w
 
 def thk_paged_copy(shape, pages, moves, n_moves, pool, stream=None):
     w = "thk_paged_copy"
+    if _call is not None and _issued(_call.paged_copy(shape, pages, moves, n_moves, pool, stream), w):
+        return
     t = _Tensors(shape, w)
     _check(load().thk_paged_copy(ctypes.byref(shape), ctypes.byref(pages), t.ints(moves, 4 * n_moves, "moves"), n_moves,
                                  t.raw(pool, thk_paged_pool_bytes(shape, pages), "pool"), _stream(stream)), w)
@@ -653,6 +663,8 @@ def thk_beam_workspace_bytes(beams):
 
 def thk_beam_select(beams, logits, scores, done, parent, token, score_out, done_out, ws, stream=None):
     w = "thk_beam_select"
+    if _call is not None and _issued(_call.beam_select(beams, logits, scores, done, parent, token, score_out, done_out, ws, stream), w):
+        return
     t = _Tensors(beams, w)
     rows, n = beams.B * beams.W, beams.B * beams.K
     f32 = t.torch.float32
@@ -664,6 +676,8 @@ def thk_beam_select(beams, logits, scores, done, parent, token, score_out, done_
 
 def thk_beam_reorder(shape, pages, W, parent, ld_parent, k_tail, v_tail, s_tail, s_tail_cap, s_pages, held, table, refs, stream=None):
     w = "thk_beam_reorder"
+    if _call is not None and _issued(_call.beam_reorder(shape, pages, W, parent, ld_parent, k_tail, v_tail, s_tail, s_tail_cap, s_pages, held, table, refs, stream), w):
+        return
     t = _Tensors(shape, w)
     U, _, D, _, _, _, _, _, _ = _dims(shape)
     B, m = shape.B, U * s_tail_cap * D
