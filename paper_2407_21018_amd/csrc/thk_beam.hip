@@ -11,16 +11,19 @@ namespace {
 typedef unsigned long long u64;
 
 // ---- selection ----------------------------------------------------------------------------
-// A row of logits is cut into pieces, a block each.  A block's waves each go over a part of theirs once, with a running maximum and
-// sum of exp(x - max) per lane and the part's best K elements as a sorted list, one a lane; a second launch joins the pieces of a
-// prompt's rows.  An element is a key: its value in the order of unsigned numbers, above the complement of its index, so that of
-// equal values the first is the larger key; 0 is no element.
+// A row of logits is cut into pieces, a block each, whose waves go over a part of theirs once: a running sum of exp(x - r) per lane, r what the
+// lane's largest element was or not much less, and each lane's largest element of every tile, which waits in LDS.  Then the K-th of the block's lanes'
+// largest says what is certainly not among the K best, and the lanes' tiles that have something above it, little more than K of them, are looked at
+// again, element by element, for the piece's list.  A second launch joins the pieces of a prompt's rows.  An element is a key: its
+// value in the order of unsigned numbers, above the complement of its index, so that of equal values the first is the larger key; 0
+// is no element.
 constexpr int kWaves = 4;
-constexpr int kLoads = 4;   // 16-byte loads of a lane for a tile
+constexpr int kTileElems = 2048;     // of a wave: 32 elements a lane
+constexpr int kMostTiles = 16;       // of a wave
+constexpr int kLooks = 4;
+constexpr float kLeast = -3.402823466e38f;   // the lowest finite value
 
-template <int DT> constexpr int kTileElems = 64 * kLoads * Elem<DT>::VEC;
-
-struct PieceStats { float top; uint32_t bad; double sum; };
+struct PieceStats { float at; uint32_t none; double sum; };   // sum of exp(x - at)
 
 __device__ __forceinline__ u64 key_of(float x, uint32_t at) {
   const uint32_t b = __float_as_uint(x + 0.f);   // -0 is 0
@@ -31,25 +34,67 @@ __device__ __forceinline__ float value_of(u64 key) {
   return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
 
-__device__ __forceinline__ u64 exchange(u64 key, int j, bool larger) {
-  const u64 other = __shfl_xor(key, j);
-  return (key > other) == larger ? key : other;
+// Bitonic sorting of 64 keys, one a lane, in registers: a step takes the key of the lane J away, by moves inside 16 lanes or a
+// swap of 16 or 32, and keeps the larger of the two in the lanes of a mask that is known in advance.  Nine instructions a step; through
+// the LDS crossbar a sort takes 1.3 us, so 0.35.
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xf, 0xf, false); }
+constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kXor3 = 0x1b, kXor7 = 0x141, kXor8 = 0x128, kXor15 = 0x140;
+template <int J>
+__device__ __forceinline__ uint32_t lane_across(uint32_t x) {
+  if constexpr (J == 1) return moved<kXor1>(x);
+  else if constexpr (J == 2) return moved<kXor2>(x);
+  else if constexpr (J == 4) return moved<kXor3>(moved<kXor7>(x));
+  else return moved<kXor8>(x);
 }
-// 64 keys, one a lane, in descending order
-__device__ __forceinline__ u64 sorted(u64 key, int lane) {
-#pragma unroll
-  for (int k = 2; k <= 64; k <<= 1)
-#pragma unroll
-    for (int j = k >> 1; j > 0; j >>= 1) key = exchange(key, j, ((lane & k) == 0) == ((lane & j) == 0));
-  return key;
+struct Pair { u64 a, b; };   // the keys of two lanes: J = 16, 32: the same pair in both, the lower lane's first
+template <int J>
+__device__ __forceinline__ Pair pair_across(u64 key) {
+  const uint32_t lo = (uint32_t)key, hi = (uint32_t)(key >> 32);
+  if constexpr (J == 16) {
+    const auto l = __builtin_amdgcn_permlane16_swap(lo, lo, false, false), h = __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+    return {(u64)h[0] << 32 | l[0], (u64)h[1] << 32 | l[1]};
+  } else if constexpr (J == 32) {
+    const auto l = __builtin_amdgcn_permlane32_swap(lo, lo, false, false), h = __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
+    return {(u64)h[0] << 32 | l[0], (u64)h[1] << 32 | l[1]};
+  } else {
+    return {key, (u64)lane_across<J>(hi) << 32 | lane_across<J>(lo)};
+  }
+}
+// The lanes that keep the larger key in the step of distance j in runs of k lanes.
+constexpr u64 larger_lanes(int k, int j) {
+  u64 m = 0;
+  for (int l = 0; l < 64; ++l)
+    if (((l & k) == 0) == ((l & j) == 0)) m |= 1ull << l;
+  return m;
+}
+template <int K, int J>
+__device__ __forceinline__ u64 run_merged(u64 key) {
+  const Pair p = pair_across<J>(key);
+  key = __builtin_amdgcn_inverse_ballot_w64(__builtin_amdgcn_ballot_w64(p.a > p.b) ^ ~larger_lanes(K, J)) ? p.a : p.b;
+  if constexpr (J > 1) return run_merged<K, J / 2>(key);
+  else return key;
+}
+// in descending order
+__device__ __forceinline__ u64 sorted(u64 key) {
+  key = run_merged<2, 1>(key);
+  key = run_merged<4, 2>(key);
+  key = run_merged<8, 4>(key);
+  key = run_merged<16, 8>(key);
+  key = run_merged<32, 16>(key);
+  return run_merged<64, 32>(key);
 }
 // the largest 64 of two such lists
-__device__ __forceinline__ u64 joined(u64 list, u64 more, int lane) {
-  const u64 reversed = __shfl_xor(more, 63);
-  list = list > reversed ? list : reversed;
-#pragma unroll
-  for (int j = 32; j > 0; j >>= 1) list = exchange(list, j, (lane & j) == 0);
-  return list;
+__device__ __forceinline__ u64 joined(u64 list, u64 more) {
+  const uint32_t lo = moved<kXor15>((uint32_t)more), hi = moved<kXor15>((uint32_t)(more >> 32));
+  const Pair p = pair_across<16>((u64)hi << 32 | lo);
+  more = __builtin_amdgcn_inverse_ballot_w64(0x0000ffff0000ffffull) ? p.b : p.a;
+  const Pair q = pair_across<32>(more);
+  more = __builtin_amdgcn_inverse_ballot_w64(0x00000000ffffffffull) ? q.b : q.a;   // the other list backwards
+  return run_merged<64, 32>(list > more ? list : more);
+}
+__device__ __forceinline__ u64 key_at(u64 key, int lane) {   // (the same lane for all)
+  return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)key, lane);
 }
 
 __device__ __forceinline__ void wave_lds() {
@@ -57,132 +102,235 @@ __device__ __forceinline__ void wave_lds() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Joins (top, sum) of all lanes, in an order that does not depend on the values.
-__device__ __forceinline__ void join_sums(float &top, double &sum) {
-  float t = top;
+// Joins the sums of all lanes, in an order that does not depend on the values.
+template <int J>
+__device__ __forceinline__ void join_step(float &t) { t = fmaxf(t, __uint_as_float(lane_across<J>(__float_as_uint(t)))); }
+template <int J>
+__device__ __forceinline__ void join_step(double &x) {
+  const u64 b = (u64)__double_as_longlong(x);
+  x += __longlong_as_double((long long)((u64)lane_across<J>((uint32_t)(b >> 32)) << 32 | lane_across<J>((uint32_t)b)));
+}
+__device__ __forceinline__ void join_sums(float &at, double &sum) {
+  float t = at;
+  join_step<1>(t);
+  join_step<2>(t);
+  join_step<4>(t);
+  join_step<8>(t);
+  LanePair p = pair16(t);
+  p = pair32(fmaxf(p.a, p.b));
+  t = fmaxf(p.a, p.b);
+  sum = sum != 0 ? sum * exp((double)at - (double)t) : 0.0;
+  join_step<1>(sum);
+  join_step<2>(sum);
+  join_step<4>(sum);
+  join_step<8>(sum);
+  sum = add_across<32>(add_across<16>(sum));
+  at = t;
+}
+
+// A value that at least K of the block's lanes' best are not below, in the order of keys, to its upper 16 bits (all of a bf16's): by bisection,
+// four compares and scalar instructions a bit.  0: fewer than K lanes have a finite one.
+__device__ __forceinline__ uint32_t kth_of_lanes(const float *best, int lane, int K) {
+  uint32_t mine[kWaves];
 #pragma unroll
-  for (int j = 1; j < 64; j <<= 1) t = fmaxf(t, __shfl_xor(t, j));
-  sum = top > -INFINITY ? sum * exp((double)top - (double)t) : 0.0;
+  for (int w = 0; w < kWaves; ++w) {
+    const float x = best[w * 64 + lane];
+    mine[w] = x >= kLeast ? (uint32_t)(key_of(x, 0) >> 32) : 0u;
+  }
+  uint32_t t = 0;
 #pragma unroll
-  for (int j = 1; j < 64; j <<= 1) sum += __shfl_xor(sum, j);
-  top = t;
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t more = t | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) n += __popcll(__builtin_amdgcn_ballot_w64(mine[w] >= more));
+    if (n >= K) t = more;
+  }
+  return t;
+}
+
+// The largest of three, as the instruction itself: the library function first brings operands into canonical form.  (NaN are left out.)
+__device__ __forceinline__ float larger(float a, float b, float c) { float r; asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c)); return r; }
+
+// A lane's 32 elements of a tile are 16-byte chunks 64 apart.  Rows start anywhere (the loads are not aligned).  A chunk that ends behind the
+// row's end is the row's last 16 bytes, of which what the chunk before it has counts as -inf.
+template <int DT>
+struct Tile {
+  using E = Elem<DT>;
+  static constexpr int VEC = E::VEC, CHUNKS = 32 / VEC;
+  u32x4 raw[CHUNKS];
+
+  static __device__ __forceinline__ int begin(int tile, int i, int lane) { return tile * kTileElems + (i * 64 + lane) * VEC; }
+  static __device__ __forceinline__ int shifted(int V, int e) { return min(e, V - VEC); }
+  __device__ __forceinline__ void load(const char *row, int V, int tile, int lane) {
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) __builtin_memcpy(&raw[i], row + (int64_t)shifted(V, begin(tile, i, lane)) * E::EB, 16);
+  }
+  // V < VEC: what the shifted chunk has of the row, whose other elements count as -inf anyway
+  __device__ __forceinline__ void load_short(const char *row, int V) {
+    typename E::Bits b[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) b[j] = ((const typename E::Bits *)row)[max(j - (VEC - V), 0)];
+    __builtin_memcpy(&raw[0], b, 16);
+#pragma unroll
+    for (int i = 1; i < CHUNKS; ++i) raw[i] = raw[0];
+  }
+  __device__ __forceinline__ void values(int V, int tile, int lane, float (&x)[32]) const {
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) E::unpack(raw[i], (float (&)[VEC])x[i * VEC]);
+    if ((tile + 1) * kTileElems > V) {
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i) {
+        const int e = begin(tile, i, lane), lost = e - shifted(V, e);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[i * VEC + j] = j < lost ? -INFINITY : x[i * VEC + j];
+      }
+    }
+  }
+};
+
+// The sum's exponents are relative to a value `at` of the lane, at most 8 below its largest element: sum of 2^(x L - c), L = log2 e in 32 bits
+// and c = at L, one rounding for an element, and what c's rounding leaves is made good when the sum is used.  Where at L has no place in 32
+// bits (values below -1e38, and lanes that have seen nothing but -inf), the difference is taken first.  NaN and +inf make the sum NaN.
+constexpr float kLog2e = 0x1.715476p0f, kFar = -1e38f;
+__device__ __forceinline__ double relative(double sum, float at) {   // ... to the value itself
+  const float c = at * kLog2e;
+  return at < kFar ? sum : sum * (double)__builtin_amdgcn_exp2f(-fmaf(at, kLog2e, -c));
 }
 
 template <int DT>
-__global__ __launch_bounds__(kWaves * 64) void k_beam_pieces(BeamArgs a, int pieces, int tiles_each) {
-  using E = Elem<DT>;
-  constexpr int VEC = E::VEC, ELEMS = kLoads * VEC;
-  __shared__ u64 pending[kWaves][128];
-  __shared__ u64 lists[kWaves][64];
+__global__ __launch_bounds__(kWaves * 64, DT == THK_F32 ? 3 : 4) void k_beam_pieces(BeamArgs a, int pieces, int tiles_each) {
+  using T = Tile<DT>;
+  constexpr int EB = Elem<DT>::EB, VEC = T::VEC;
+  __shared__ float tile_best[kWaves][kMostTiles][64];
+  __shared__ float lane_best[kWaves * 64];
+  __shared__ uint16_t looks[kWaves][kMostTiles * 64];         // lanes' tiles to be looked at again
+  __shared__ u64 waiting[kWaves][128];
+  __shared__ u64 all_keys[kWaves * 128];
   __shared__ PieceStats stats[kWaves];
+  __shared__ int n_keys;
   const int64_t row = blockIdx.x / (unsigned)pieces;
-  const int piece = (int)(blockIdx.x - row * pieces), wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  if ((a.done != nullptr && a.done[row] != 0) || !(fabsf(a.scores[row]) < INFINITY)) return;
-  const char *const x_row = (const char *)a.logits + row * a.ld * E::EB;
-  u64 *const buffer = pending[wave];
+  const int piece = (int)(blockIdx.x - row * pieces), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const char *const x_row = (const char *)a.logits + row * a.ld * EB;
+  const int first = (piece * kWaves + wave) * tiles_each, last = min(first + tiles_each, (a.V + kTileElems - 1) / kTileElems);
+  const int end = a.done != nullptr ? a.done[row] : 0;
+  const float before = a.scores[row];
+  T next;
+  if (a.V < VEC) next.load_short(x_row, a.V);
+  else if (first < last) next.load(x_row, a.V, first, lane);
+  if (end != 0 || !(fabsf(before) < INFINITY)) return;
+  if (threadIdx.x == 0) n_keys = 0;
 
-  float top = -INFINITY;
+  float at = kLeast, c = 0, best = -INFINITY;
   double sum = 0;
-  bool bad = false;
-  u64 list = 0, least = 0;       // least: the list's last of K, or what is known to be below it
-  float least_value = -INFINITY;
-  int n = 0;
-  auto flush = [&](int count) {
-    wave_lds();
-    const u64 more = lane < count ? buffer[lane] : 0, rest = buffer[64 + lane];
-    wave_lds();
-    if (lane < n - count) buffer[lane] = rest;
-    n -= count;
-    list = joined(list, sorted(more, lane), lane);
-    const u64 last = __shfl(list, a.K - 1);
-    if (last > least) {
-      least = last;
-      least_value = value_of(last);
+  for (int tile = first; tile < last; ++tile) {
+    float x[32];
+    const T now = next;
+    if (tile + 1 < last) next.load(x_row, a.V, tile + 1, lane);
+    now.values(a.V, tile, lane, x);
+    float most = larger(x[0], x[1], x[2]);
+#pragma unroll
+    for (int i = 3; i < 31; i += 2) most = larger(most, x[i], x[i + 1]);
+    most = larger(most, x[31], x[31]);
+    best = larger(best, most, most);
+    tile_best[wave][tile - first][lane] = most;
+    if (__ballot(most > at + 8.f) != 0) {
+      const float to = most > at + 8.f ? most : at;
+      if (to > at) sum = relative(sum, at) * exp((double)at - (double)to);
+      at = to;
+      c = at * kLog2e;
     }
-  };
+    if (__ballot(at < kFar) != 0) {
+      const float left = at < kFar ? 0.f : fmaf(at, kLog2e, -c);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] = fmaf(x[i] - at, kLog2e, left);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] = fmaf(x[i], kLog2e, -c);
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float p[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(x[8 * g + j]);
+      sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    }
+  }
+  lane_best[threadIdx.x] = best;
+  sum = relative(sum, at);
+  join_sums(at, sum);
+  if (lane == 0) stats[wave] = {at, 0, sum};
+  __syncthreads();
 
-  const int64_t first = ((int64_t)piece * kWaves + wave) * tiles_each;
-  for (int64_t tile = first; tile < first + tiles_each; ++tile) {
-    const int64_t e0 = tile * kTileElems<DT> + lane * VEC;
-    if (tile * kTileElems<DT> >= a.V) break;
-    float x[ELEMS];
+  // the list
+  u64 *const buffer = waiting[wave];
+  u64 list = 0;
+  const uint32_t kth = kth_of_lanes(lane_best, lane, a.K);
+  u64 least = kth != 0 ? ((u64)kth << 32) - 1 : 0;      // keys up to this are not among the K best, or are in the list
+  const float least_value = kth != 0 ? value_of((u64)kth << 32) : kLeast;
+  int n = 0;                                            // keys that wait for their way into the list
+  auto flush = [&]() {                                  // the last (up to) 64 of them
+    const int from = max(n - 64, 0);
+    wave_lds();
+    const u64 more = from + lane < n ? buffer[from + lane] : 0;
+    wave_lds();
+    n = from;
+    list = joined(list, sorted(more));
+    const u64 last_of_k = key_at(list, a.K - 1);
+    least = last_of_k > least ? last_of_k : least;
+  };
+  int found = 0;
+  for (int t0 = 0; t0 < last - first; t0 += 4) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int64_t e = e0 + i * 64 * VEC;
-      float f[VEC];
-      if (e + VEC <= a.V) {
-        u32x4 r;
-        __builtin_memcpy(&r, x_row + e * E::EB, 16);   // (rows start anywhere)
-        E::unpack(r, f);
-      } else {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) f[j] = e + j < a.V ? E::load1(x_row, e + j) : -INFINITY;
-      }
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) x[i * VEC + j] = f[j];
+    for (int u = 0; u < 4; ++u) {      // (kMostTiles is a multiple of four)
+      const int t = t0 + u;
+      const bool mine = t < last - first && tile_best[wave][t][lane] >= least_value;
+      const u64 who = __ballot(mine);
+      if (mine) looks[wave][found + __popcll(who & ((1ull << lane) - 1))] = (uint16_t)(t << 6 | lane);
+      found += __popcll(who);
     }
-    float most = x[0];
-    bool nan = false;
+  }
+  wave_lds();
+  for (int f0 = 0; f0 < found; f0 += 2 * kLooks) {      // two lanes' elements at a time, one a lane, their loads under way together
+    float y[kLooks];
+    int where[kLooks];
 #pragma unroll
-    for (int i = 0; i < ELEMS; ++i) {
-      most = fmaxf(most, x[i]);
-      nan |= x[i] != x[i];
+    for (int u = 0; u < kLooks; ++u) {
+      const int f = f0 + 2 * u + (lane >> 5), i = lane & 31, look = looks[wave][min(f, found - 1)];
+      const int e = T::begin(first + (look >> 6), i / VEC, look & 63), from = T::shifted(a.V, e), j = i % VEC;
+      where[u] = f < found && j >= e - from ? from + j : -1;
+      y[u] = Elem<DT>::load1(x_row, max(where[u], 0));
     }
-    bad |= nan || most == INFINITY;
-    // the sum
-    if (most > top) {
-      sum *= exp((double)top - (double)most);   // (0 where there was nothing)
-      top = most;
-    }
 #pragma unroll
-    for (int i = 0; i < ELEMS; i += 8) {
-      float part = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        // 2^y, y = d log2 e with what its rounding leaves
-        constexpr float kLog2e = 0x1.715476p0f, kRest = 0x1.4ae0cp-26f;
-        const float d = fmaxf(x[i + j] - top, -200.f);   // (-inf, and -inf - -inf)
-        const float y = d * kLog2e, left = fmaf(d, kRest, fmaf(d, kLog2e, -y)), p = __builtin_amdgcn_exp2f(y);
-        part += fmaf(p, left * 0x1.62e43p-1f, p);
-      }
-      sum += part;
-    }
-    // the list
-    if (tile == first) {   // a start for `least`: at least K elements are not below the K-th best of the lanes' best
-      int at = 0;
-#pragma unroll
-      for (int i = ELEMS - 1; i >= 0; --i) at = x[i] == most ? i : at;
-      const u64 best = most > -INFINITY ? key_of(most, (uint32_t)(e0 + at / VEC * 64 * VEC + at % VEC)) : 0;
-      const u64 kth = __shfl(sorted(best, lane), a.K - 1);
-      if (kth != 0) {
-        least = kth - 1;
-        least_value = value_of(kth);
-      }
-    }
-    if (__ballot(most >= least_value && most > -INFINITY) == 0) continue;
-#pragma unroll
-    for (int i = 0; i < ELEMS; ++i) {
-      if (__ballot(x[i] >= least_value && x[i] > -INFINITY) == 0) continue;
-      const u64 key = key_of(x[i], (uint32_t)(e0 + i / VEC * 64 * VEC + i % VEC));
-      const bool take = x[i] > -INFINITY && key > least;
+    for (int u = 0; u < kLooks; ++u) {
+      const u64 key = key_of(y[u], (uint32_t)where[u]);
+      const bool take = where[u] >= 0 && y[u] >= kLeast && y[u] < INFINITY && key > least;
       const u64 m = __ballot(take);
       if (take) buffer[n + __popcll(m & ((1ull << lane) - 1))] = key;
       n += __popcll(m);
-      if (n >= 64) flush(64);
+      if (n >= 64) flush();
     }
   }
-  if (n > 0) flush(n);
-  lists[wave][lane] = list;
-  join_sums(top, sum);
-  bad = __ballot(bad) != 0;
-  if (lane == 0) stats[wave] = {top, bad, sum};
+  wave_lds();
+#pragma unroll
+  for (int part = 0; part < 2; ++part) {   // the waves' keys together
+    const u64 key = part == 0 ? (lane < n ? buffer[lane] : 0) : (lane < a.K ? list : 0);
+    const u64 m = __ballot(key != 0);
+    if (m == 0) continue;
+    int base = lane == 0 ? atomicAdd(&n_keys, __popcll(m)) : 0;
+    base = __builtin_amdgcn_readfirstlane(base);
+    if (key != 0) all_keys[base + __popcll(m & ((1ull << lane) - 1))] = key;
+  }
   __syncthreads();
+  if (wave == 1) {
+    PieceStats s = lane < kWaves ? stats[lane] : PieceStats{kLeast, 0, 0.0};
+    join_sums(s.at, s.sum);
+    if (lane == 0) ((PieceStats *)a.ws)[blockIdx.x] = s;
+  }
   if (wave != 0) return;
-  for (int w = 1; w < kWaves; ++w) list = joined(list, lists[w][lane], lane);
-  PieceStats s = lane < kWaves ? stats[lane] : PieceStats{-INFINITY, 0, 0.0};
-  join_sums(s.top, s.sum);
-  s.bad = __ballot(s.bad != 0) != 0;
-  if (lane == 0) ((PieceStats *)a.ws)[blockIdx.x] = s;
+  const int total = n_keys;
+  list = sorted(lane < total ? all_keys[lane] : 0);
+  for (int i = 64; i < total; i += 64) list = joined(list, sorted(i + lane < total ? all_keys[i + lane] : 0));
   u64 *const out = (u64 *)((PieceStats *)a.ws + (int64_t)a.B * a.W * pieces) + (int64_t)blockIdx.x * a.K;
   if (lane < a.K) out[lane] = list;
 }
@@ -201,12 +349,16 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
   const int64_t b = blockIdx.x;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const PieceStats *const stats = (const PieceStats *)a.ws;
-  const u64 *const lists = (const u64 *)(stats + (int64_t)a.B * a.W * pieces);
   if (tid == 0) n_live = 0;
+  const int count = pieces * a.K;
   for (int w = wave; w < a.W; w += kJoinWaves) {
     const int64_t row = b * a.W + w;
     const float before = a.scores[row];
     const bool end = a.done != nullptr && a.done[row] != 0;
+    // (asked for before it is known whether they are there)
+    const u64 *const keys = (const u64 *)(stats + (int64_t)a.B * a.W * pieces) + row * count;
+    u64 more = lane < count ? keys[lane] : 0;
+    PieceStats x = lane < pieces ? stats[row * pieces + lane] : PieceStats{kLeast, 0, 0.0};
     double s = -INFINITY;
     int token = 0;
     if (!(fabsf(before) < INFINITY)) {
@@ -214,27 +366,20 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
       if (lane == 0) s = before;
       token = a.eos;
     } else {
-      float top = -INFINITY;
-      double sum = 0;
-      bool bad = false;
-      for (int p = lane; p < pieces; p += 64) {
-        const PieceStats x = stats[row * pieces + p];
-        bad |= x.bad != 0;
-        if (x.top > top) {
-          sum = sum * exp((double)top - (double)x.top) + x.sum;
-          top = x.top;
-        } else if (x.top > -INFINITY) {
-          sum += x.sum * exp((double)x.top - (double)top);
-        }
+      for (int p = lane + 64; p < pieces; p += 64) {
+        const PieceStats y = stats[row * pieces + p];
+        const float to = fmaxf(x.at, y.at);
+        x.sum = (x.sum != 0 ? x.sum * exp((double)x.at - (double)to) : 0) + (y.sum != 0 ? y.sum * exp((double)y.at - (double)to) : 0);
+        x.at = to;
       }
-      join_sums(top, sum);
-      u64 list = lane < a.K ? lists[row * pieces * a.K + lane] : 0;
-      for (int p = 1; p < pieces; ++p) {
-        const u64 more = lane < a.K ? lists[(row * pieces + p) * a.K + lane] : 0;
-        if (__ballot(more > __shfl(list, a.K - 1)) != 0) list = joined(list, more, lane);
+      u64 list = sorted(more);
+      for (int i = 64; i < count; i += 64) {
+        more = i + lane < count ? keys[i + lane] : 0;
+        if (__ballot(more > key_at(list, a.K - 1)) != 0) list = joined(list, sorted(more));
       }
-      if (__ballot(bad) == 0 && list != 0 && lane < a.K) {
-        s = (double)before + (((double)value_of(list) - (double)top) - log(sum));
+      join_sums(x.at, x.sum);
+      if (list != 0 && lane < a.K) {   // (a sum that is NaN leaves no score)
+        s = (double)before + (((double)value_of(list) - (double)x.at) - log(x.sum));
         token = (int)~(uint32_t)list;
         if (!(fabs(s) < INFINITY)) s = -INFINITY;
       }
@@ -262,6 +407,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
     const double s = live_score[i];
     const int mine = live_at[i];
     int rank = 0;
+#pragma unroll 8
     for (int j = 0; j < n; ++j) rank += live_score[j] > s || (live_score[j] == s && live_at[j] < mine);
     if (rank >= a.K) continue;
     const int64_t out = b * a.K + rank;
@@ -372,9 +518,11 @@ hipError_t launch(const void *k, int64_t blocks, int threads, hipStream_t st, A.
 }
 
 struct BeamPlan { int pieces, tiles_each; };
-BeamPlan beam_plan(int dtype, const BeamArgs &a) {
-  const int64_t elems = dtype == THK_F32 ? kTileElems<THK_F32> : kTileElems<THK_BF16>, tiles = (a.V + elems - 1) / elems;
-  const int64_t each = std::min<int64_t>(std::max<int64_t>(1, (int64_t)a.B * a.W * tiles / (16 * kCUs * kWaves)), 16);
+// As many blocks as are on the card at once, four on a compute unit; but two tiles a wave where there are more than one for every wave of a block a
+// compute unit (35 rows of 100003 fp32 logits: 7.7 us, one tile 9.2, four 10.0; 512 rows of 131072 bf16: 56, 39, 35, 32 and 33 us with 1 to 16).
+BeamPlan beam_plan(const BeamArgs &a) {
+  const int64_t tiles = ((int64_t)a.V + kTileElems - 1) / kTileElems, waves = kCUs * kWaves, n = (int64_t)a.B * a.W * tiles;
+  const int64_t each = std::min<int64_t>(std::max<int64_t>(n > waves ? 2 : 1, (n + 4 * waves - 1) / (4 * waves)), kMostTiles);
   return {(int)((tiles + each * kWaves - 1) / (each * kWaves)), (int)each};
 }
 
@@ -383,14 +531,14 @@ const void *tails_kernel(int dtype) { return dtype == THK_F32 ? (const void *)k_
 
 }  // namespace
 
-size_t beam_ws_bytes(int dtype, const BeamArgs &a) {
-  const int64_t pieces = beam_plan(dtype, a).pieces, blocks = (int64_t)a.B * a.W * pieces;
+size_t beam_ws_bytes(const BeamArgs &a) {
+  const int64_t pieces = beam_plan(a).pieces, blocks = (int64_t)a.B * a.W * pieces;
   return blocks * kWaves * 64 > 0xffffffffll ? 0 : (size_t)blocks * (sizeof(PieceStats) + a.K * sizeof(u64));
 }
 
 hipError_t launch_beam_select(int dtype, const BeamArgs &a, hipStream_t st) {
   clear_stale_hip_error();
-  const BeamPlan p = beam_plan(dtype, a);
+  const BeamPlan p = beam_plan(a);
   const hipError_t e = launch(dtype == THK_F32 ? (const void *)k_beam_pieces<THK_F32> : (const void *)k_beam_pieces<THK_BF16>, (int64_t)a.B * a.W * p.pieces,
                               kWaves * 64, st, a, p.pieces, p.tiles_each);
   return e != hipSuccess ? e : launch((const void *)k_beam_join, a.B, kJoinWaves * 64, st, a, p.pieces);
