@@ -1585,7 +1585,7 @@ thk_status thk_beam_reorder(const thk_shape *s, const thk_pages *p, int32_t W, c
   a.prompts = s->B / W; a.n_pages = paged ? p->n_pages : 0;
   a.L = s->L; a.W = W; a.N_kv = s->N_kv; a.ld_parent = ld_parent; a.cap = s_tail_cap;
   a.max_pages = paged ? p->max_pages : 0; a.page_shift = paged ? __builtin_ctz((unsigned)p->page_rows) : 0;
-  if (tail && (uint64_t)(units_of(s) / W) > kMaxThreads / 32 / (uint64_t)s_tail_cap - 8) return THK_ERR_SHAPE;   // up to 32 threads a row
+  if (tail && (uint64_t)(units_of(s) / W) > kMaxThreads / 2 / (32 * ((uint64_t)s_tail_cap + 8))) return THK_ERR_SHAPE;   // up to 32 threads a row of keys or values, whole blocks
   if ((uint64_t)a.prompts > kMaxThreads / 256) return THK_ERR_SHAPE;
   return failed(launch_reorder(s->dtype, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
 }

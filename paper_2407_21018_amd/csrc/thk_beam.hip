@@ -427,86 +427,97 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
 }
 
 // ---- caches that follow -------------------------------------------------------------------
-// A thread has one place of 16 bytes in the tails of all beams of a prompt: it reads the parents' before it writes any, so that
-// beams may go on from each other in place.
+// A thread has one place of 16 bytes in the keys' (or values') tails of all beams of a prompt: it reads the parents' before it writes any, so
+// that beams may go on from each other in place.  (Parents and row counts are the same for a block: they go through the scalar unit.)
 template <int DT, int W>
 __global__ __launch_bounds__(256) void k_reorder_tails(ReorderArgs a, int blocks) {
   constexpr int CPR = kD * Elem<DT>::EB / 16;
-  __shared__ int from[kMostBeams], rows[kMostBeams];
-  const int64_t g = blockIdx.x / (unsigned)blocks;    // (layer, prompt, head)
+  __shared__ int from[kMostBeams], rows[kMostBeams], most;
+  const int64_t g2 = blockIdx.x / (unsigned)blocks, g = g2 >> 1;    // (layer, prompt, head), keys or values
   const int64_t lp = g / a.N_kv, h = g - lp * a.N_kv, p = lp % a.prompts;
   const int tid = threadIdx.x;
+  if (tid == 0) most = 0;
+  if (tid < W) rows[tid] = from[tid] = 0;
+  __syncthreads();
   if (tid < a.W) {
     const int par = a.parent[p * a.ld_parent + tid];
     const bool other = par >= 0 && par < a.W && par != tid;
-    from[tid] = other ? par : -1;
-    rows[tid] = other ? min(a.s_tail[p * a.W + par], a.cap) : 0;
+    const int n = other ? min(a.s_tail[p * a.W + par], a.cap) : 0;
+    from[tid] = other ? par : 0;
+    rows[tid] = n;
+    if (n > 0) atomicMax(&most, n);
   }
   __syncthreads();
-  const int64_t c = (blockIdx.x - g * blocks) * 256 + tid, row = c / CPR;
-  if (row >= a.cap) return;
-  const int64_t stride = (int64_t)a.N_kv * a.cap * CPR, base = (lp * a.W * a.N_kv + h) * a.cap * CPR + c;
+  const int64_t block = blockIdx.x - g2 * blocks;
+  const int64_t c = block * 256 + tid;
+  const int row = (int)(c / CPR);
+  if (row >= most) return;
+  const int64_t stride = (int64_t)a.N_kv * a.cap * CPR;
+  u32x4 *const x = (u32x4 *)(g2 & 1 ? a.v_tail : a.k_tail) + ((lp * a.W * a.N_kv + h) * a.cap * CPR + c);
+  int n[W];
+  int64_t at[W];
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    u32x4 *const x = (u32x4 *)(kv ? a.v_tail : a.k_tail) + base;
-    u32x4 v[W];
-#pragma unroll
-    for (int j = 0; j < W; ++j)
-      if (j < a.W && row < rows[j]) v[j] = x[from[j] * stride];
-#pragma unroll
-    for (int j = 0; j < W; ++j)
-      if (j < a.W && row < rows[j]) x[j * stride] = v[j];
+  for (int j = 0; j < W; ++j) {
+    n[j] = __builtin_amdgcn_readfirstlane(rows[j]);
+    at[j] = (int64_t)__builtin_amdgcn_readfirstlane(from[j]) * stride;
   }
+  u32x4 v[W];
+#pragma unroll
+  for (int j = 0; j < W; ++j) v[j] = x[row < n[j] ? at[j] : at[0]];   // (any of the thread's own places where there is nothing to take)
+#pragma unroll
+  for (int j = 0; j < W; ++j)
+    if (row < n[j]) x[j * stride] = v[j];
 }
 
 // A prompt's table rows and counts, likewise: a thread has one entry of all beams.
+template <int W>
 __global__ __launch_bounds__(256) void k_reorder_pages(ReorderArgs a) {
-  __shared__ int from[kMostBeams], held[kMostBeams], keep[kMostBeams], pages[kMostBeams], tail[kMostBeams];
+  __shared__ int from[W], mine[W], keep[W], old_held[W], old_pages[W], old_tail[W], most;
   const int64_t p = blockIdx.x;
   const int tid = threadIdx.x;
+  if (tid == 0) most = 0;
   if (tid < a.W) {
     const int64_t b = p * a.W + tid;
     const int par = a.parent[p * a.ld_parent + tid];
-    const bool other = par >= 0 && par < a.W && par != tid;
-    from[tid] = other ? par : -1;
-    held[tid] = a.max_pages > 0 ? min(max(a.held[b], 0), a.max_pages) : 0;
-    pages[tid] = a.s_pages != nullptr ? a.s_pages[b] : 0;
-    tail[tid] = a.s_tail != nullptr ? a.s_tail[b] : 0;
+    from[tid] = par >= 0 && par < a.W && par != tid ? par : -1;
+    old_held[tid] = a.max_pages > 0 ? min(max(a.held[b], 0), a.max_pages) : 0;
+    old_pages[tid] = a.s_pages != nullptr ? a.s_pages[b] : 0;
+    old_tail[tid] = a.s_tail != nullptr ? a.s_tail[b] : 0;
   }
   __syncthreads();
   if (tid < a.W) {
     const int64_t b = p * a.W + tid;
     const int f = from[tid];
+    mine[tid] = keep[tid] = 0;     // entries given up, entries taken over
     if (f >= 0) {
-      keep[tid] = (int)min((int64_t)held[f], ((int64_t)max(pages[f], 0) + ((int64_t)1 << a.page_shift) - 1) >> a.page_shift);
+      mine[tid] = old_held[tid];
+      keep[tid] = (int)min((int64_t)old_held[f], ((int64_t)max(old_pages[f], 0) + ((int64_t)1 << a.page_shift) - 1) >> a.page_shift);
+      atomicMax(&most, max(mine[tid], keep[tid]));
       if (a.max_pages > 0) a.held[b] = keep[tid];
-      if (a.s_pages != nullptr) a.s_pages[b] = pages[f];
-      if (a.s_tail != nullptr) a.s_tail[b] = tail[f];
+      if (a.s_pages != nullptr) a.s_pages[b] = old_pages[f];
+      if (a.s_tail != nullptr) a.s_tail[b] = old_tail[f];
     }
   }
   __syncthreads();
-  int most = 0;
-  for (int j = 0; j < a.W; ++j)
-    if (from[j] >= 0) most = max(most, max(held[j], keep[j]));
+  const int last = most;
   int32_t *const table = a.table + p * a.W * a.max_pages;
-  for (int e = tid; e < most; e += 256) {
-    int old[kMostBeams];
+  for (int e = tid; e < last; e += 256) {
+    int old[W], now[W];
 #pragma unroll
-    for (int j = 0; j < kMostBeams; ++j)
-      if (j < a.W) old[j] = table[(int64_t)j * a.max_pages + e];
+    for (int j = 0; j < W; ++j) {
+      if (j >= a.W) break;
+      old[j] = e < mine[j] ? table[(int64_t)j * a.max_pages + e] : -1;
+      now[j] = e < keep[j] ? table[(int64_t)from[j] * a.max_pages + e] : -1;
+    }
 #pragma unroll
-    for (int j = 0; j < kMostBeams; ++j) {
-      if (j >= a.W || from[j] < 0) continue;
-      const int mine = e < held[j] ? old[j] : -1;
-      int now = -1;
-#pragma unroll
-      for (int i = 0; i < kMostBeams; ++i)
-        if (i == from[j] && e < keep[j]) now = old[i];
-      if (now != mine) {
-        if (mine >= 0 && mine < a.n_pages) atomicAdd(a.refs + mine, -1);
-        if (now >= 0 && now < a.n_pages) atomicAdd(a.refs + now, 1);
+    for (int j = 0; j < W; ++j) {
+      if (j >= a.W) break;
+      if (e >= max(mine[j], keep[j])) continue;
+      if (now[j] != old[j]) {
+        if (old[j] >= 0 && old[j] < a.n_pages) atomicAdd(a.refs + old[j], -1);
+        if (now[j] >= 0 && now[j] < a.n_pages) atomicAdd(a.refs + now[j], 1);
       }
-      table[(int64_t)j * a.max_pages + e] = now;
+      table[(int64_t)j * a.max_pages + e] = now[j];
     }
   }
 }
@@ -527,7 +538,15 @@ BeamPlan beam_plan(const BeamArgs &a) {
 }
 
 template <int W>
-const void *tails_kernel(int dtype) { return dtype == THK_F32 ? (const void *)k_reorder_tails<THK_F32, W> : (const void *)k_reorder_tails<THK_BF16, W>; }
+hipError_t reorder(int dtype, const ReorderArgs &a, hipStream_t st) {
+  if (a.cap > 0) {
+    const int blocks = (int)((a.cap * (int64_t)(dtype == THK_F32 ? 32 : 16) + 255) / 256);
+    const hipError_t e = launch(dtype == THK_F32 ? (const void *)k_reorder_tails<THK_F32, W> : (const void *)k_reorder_tails<THK_BF16, W>,
+                                2 * a.L * a.prompts * a.N_kv * blocks, 256, st, a, blocks);
+    if (e != hipSuccess) return e;
+  }
+  return launch((const void *)k_reorder_pages<W>, a.prompts, 256, st, a);
+}
 
 }  // namespace
 
@@ -546,13 +565,7 @@ hipError_t launch_beam_select(int dtype, const BeamArgs &a, hipStream_t st) {
 
 hipError_t launch_reorder(int dtype, const ReorderArgs &a, hipStream_t st) {
   clear_stale_hip_error();
-  if (a.cap > 0) {
-    const int blocks = (int)((a.cap * (int64_t)(dtype == THK_F32 ? 32 : 16) + 255) / 256);
-    const void *k = a.W <= 4 ? tails_kernel<4>(dtype) : a.W <= 8 ? tails_kernel<8>(dtype) : a.W <= 16 ? tails_kernel<16>(dtype) : tails_kernel<32>(dtype);
-    const hipError_t e = launch(k, a.L * a.prompts * a.N_kv * blocks, 256, st, a, blocks);
-    if (e != hipSuccess) return e;
-  }
-  return launch((const void *)k_reorder_pages, a.prompts, 256, st, a);
+  return a.W <= 4 ? reorder<4>(dtype, a, st) : a.W <= 8 ? reorder<8>(dtype, a, st) : a.W <= 16 ? reorder<16>(dtype, a, st) : reorder<32>(dtype, a, st);
 }
 
 }  // namespace thk
