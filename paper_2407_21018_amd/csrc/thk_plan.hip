@@ -7,14 +7,17 @@
 namespace thk {
 namespace {
 
+typedef unsigned long long u64;
+
 // Sum of x over the lanes in front (of a wave), and of all lanes.
-struct WaveSum { int64_t before, all; };
-__device__ __forceinline__ WaveSum wave_sum(int64_t x) {
+template <class I> struct WaveSum { I before, all; };
+template <class I>
+__device__ __forceinline__ WaveSum<I> wave_sum(I x) {
   const int lane = threadIdx.x & 63;
-  int64_t s = x;
+  I s = x;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int64_t y = __shfl_up(s, d);
+    const I y = __shfl_up(s, d);
     if (lane >= d) s += y;
   }
   return {s - x, __shfl(s, 63)};
@@ -31,7 +34,7 @@ __device__ __forceinline__ void running_sums(const TokenMapArgs &a, int64_t *wav
   for (int b0 = 0; b0 < a.B; b0 += THREADS) {
     const int b = b0 + tid;
     const int64_t x = b >= a.B ? 0 : a.n_new == nullptr ? 1 : max(a.n_new[b], 0);
-    const WaveSum w = wave_sum(x);
+    const WaveSum<int64_t> w = wave_sum(x);
     if ((tid & 63) == 63) wave_total[wave] = w.all;
     __syncthreads();
     int64_t before = base + w.before;
@@ -98,7 +101,7 @@ __device__ __forceinline__ void phase_end() {
   __syncthreads();
 }
 
-// A sequence's wishes.  `plan` in memory: what the phases tell each other.
+// A sequence's wishes.  In the workspace: what the phases tell each other.
 struct SequencePlan {
   int have, need;   // pages kept, pages wanted
   int from;         // page that is to be replaced, -1: none
@@ -106,64 +109,400 @@ struct SequencePlan {
 };
 constexpr int kOwner = -(1 << 30);   // + b: marks a page whose users all grow with the first of them
 
-__device__ __forceinline__ SequencePlan wishes(const ReserveArgs &a, int b, int &held, bool &grows) {
-  SequencePlan s;
+__device__ __forceinline__ int held_of(const ReserveArgs &a, int b) { return min(max(a.held[b], 0), a.max_pages); }
+__device__ __forceinline__ int needed(const ReserveArgs &a, int b) {
   const int64_t rows = max(a.rows[b], 0);
-  held = min(max(a.held[b], 0), a.max_pages);
-  s.need = (int)min((rows + ((int64_t)1 << a.page_shift) - 1) >> a.page_shift, (int64_t)a.max_pages);
-  s.have = min(held, s.need);
-  s.from = -1;
-  s.start = 0;
-  grows = false;
-  if (a.now != nullptr) {
-    const int now = a.now[b];
-    const int64_t e = now >> a.page_shift;
-    grows = now > 0 && rows > now && (now & ((1 << a.page_shift) - 1)) != 0 && e < s.have;
-    if (grows) {
-      s.from = a.table[(int64_t)b * a.max_pages + e];
-      grows = s.from >= 0 && s.from < a.n_pages;
-      if (!grows) s.from = -1;
+  return (int)min((rows + ((int64_t)1 << a.page_shift) - 1) >> a.page_shift, (int64_t)a.max_pages);
+}
+// The page that holds some of the rows of a sequence that is to grow, -1: none.  have: pages that it keeps.
+__device__ __forceinline__ int growing_page(const ReserveArgs &a, int b, int have) {
+  const int now = a.now[b], e = now >> a.page_shift;
+  if (now <= 0 || a.rows[b] <= now || (now & ((1 << a.page_shift) - 1)) == 0 || e >= have) return -1;
+  const int p = a.table[(int64_t)b * a.max_pages + e];
+  return p >= 0 && p < a.n_pages ? p : -1;
+}
+// A wave gives back the entries [from, to) of sequence b.
+__device__ __forceinline__ void give_back(const ReserveArgs &a, int b, int from, int to, int lane) {
+  int32_t *const row = a.table + (int64_t)b * a.max_pages;
+  for (int e0 = from; e0 < to; e0 += 256) {
+    int p[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = row[min(e0 + i * 64 + lane, to - 1)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (e0 + i * 64 + lane >= to) break;
+      row[e0 + i * 64 + lane] = -1;
+      if (p[i] >= 0 && p[i] < a.n_pages) refs_add(a.refs, p[i], -1);
     }
   }
-  return s;
+}
+// Wish k, of sequence b whose wishes begin at `start`, gets page p.
+__device__ __forceinline__ void grant(const ReserveArgs &a, int b, int64_t k, int start, int have, int from, int p) {
+  const int nth = (int)(k - start) - (from >= 0);
+  const int e = nth < 0 ? a.now[b] >> a.page_shift : have + nth;
+  a.table[(int64_t)b * a.max_pages + e] = p;
+  refs_set(a.refs, p, 1);
+  if (nth < 0) {
+    const int rows = a.now[b] & ((1 << a.page_shift) - 1);
+    *(i32x4 *)(a.moves + (int64_t)b * 4) = i32x4{from, p, (rows + kTile - 1) / kTile, 0};
+    refs_add(a.refs, from, -1);
+  }
+}
+// ... of `found` free pages: what the sequence has now.
+__device__ __forceinline__ void settle(const ReserveArgs &a, int b, int64_t found, int start, int have, int from, int want) {
+  const bool moved = from >= 0;
+  const int got = (int)min(max(found - start, (int64_t)0), (int64_t)want);
+  const bool stuck = moved && got == 0;
+  const int held = have + got - (moved && !stuck);
+  a.held[b] = held;
+  a.room[b] = stuck ? a.now[b] : held << a.page_shift;
+  if (a.moves != nullptr && (!moved || stuck)) *(i32x4 *)(a.moves + (int64_t)b * 4) = i32x4{-1, -1, 0, 0};
 }
 
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+constexpr int kPlanEach = 4, kPlanSequences = kPlanEach * kPlanThreads;   // sequences of a thread, and of a block, in LDS
 
-// Everything by one block.
-__global__ __launch_bounds__(kPlanThreads) void k_reserve(ReserveArgs a) {
-  constexpr int WAVES = kPlanThreads / 64, EACH = 8;   // EACH: pages a thread looks at in a step
-  __shared__ int64_t wave_total[WAVES];
-  __shared__ int counts[EACH * WAVES];
+// Which of the pages that several use have to be replaced for whom: the growing users of a page meet in a table in LDS.
+struct Meeting {
+  int page[2 * kPlanSequences], count[2 * kPlanSequences];   // as many slots are used as twice the sequences, up to a power of two
+  uint32_t mask;
+  __device__ __forceinline__ void clear(int B, int tid) {
+    const uint32_t m = (2u << (32 - __builtin_clz(max(B - 1, 1)))) - 1;
+    if (tid == 0) mask = m;
+    for (uint32_t i = tid; i <= m; i += kPlanThreads) {
+      page[i] = -1;
+      count[i] = 0;
+    }
+  }
+  __device__ __forceinline__ int enter(int p) {
+    uint32_t at = ((uint32_t)p * 2654435761u) >> 7;
+    for (;; ++at) {   // (fewer pages than slots)
+      const int was = atomicCAS(&page[at & mask], -1, p);
+      if (was == -1 || was == p) break;
+    }
+    atomicAdd(&count[at & mask], 1);
+    return at & mask;
+  }
+};
+template <bool MOVES> struct MeetingOf { Meeting m; };
+template <> struct MeetingOf<false> { };
+
+constexpr int kStep = 8 * kPlanThreads;   // pages that a block looks at in a step
+struct PlanLds {
+  int start[kPlanSequences], have[kPlanSequences], from[kPlanSequences];
+  int64_t wave_total[2][kPlanWaves];
+  int n_ending;
+  union {
+    struct { int ending[kPlanSequences], held[kPlanSequences]; };
+    int pages[kStep];   // free ones, in order
+  };
+};
+
+// The block's sequences: what they give back (ONE), whose growing page is to be replaced, and their wishes in order.  Returns all wishes.
+template <bool ONE, bool MOVES>
+__device__ __forceinline__ int64_t plan_sequences(const ReserveArgs &a, PlanLds &s, MeetingOf<MOVES> &meeting, int (&want)[kPlanEach]) {
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  int need[kPlanEach], have[kPlanEach], from[kPlanEach], held[kPlanEach];
+  if (tid == 0) s.n_ending = 0;
+  if constexpr (MOVES) meeting.m.clear(a.B, tid);
+#pragma unroll
+  for (int i = 0; i < kPlanEach; ++i) {
+    const int b = i * kPlanThreads + tid;
+    need[i] = have[i] = held[i] = 0;
+    from[i] = -1;
+    if (b >= a.B) continue;
+    need[i] = needed(a, b);
+    held[i] = held_of(a, b);
+    have[i] = min(held[i], need[i]);
+    if constexpr (MOVES) from[i] = growing_page(a, b, have[i]);
+  }
+  __syncthreads();
+  if constexpr (ONE) {
+#pragma unroll
+    for (int i = 0; i < kPlanEach; ++i) {
+      const int b = i * kPlanThreads + tid;
+      if (held[i] > need[i]) s.ending[atomicAdd(&s.n_ending, 1)] = b;
+      if (b < a.B) {
+        s.have[b] = have[i];
+        s.held[b] = held[i];
+      }
+    }
+    __syncthreads();
+    for (int i = wave; i < s.n_ending; i += kPlanWaves) give_back(a, s.ending[i], s.have[s.ending[i]], s.held[s.ending[i]], lane);
+    if (s.n_ending > 0) phase_end();
+  }
+  if constexpr (MOVES) {
+    Meeting &m = meeting.m;
+    int slot[kPlanEach], users[kPlanEach];
+#pragma unroll
+    for (int i = 0; i < kPlanEach; ++i) {
+      slot[i] = from[i] >= 0 ? m.enter(from[i]) : -1;
+      users[i] = from[i] >= 0 ? refs_at(a.refs, from[i]) : 0;
+    }
+    __syncthreads();
+    bool all[kPlanEach];   // all users of the page grow: the first of them keeps it
+#pragma unroll
+    for (int i = 0; i < kPlanEach; ++i) all[i] = slot[i] >= 0 && m.count[slot[i]] >= users[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPlanEach; ++i)
+      if (all[i]) m.count[slot[i]] = INT32_MAX;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPlanEach; ++i)
+      if (all[i]) atomicMin(&m.count[slot[i]], i * kPlanThreads + tid);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPlanEach; ++i)
+      if (all[i] && m.count[slot[i]] == i * kPlanThreads + tid) from[i] = -1;
+  }
+  int64_t wanted = 0;
+#pragma unroll
+  for (int i = 0; i < kPlanEach; ++i) {
+    want[i] = (from[i] >= 0) + need[i] - have[i];
+    if (i * kPlanThreads >= a.B) continue;
+    const int b = i * kPlanThreads + tid;
+    const WaveSum<uint32_t> w = wave_sum((uint32_t)want[i]);   // (fewer than 2^25 each)
+    if (lane == 63) s.wave_total[i & 1][wave] = w.all;
+    __syncthreads();
+    int64_t before = wanted + w.before;
+#pragma unroll
+    for (int j = 0; j < kPlanWaves; ++j) {
+      const int64_t x = s.wave_total[i & 1][j];
+      before += j < wave ? x : 0;
+      wanted += x;
+    }
+    if (b < a.B) {
+      s.start[b] = (int)min(before, (int64_t)INT32_MAX);
+      s.have[b] = have[i];
+      s.from[b] = from[i];
+    }
+  }
+  __syncthreads();
+  return wanted;
+}
+
+// The last sequence whose wishes start at or before wish k.
+__device__ __forceinline__ int wisher(const int *start, int B, int64_t k) {
+  int lo = 0, hi = B;
+  while (hi - lo > 1) {
+    const int mid = lo + (hi - lo) / 2;
+    if (start[mid] <= k) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// Everything by one block: latency is all there is to it.
+template <bool MOVES>
+__global__ __launch_bounds__(kPlanThreads) void k_reserve_one(ReserveArgs a) {
+  constexpr int EACH = kStep / kPlanThreads;   // a wave's pages lie side by side
+  __shared__ PlanLds s;
+  __shared__ MeetingOf<MOVES> meeting;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  int want[kPlanEach];
+  const int64_t wanted = plan_sequences<true, MOVES>(a, s, meeting, want);
+  // free pages in order: the one of rank k fulfils wish k
+  int64_t found = 0;
+  int users[EACH];
+  auto look = [&](int64_t p0) {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int64_t p = p0 + (wave * EACH + i) * 64 + lane;
+      users[i] = refs_at(a.refs, min(p, a.n_pages - 1));   // (all loads under way at once)
+    }
+  };
+  if (wanted > 0) look(0);
+  for (int64_t p0 = 0, step = 0; p0 < a.n_pages && found < wanted; p0 += kStep, ++step) {
+    u64 free[EACH];
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      free[i] = __ballot(users[i] <= 0 && p0 + (wave * EACH + i) * 64 + lane < a.n_pages);
+      mine += __popcll(free[i]);
+    }
+    if (lane == 0) s.wave_total[step & 1][wave] = mine;
+    __syncthreads();
+    int k = 0, here = 0;
+#pragma unroll
+    for (int j = 0; j < kPlanWaves; ++j) {
+      const int x = (int)s.wave_total[step & 1][j];
+      k += j < wave ? x : 0;
+      here += x;
+    }
+    if (found + here < wanted) look(p0 + kStep);
+    const int most = (int)min((int64_t)here, wanted - found);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int rank = k + __popcll(free[i] & ((1ull << lane) - 1));
+      k += __popcll(free[i]);
+      if ((free[i] >> lane & 1) != 0 && rank < most) s.pages[rank] = (int)(p0 + (wave * EACH + i) * 64 + lane);
+    }
+    __syncthreads();
+    for (int r = tid; r < most; r += kPlanThreads) {
+      const int b = wisher(s.start, a.B, found + r);
+      grant(a, b, found + r, s.start[b], s.have[b], s.from[b], s.pages[r]);
+    }
+    found += here;
+  }
+#pragma unroll
+  for (int i = 0; i < kPlanEach; ++i) {
+    const int b = i * kPlanThreads + tid;
+    if (b < a.B) settle(a, b, found, s.start[b], s.have[b], s.from[b], want[i]);
+  }
+}
+
+// Pools of more pages than this: four launches.
+constexpr int64_t kOnePages = 65536;
+// What is given back by a wave for each sequence, the sequences' plan by one block, the free pages counted by chunk, and given out.
+constexpr int kChunk = 4096, kChunkThreads = 1024, kChunkWaves = kChunkThreads / 64, kChunkEach = kChunk / kChunkThreads;   // pages that a block looks at together: its part of the pool is as many of them as make
+constexpr int kMostChunks = 1024;   // at most so many parts
+struct ReserveWs {
+  SequencePlan *plan;
+  int64_t *wanted;
+  int32_t *counts;
+};
+__host__ __device__ inline ReserveWs reserve_ws(void *ws, int64_t B) {
+  char *const p = (char *)ws;
+  return {(SequencePlan *)p, (int64_t *)(p + B * sizeof(SequencePlan)), (int32_t *)(p + B * sizeof(SequencePlan) + 16)};
+}
+__global__ __launch_bounds__(256) void k_give_back(ReserveArgs a) {
+  const int64_t b = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (b >= a.B) return;
+  const int need = needed(a, (int)b), held = held_of(a, (int)b);
+  if (held > need) give_back(a, (int)b, need, held, threadIdx.x & 63);
+}
+template <bool MOVES>
+__global__ __launch_bounds__(kPlanThreads) void k_plan_sequences(ReserveArgs a) {
+  __shared__ PlanLds s;
+  __shared__ MeetingOf<MOVES> meeting;
+  int want[kPlanEach];
+  const int64_t wanted = plan_sequences<false, MOVES>(a, s, meeting, want);
+  const ReserveWs w = reserve_ws(a.ws, a.B);
+  if (threadIdx.x == 0) *w.wanted = wanted;
+#pragma unroll
+  for (int i = 0; i < kPlanEach; ++i) {
+    const int b = i * kPlanThreads + threadIdx.x;
+    if (b < a.B) w.plan[b] = {s.have[b], s.have[b] + want[i] - (s.from[b] >= 0), s.from[b], s.start[b]};
+  }
+}
+// A thread's pages of a chunk, in order of waves, 64 pages at a time, lanes.
+__device__ __forceinline__ void chunk_pages(const ReserveArgs &a, int64_t p0, u64 (&free)[kChunkEach]) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  int users[kChunkEach];
+#pragma unroll
+  for (int i = 0; i < kChunkEach; ++i) {
+    const int64_t p = p0 + (wave * kChunkEach + i) * 64 + lane;
+    users[i] = a.refs[min(p, a.n_pages - 1)];   // (all loads under way at once)
+  }
+#pragma unroll
+  for (int i = 0; i < kChunkEach; ++i) free[i] = __ballot(users[i] <= 0 && p0 + (wave * kChunkEach + i) * 64 + lane < a.n_pages);
+}
+__global__ __launch_bounds__(kChunkThreads) void k_count_free(ReserveArgs a, int64_t part) {
+  __shared__ int total;
+  if (threadIdx.x == 0) total = 0;
+  __syncthreads();
+  int n = 0;
+  for (int64_t p0 = blockIdx.x * part; p0 < min((blockIdx.x + 1) * part, a.n_pages); p0 += kChunk) {
+    u64 free[kChunkEach];
+    chunk_pages(a, p0, free);
+#pragma unroll
+    for (int i = 0; i < kChunkEach; ++i) n += __popcll(free[i]);
+  }
+  if ((threadIdx.x & 63) == 0) atomicAdd(&total, n);
+  __syncthreads();
+  if (threadIdx.x == 0) reserve_ws(a.ws, a.B).counts[blockIdx.x] = total;
+}
+__global__ __launch_bounds__(kChunkThreads) void k_give_out(ReserveArgs a, int64_t part) {
+  __shared__ int start[kPlanSequences], have[kPlanSequences];   // have: its highest bit where a page is to be replaced
+  __shared__ int64_t sums[kChunkWaves][2];
+  __shared__ int wave_total[2][kChunkWaves], pages[kChunk];
+  const ReserveWs w = reserve_ws(a.ws, a.B);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  u64 free[kChunkEach];
+  chunk_pages(a, blockIdx.x * part, free);
+  const int64_t wanted = *w.wanted;
+  int64_t before = 0, all = 0;
+  for (int i = tid; i < (int)gridDim.x; i += kChunkThreads) {
+    const int x = w.counts[i];
+    all += x;
+    before += i < (int)blockIdx.x ? x : 0;
+  }
+  before = wave_sum(before).all;
+  all = wave_sum(all).all;
+  if (lane == 0) {
+    sums[wave][0] = before;
+    sums[wave][1] = all;
+  }
+  for (int b = tid; b < a.B; b += kChunkThreads) {
+    const SequencePlan s = w.plan[b];
+    start[b] = s.start;
+    have[b] = s.have | (s.from >= 0 ? INT32_MIN : 0);
+  }
+  __syncthreads();
+  int64_t ahead = 0, found = 0;   // free pages in front of what is looked at, and in all
+#pragma unroll
+  for (int j = 0; j < kChunkWaves; ++j) {
+    ahead += sums[j][0];
+    found += sums[j][1];
+  }
+  for (int64_t b = (int64_t)blockIdx.x * kChunkThreads + tid; b < a.B; b += (int64_t)gridDim.x * kChunkThreads) {
+    const SequencePlan s = w.plan[b];
+    settle(a, (int)b, found, s.start, s.have, s.from, (s.from >= 0) + s.need - s.have);
+  }
+  const int64_t end = min((blockIdx.x + 1) * part, a.n_pages);
+  int step = 0;
+  for (int64_t p0 = blockIdx.x * part; p0 < end && ahead < wanted; p0 += kChunk, step ^= 1) {
+    if (p0 != blockIdx.x * part) chunk_pages(a, p0, free);
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < kChunkEach; ++i) mine += __popcll(free[i]);
+    if (lane == 0) wave_total[step][wave] = mine;
+    __syncthreads();
+    int k = 0, here = 0;
+#pragma unroll
+    for (int j = 0; j < kChunkWaves; ++j) {
+      k += j < wave ? wave_total[step][j] : 0;
+      here += wave_total[step][j];
+    }
+    const int most = (int)min((int64_t)here, wanted - ahead);
+#pragma unroll
+    for (int i = 0; i < kChunkEach; ++i) {
+      const int rank = k + __popcll(free[i] & ((1ull << lane) - 1));
+      k += __popcll(free[i]);
+      if ((free[i] >> lane & 1) != 0 && rank < most) pages[rank] = (int)(p0 + (wave * kChunkEach + i) * 64 + lane);
+    }
+    __syncthreads();
+    for (int r = tid; r < most; r += kChunkThreads) {
+      const int b = wisher(start, a.B, ahead + r), h = have[b];
+      grant(a, b, ahead + r, start[b], h & INT32_MAX, h < 0 ? w.plan[b].from : -1, pages[r]);
+    }
+    ahead += here;
+  }
+}
+
+// More sequences than a block's LDS holds, likewise by one block, their plan in memory.
+__global__ __launch_bounds__(kPlanThreads) void k_reserve_many(ReserveArgs a) {
+  constexpr int EACH = 8;
+  __shared__ int64_t wave_total[kPlanWaves];
   __shared__ int n_ending, ending[kPlanThreads];
   SequencePlan *const plan = (SequencePlan *)a.ws;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  // what sequences give back: by a wave for each that gives something
   for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
     if (tid == 0) n_ending = 0;
     __syncthreads();
     const int b = b0 + tid;
     if (b < a.B) {
-      int held;
-      bool grows;
-      const SequencePlan s = wishes(a, b, held, grows);
-      plan[b] = s;
-      if (held > s.need) ending[atomicAdd(&n_ending, 1)] = b;
-      if (grows) {}
+      const int need = needed(a, b), held = held_of(a, b), have = min(held, need);
+      plan[b] = {have, need, a.now != nullptr ? growing_page(a, b, have) : -1, 0};
+      if (held > need) ending[atomicAdd(&n_ending, 1)] = b;
     }
     phase_end();
-    for (int i = wave; i < n_ending; i += WAVES) {
-      const int g = ending[i], held = min(max(a.held[g], 0), a.max_pages);
-      int32_t *const row = a.table + (int64_t)g * a.max_pages;
-      for (int e = plan[g].need + lane; e < held; e += 64) {
-        const int p = row[e];
-        row[e] = -1;
-        if (p >= 0 && p < a.n_pages) refs_add(a.refs, p, -1);
-      }
-    }
+    for (int i = wave; i < n_ending; i += kPlanWaves) give_back(a, ending[i], plan[ending[i]].need, held_of(a, ending[i]), lane);
     phase_end();
   }
-  // pages that several use and at least one of them is to write
+  // Pages that several use and at least one of them is to write: the growing users take themselves off the page's count, and where
+  // nobody is left the first of them marks it as his.
   if (a.now != nullptr) {
     for (int b = tid; b < a.B; b += kPlanThreads)
       if (plan[b].from >= 0) refs_add(a.refs, plan[b].from, -1);
@@ -171,35 +510,34 @@ __global__ __launch_bounds__(kPlanThreads) void k_reserve(ReserveArgs a) {
     for (int b = tid; b < a.B; b += kPlanThreads)
       if (plan[b].from >= 0 && refs_at(a.refs, plan[b].from) <= 0) __hip_atomic_fetch_min(a.refs + plan[b].from, kOwner + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     phase_end();
-    // (the owner's page gets its number back when all have looked)
-    for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
-      const int b = b0 + tid;
-      const bool owner = b < a.B && plan[b].from >= 0 && refs_at(a.refs, plan[b].from) == kOwner + b;
-      if (owner) plan[b].from = -2 - plan[b].from;
-    }
+    for (int b = tid; b < a.B; b += kPlanThreads)
+      if (plan[b].from >= 0 && refs_at(a.refs, plan[b].from) == kOwner + b) plan[b].from = -2 - plan[b].from;
     phase_end();
     for (int b = tid; b < a.B; b += kPlanThreads)
       if (plan[b].from < -1) {
-        refs_set(a.refs, -2 - plan[b].from, 1);
-        plan[b].from = -1;
+        refs_set(a.refs, -2 - plan[b].from, 0);
+        plan[b].from = -2 - plan[b].from;
+        plan[b].start = 1;
+      }
+    phase_end();
+    for (int b = tid; b < a.B; b += kPlanThreads)   // the counts as they were
+      if (plan[b].from >= 0) {
+        refs_add(a.refs, plan[b].from, 1);
+        if (plan[b].start != 0) plan[b].from = -1;
       }
     phase_end();
   }
-  // wishes in order
   int64_t wanted = 0;
   for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
     const int b = b0 + tid;
     SequencePlan s{};
-    int want = 0;
-    if (b < a.B) {
-      s = plan[b];
-      want = (s.from >= 0) + s.need - s.have;
-    }
-    const WaveSum w = wave_sum(want);
+    s.from = -1;
+    if (b < a.B) s = plan[b];
+    const WaveSum<uint32_t> w = wave_sum((uint32_t)((s.from >= 0) + s.need - s.have));   // (fewer than 2^25 each)
     if (lane == 63) wave_total[wave] = w.all;
     __syncthreads();
     int64_t before = wanted + w.before;
-    for (int i = 0; i < WAVES; ++i) {
+    for (int i = 0; i < kPlanWaves; ++i) {
       if (i < wave) before += wave_total[i];
       wanted += wave_total[i];
     }
@@ -207,64 +545,41 @@ __global__ __launch_bounds__(kPlanThreads) void k_reserve(ReserveArgs a) {
     __syncthreads();
   }
   phase_end();
-  // free pages in order: the one of rank k fulfils wish k
   int64_t found = 0;
   for (int64_t p0 = 0; p0 < a.n_pages && found < wanted; p0 += EACH * kPlanThreads) {
-    bool free[EACH];
-    int before[EACH];
+    u64 free[EACH];
+    int mine = 0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      const int64_t p = p0 + i * kPlanThreads + tid;
-      free[i] = p < a.n_pages && refs_at(a.refs, p) <= 0;
+      const int64_t p = p0 + (wave * EACH + i) * 64 + lane;
+      free[i] = __ballot(refs_at(a.refs, min(p, a.n_pages - 1)) <= 0 && p < a.n_pages);
+      mine += __popcll(free[i]);
     }
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const uint64_t m = __ballot(free[i]);
-      before[i] = __popcll(m & ((1ull << lane) - 1));
-      if (lane == 0) counts[i * WAVES + wave] = __popcll(m);
+    if (lane == 0) wave_total[wave] = mine;
+    __syncthreads();
+    int64_t k = found;
+    for (int j = 0; j < kPlanWaves; ++j) {
+      if (j < wave) k += wave_total[j];
+      found += wave_total[j];
     }
     __syncthreads();
-    int sum = 0, mine[EACH];
-    for (int i = 0; i < EACH * WAVES; ++i) {
-#pragma unroll
-      for (int j = 0; j < EACH; ++j)
-        if (i == j * WAVES + wave) mine[j] = sum;
-      sum += counts[i];
-    }
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      const int64_t k = found + mine[i] + before[i];
-      if (!free[i] || k >= wanted) continue;
-      const int p = (int)(p0 + i * kPlanThreads + tid);
-      int lo = 0, hi = a.B;   // the last sequence that starts at or before wish k
+      const int64_t rank = k + __popcll(free[i] & ((1ull << lane) - 1));
+      k += __popcll(free[i]);
+      if ((free[i] >> lane & 1) == 0 || rank >= wanted) continue;
+      int lo = 0, hi = a.B;
       while (hi - lo > 1) {
         const int mid = lo + (hi - lo) / 2;
-        if (plan[mid].start <= k) lo = mid;
+        if (plan[mid].start <= rank) lo = mid;
         else hi = mid;
       }
-      const SequencePlan s = plan[lo];
-      const int nth = (int)(k - s.start) - (s.from >= 0);
-      const int e = nth < 0 ? a.now[lo] >> a.page_shift : s.have + nth;
-      a.table[(int64_t)lo * a.max_pages + e] = p;
-      refs_set(a.refs, p, 1);
-      if (nth < 0) {
-        const int rows = a.now[lo] & ((1 << a.page_shift) - 1);
-        *(i32x4 *)(a.moves + (int64_t)lo * 4) = i32x4{s.from, p, (rows + kTile - 1) / kTile, 0};
-      }
+      grant(a, lo, rank, plan[lo].start, plan[lo].have, plan[lo].from, (int)(p0 + (wave * EACH + i) * 64 + lane));
     }
-    found += sum;
-    __syncthreads();
   }
   for (int b = tid; b < a.B; b += kPlanThreads) {
     const SequencePlan s = plan[b];
-    const int moved = s.from >= 0, want = moved + s.need - s.have;
-    const int got = (int)min(max(found - s.start, (int64_t)0), (int64_t)want);
-    const bool stuck = moved && got == 0;
-    const int held = s.have + got - (moved && !stuck);
-    a.held[b] = held;
-    a.room[b] = stuck ? a.now[b] : held << a.page_shift;
-    if (stuck) refs_add(a.refs, s.from, 1);
-    if (a.moves != nullptr && (!moved || stuck)) *(i32x4 *)(a.moves + (int64_t)b * 4) = i32x4{-1, -1, 0, 0};
+    settle(a, b, found, s.start, s.have, s.from, (s.from >= 0) + s.need - s.have);
   }
 }
 
@@ -298,10 +613,16 @@ hipError_t launch_token_map(const TokenMapArgs &a, hipStream_t st) {
   return e != hipSuccess || a.n == 0 ? e : launch((const void *)k_token_map_of, blocks, kMapThreads, st, a);
 }
 
-size_t reserve_ws_bytes(int64_t B) { return (size_t)B * sizeof(SequencePlan); }
+size_t reserve_ws_bytes(int64_t B) { return (size_t)B * sizeof(SequencePlan) + 16 + kMostChunks * sizeof(int32_t); }
 hipError_t launch_reserve(const ReserveArgs &a, hipStream_t st) {
   clear_stale_hip_error();
-  return launch((const void *)k_reserve, 1, kPlanThreads, st, a);
+  if (a.B > kPlanSequences) return launch((const void *)k_reserve_many, 1, kPlanThreads, st, a);
+  if (a.n_pages <= kOnePages) return launch(a.now != nullptr ? (const void *)k_reserve_one<true> : (const void *)k_reserve_one<false>, 1, kPlanThreads, st, a);
+  const int64_t chunks = (a.n_pages + kChunk - 1) / kChunk, part = (chunks + kMostChunks - 1) / kMostChunks * kChunk, parts = (a.n_pages + part - 1) / part;
+  hipError_t e = launch((const void *)k_give_back, (a.B + 3) / 4, 256, st, a);
+  if (e == hipSuccess) e = launch(a.now != nullptr ? (const void *)k_plan_sequences<true> : (const void *)k_plan_sequences<false>, 1, kPlanThreads, st, a);
+  if (e == hipSuccess) e = launch((const void *)k_count_free, parts, kChunkThreads, st, a, part);
+  return e == hipSuccess ? launch((const void *)k_give_out, parts, kChunkThreads, st, a, part) : e;
 }
 
 hipError_t launch_paged_copy(const PagedCopyArgs &a, hipStream_t st) {
