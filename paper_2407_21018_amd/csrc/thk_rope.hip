@@ -11,7 +11,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
-constexpr int kTokens = 4;   // most tokens of a block
+constexpr int kTokens = 32;   // most tokens of a block
 
 // Sine and cosine of `pos` times `turn` 2^64ths of a turn.  Whole turns fall out of the product's low 64 bits, of which the upper 32
 // say where on the circle it ends (to 2^-32 of a turn); the nearest quarter turn is taken off, and the rest, within pi / 4 of
@@ -46,87 +46,101 @@ __device__ __forceinline__ u32x4 packed(const float (&f)[Elem<DT>::VEC]) {
 // of the rest, and in the other forms, two neighbours).
 enum { kHalves = 0, kPairs = 1, kHalvesAny = 2 };
 
+// A row that a lane has a part of: where from, where to (nullptr: nowhere), which of the block's tokens, whether it is turned.
+struct Row {
+  const char *src;
+  char *dst;
+  int tok;
+  bool turns;
+};
+
 // A block has `tokens` tokens (of all layers) and `part` rows of each, a row in the hands of CPR / 2 lanes of a wave.  Its sines and
-// cosines are computed once and lie in LDS: a lane takes those of its VEC pairs for every row.
+// cosines are computed once, while the first rows are under way, and lie in LDS: a lane takes those of its VEC pairs for every row.
+// early: rows are asked for before it is known whether they go anywhere, which spares a short call a trip to memory.
 template <int DT, int FORM>
-__global__ __launch_bounds__(kThreads) void k_rope(RopeArgs a, int tokens, int part, int parts) {
+__global__ __launch_bounds__(kThreads) void k_rope(RopeArgs a, int tokens, int part, int parts, int early) {
   using E = Elem<DT>;
   constexpr int VEC = E::VEC, CPR = kD / VEC, LANES = CPR / 2, ROWS = kThreads / LANES;
-  constexpr int LDR = FORM == kHalvesAny ? kD + 1 : 1;
+  constexpr int LDR = kD + 4;
   __shared__ float sn[kTokens * 64], cs[kTokens * 64];
-  __shared__ i32x4 rec[kTokens];
   __shared__ float row_lds[FORM == kHalvesAny ? ROWS * LDR : 1];
   const int tid = threadIdx.x, half = a.rot / 2;
   const int64_t group = blockIdx.x / (unsigned)parts;
   const int r0 = (int)(blockIdx.x - group * parts) * part, rows = min(part, a.rows - r0);
   const int64_t t0 = group * tokens, all = a.L * a.n;
-  const int here = (int)min((int64_t)tokens, all - t0);
-  if (tid < here) rec[tid] = *(const i32x4 *)(a.map + (t0 + tid) % a.n * 4);
-  for (int i = tid; i < here * 64; i += kThreads)
-    if ((i & 63) < half) turned(a.map[(t0 + (i >> 6)) % a.n * 4 + 1], a.turns[i & 63], a.gain, sn[i], cs[i]);
-  __syncthreads();
+  const int here = (int)min((int64_t)tokens, all - t0), items = here * rows;
   const int nq = a.q != nullptr ? a.N_q : 0, nk = a.k != nullptr ? a.N_kv : 0;
   const int p = tid % LANES;
   const bool split = FORM == kHalves && p < half / VEC;
   const int c0 = split ? p : 2 * p, c1 = split ? p + half / VEC : 2 * p + 1;
-  const int items = here * rows;
-  for (int first = 0; first < items; first += ROWS) {
-    const int i = first + tid / LANES, tok = i / rows, r = r0 + i - tok * rows;
-    bool live = i < items;
-    const char *src = nullptr;
-    char *dst = nullptr;
+
+  auto row_of = [&](int first) {
+    const int i = first + tid / LANES;
+    if (i >= items) return Row{nullptr, nullptr, 0, false};
+    const int tok = tokens == 1 ? 0 : i / rows, r = r0 + i - tok * rows;
+    const int64_t t = t0 + tok, l = a.L == 1 ? 0 : t / a.n;
+    const i32x4 rec = *(const i32x4 *)(a.map + (t - l * a.n) * 4);
     const bool is_q = r < nq, turns = r < nq + nk;
-    if (live) {
-      const int64_t t = t0 + tok, l = t / a.n;
-      const int seq = rec[tok][0], h = is_q ? r : turns ? r - nq : r - nq - nk;
-      const int64_t most = is_q ? a.q_rows : a.cap, row = is_q ? rec[tok][3] : rec[tok][2], heads = is_q ? a.N_q : a.N_kv;
-      const bool packed_q = is_q && a.q_rows == 0;
-      live = seq >= 0 && seq < a.B && (packed_q || (row >= 0 && row < most));
-      src = (const char *)(is_q ? a.q : turns ? a.k : a.v) + (t * (is_q ? a.ld_q : turns ? a.ld_k : a.ld_v) + h * kD) * E::EB;
-      dst = (char *)(is_q ? a.q_out : turns ? a.k_out : a.v_out) + (packed_q ? t * heads + h : ((l * a.B + seq) * heads + h) * most + row) * kD * E::EB;
+    const int h = is_q ? r : turns ? r - nq : r - nq - nk, seq = rec[0];
+    const int64_t most = is_q ? a.q_rows : a.cap, row = is_q ? rec[3] : rec[2], heads = is_q ? a.N_q : a.N_kv;
+    const bool packed_q = is_q && a.q_rows == 0, live = seq >= 0 && seq < a.B && (packed_q || (row >= 0 && row < most));
+    char *const dst = (char *)(is_q ? a.q_out : turns ? a.k_out : a.v_out) + (packed_q ? t * heads + h : ((l * a.B + seq) * heads + h) * most + row) * kD * E::EB;
+    return Row{(const char *)(is_q ? a.q : turns ? a.k : a.v) + (t * (is_q ? a.ld_q : turns ? a.ld_k : a.ld_v) + h * kD) * E::EB, live ? dst : nullptr, tok, turns};
+  };
+  auto load = [&](const Row &w, bool any, u32x4 &x0, u32x4 &x1) {
+    if (any ? w.src != nullptr : w.dst != nullptr) {
+      x0 = ld_stream((const u32x4 *)w.src + c0);
+      x1 = ld_stream((const u32x4 *)w.src + c1);
     }
-    u32x4 x0{}, x1{};
-    if (live) {
-      x0 = ((const u32x4 *)src)[c0];
-      x1 = ((const u32x4 *)src)[c1];
+  };
+  Row next = row_of(0);
+  u32x4 n0{}, n1{};
+  load(next, early != 0, n0, n1);
+  for (int i = tid; i < here * 64; i += kThreads)
+    if ((i & 63) < half) turned(a.map[(t0 + (i >> 6)) % a.n * 4 + 1], a.turns[i & 63], a.gain, sn[i], cs[i]);
+  __syncthreads();
+  for (int first = 0; first < items; first += ROWS) {
+    const Row w = next;
+    u32x4 x0 = n0, x1 = n1;
+    if (first + ROWS < items) {
+      next = row_of(first + ROWS);
+      load(next, false, n0, n1);
     }
     if constexpr (FORM == kHalvesAny) {
       float f[2 * VEC];
       E::unpack(x0, (float (&)[VEC])f[0]);
       E::unpack(x1, (float (&)[VEC])f[VEC]);
-      float *const mine = row_lds + tid / LANES * LDR;
-      __syncthreads();   // (what the last rows' lanes read)
+      float *const mine = row_lds + tid / LANES * LDR;   // (a wave's own)
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-      for (int e = 0; e < 2 * VEC; ++e) mine[2 * VEC * p + e] = f[e];
-      __syncthreads();
-      if (live && turns) {
+      for (int e = 0; e < 2 * VEC; e += 4) *(float4 *)(mine + 2 * VEC * p + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      if (w.dst != nullptr && w.turns && 2 * VEC * p < a.rot) {
 #pragma unroll
         for (int e = 0; e < 2 * VEC; ++e) {
           const int c = 2 * VEC * p + e;
-          if (c < a.rot) {
-            const bool lower = c < half;
-            const float s = sn[tok * 64 + (lower ? c : c - half)], k = cs[tok * 64 + (lower ? c : c - half)], y = mine[lower ? c + half : c - half];
-            f[e] = fmaf(f[e], k, lower ? -y * s : y * s);
-          }
+          const bool lower = c < half;
+          const int i = min(lower ? c : c - half, 63);
+          const float s = sn[w.tok * 64 + i], k = cs[w.tok * 64 + i], y = mine[min(lower ? c + half : c - half, kD - 1)];
+          const float turned_e = fmaf(f[e], k, lower ? -y * s : y * s);
+          f[e] = c < a.rot ? turned_e : f[e];
         }
         const u32x4 y0 = packed<DT>((const float (&)[VEC])f[0]), y1 = packed<DT>((const float (&)[VEC])f[VEC]);
         // channels that are not turned keep their bits
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          constexpr int per = VEC / 4;   // channels of a word
-          auto keep = [&](int c, uint32_t was, uint32_t is) {
-            if (c >= a.rot) return was;
-            return per == 2 && c + 1 >= a.rot ? (was & 0xffff0000u) | (is & 0xffffu) : is;
-          };
-          x0[w] = keep(2 * VEC * p + w * per, x0[w], y0[w]);
-          x1[w] = keep(2 * VEC * p + VEC + w * per, x1[w], y1[w]);
+        for (int u = 0; u < 4; ++u) {
+          constexpr int per = VEC / 4;   // channels of a word (rot is even: a word of two has both or neither)
+          x0[u] = 2 * VEC * p + u * per < a.rot ? y0[u] : x0[u];
+          x1[u] = 2 * VEC * p + VEC + u * per < a.rot ? y1[u] : x1[u];
         }
       }
-    } else if (live && turns && p * VEC < half) {
+    } else if (w.dst != nullptr && w.turns && p * VEC < half) {
       float f0[VEC], f1[VEC];
       E::unpack(x0, f0);
       E::unpack(x1, f1);
-      const float *const s = sn + tok * 64 + p * VEC, *const k = cs + tok * 64 + p * VEC;
+      const float *const s = sn + w.tok * 64 + p * VEC, *const k = cs + w.tok * 64 + p * VEC;
       if constexpr (FORM == kHalves) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
@@ -153,16 +167,16 @@ __global__ __launch_bounds__(kThreads) void k_rope(RopeArgs a, int tokens, int p
         if (p * VEC + VEC > half) {   // pairs behind the last one keep their bits
           constexpr int per = VEC / 4;
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            if (2 * VEC * p + w * per >= a.rot) x0[w] = was0[w];
-            if (2 * VEC * p + VEC + w * per >= a.rot) x1[w] = was1[w];
+          for (int u = 0; u < 4; ++u) {
+            if (2 * VEC * p + u * per >= a.rot) x0[u] = was0[u];
+            if (2 * VEC * p + VEC + u * per >= a.rot) x1[u] = was1[u];
           }
         }
       }
     }
-    if (live) {
-      ((u32x4 *)dst)[c0] = x0;
-      ((u32x4 *)dst)[c1] = x1;
+    if (w.dst != nullptr) {
+      st_stream((u32x4 *)w.dst + c0, x0);
+      st_stream((u32x4 *)w.dst + c1, x1);
     }
   }
 }
@@ -175,17 +189,19 @@ const void *kernel_of(const RopeArgs &a) {
 
 }  // namespace
 
-// Large calls: all rows of four tokens a block.  Small ones, which would leave compute units without a block: the rows of one
+// Large calls: all rows of some tokens a block.  Small ones, which would leave compute units without a block: the rows of one
 // pass.
 hipError_t launch_rope(int dtype, const RopeArgs &a, hipStream_t st) {
   clear_stale_hip_error();
   RopeArgs copy = a;
   const int pass = dtype == THK_F32 ? 16 : 32;
-  const bool large = a.L * a.n * a.rows >= (int64_t)pass * 16 * kCUs;
-  int tokens = large ? 4 : 1, part = large ? a.rows : std::min(pass, a.rows), parts = (a.rows + part - 1) / part;
-  void *args[] = {&copy, &tokens, &part, &parts};
+  const int64_t all = a.L * a.n;
+  const bool large = all * a.rows >= (int64_t)pass * 16 * kCUs;
+  int tokens = large ? std::min(std::max(4 * pass / a.rows, 1), kTokens) : 1;
+  int part = large ? a.rows : std::min(pass, a.rows), parts = (a.rows + part - 1) / part, early = all * a.rows <= 4 * pass * kCUs;
+  void *args[] = {&copy, &tokens, &part, &parts, &early};
   return launch_main_kernel(dtype == THK_F32 ? kernel_of<THK_F32>(a) : kernel_of<THK_BF16>(a),
-                            dim3((unsigned)((a.L * a.n + tokens - 1) / tokens * parts)), dim3(kThreads), args, 0, st);
+                            dim3((unsigned)((all + tokens - 1) / tokens * parts)), dim3(kThreads), args, 0, st);
 }
 
 }  // namespace thk
