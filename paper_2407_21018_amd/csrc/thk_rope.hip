@@ -11,7 +11,6 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
-constexpr int kTokens = 32;   // most tokens of a block
 
 // Sine and cosine of `pos` times `turn` 2^64ths of a turn.  Whole turns fall out of the product's low 64 bits, of which the upper 32
 // say where on the circle it ends (to 2^-32 of a turn); the nearest quarter turn is taken off, and the rest, within pi / 4 of
@@ -45,25 +44,22 @@ __device__ __forceinline__ u32x4 packed(const float (&f)[Elem<DT>::VEC]) {
 // The chunks that a lane has of a row: chunks i and i + half / VEC, pair by pair, where the halves of what is turned are whole chunks (and
 // of the rest, and in the other forms, two neighbours).
 enum { kHalves = 0, kPairs = 1, kHalvesAny = 2 };
-
-// A row that a lane has a part of: where from, where to (nullptr: nowhere), which of the block's tokens, whether it is turned.
-struct Row {
-  const char *src;
-  char *dst;
-  int tok;
-  bool turns;
-};
+constexpr int most_tokens(int form) { return form == kHalvesAny ? 8 : 32; }   // of a block: 8 or 16 KB of sines and cosines
 
 // A block has `tokens` tokens (of all layers) and `part` rows of each, a row in the hands of CPR / 2 lanes of a wave.  Its sines and
-// cosines are computed once, while the first rows are under way, and lie in LDS: a lane takes those of its VEC pairs for every row.
-// early: rows are asked for before it is known whether they go anywhere, which spares a short call a trip to memory.
+// cosines are computed once, while the first rows are under way, and lie in LDS: a lane takes those of its VEC pairs for every row.  Rows are
+// asked for a pass ahead, and nothing in the loop waits for memory but they (a wait for a load is one for all stores in front of it too).
+// early: the first rows are asked for before it is known whether they go anywhere, which spares a short call a trip to memory.
+// kHalvesAny has a sine and a cosine for each channel, and the channels' mates change places through LDS.
 template <int DT, int FORM>
-__global__ __launch_bounds__(kThreads) void k_rope(RopeArgs a, int tokens, int part, int parts, int early) {
+__global__ __launch_bounds__(kThreads, 6) void k_rope(RopeArgs a, int tokens, int part, int parts, int early) {
   using E = Elem<DT>;
   constexpr int VEC = E::VEC, CPR = kD / VEC, LANES = CPR / 2, ROWS = kThreads / LANES;
-  constexpr int LDR = kD + 4;
-  __shared__ float sn[kTokens * 64], cs[kTokens * 64];
-  __shared__ float row_lds[FORM == kHalvesAny ? ROWS * LDR : 1];
+  constexpr bool ANY = FORM == kHalvesAny;
+  constexpr int ANGLES = ANY ? kD : 64, LDR = kD + 4;
+  __shared__ __align__(16) float sn[most_tokens(FORM) * ANGLES], cs[most_tokens(FORM) * ANGLES];
+  __shared__ __align__(16) float mates[ANY ? ROWS * LDR : 4];
+  __shared__ i32x4 records[most_tokens(FORM)];
   const int tid = threadIdx.x, half = a.rot / 2;
   const int64_t group = blockIdx.x / (unsigned)parts;
   const int r0 = (int)(blockIdx.x - group * parts) * part, rows = min(part, a.rows - r0);
@@ -74,73 +70,111 @@ __global__ __launch_bounds__(kThreads) void k_rope(RopeArgs a, int tokens, int p
   const bool split = FORM == kHalves && p < half / VEC;
   const int c0 = split ? p : 2 * p, c1 = split ? p + half / VEC : 2 * p + 1;
 
-  auto row_of = [&](int first) {
-    const int i = first + tid / LANES;
-    if (i >= items) return Row{nullptr, nullptr, 0, false};
-    const int tok = tokens == 1 ? 0 : i / rows, r = r0 + i - tok * rows;
-    const int64_t t = t0 + tok, l = a.L == 1 ? 0 : t / a.n;
-    const i32x4 rec = *(const i32x4 *)(a.map + (t - l * a.n) * 4);
-    const bool is_q = r < nq, turns = r < nq + nk;
-    const int h = is_q ? r : turns ? r - nq : r - nq - nk, seq = rec[0];
+  struct Place { int tok, r; };   // token and row of what a lane has in the pass that begins at `first`
+  auto place = [&](int first) {
+    const int i = min(first + tid / LANES, items - 1), tok = tokens == 1 ? 0 : i / rows;
+    return Place{tok, r0 + i - tok * rows};
+  };
+  auto source = [&](const Place &w) {
+    const bool is_q = w.r < nq, turns = w.r < nq + nk;
+    const int h = is_q ? w.r : turns ? w.r - nq : w.r - nq - nk;
+    return (const u32x4 *)((const char *)(is_q ? a.q : turns ? a.k : a.v) + ((t0 + w.tok) * (is_q ? a.ld_q : turns ? a.ld_k : a.ld_v) + h * kD) * E::EB);
+  };
+  auto target = [&](const Place &w, int first) -> u32x4 * {   // nullptr: nowhere
+    const i32x4 rec = records[w.tok];
+    const bool is_q = w.r < nq, turns = w.r < nq + nk;
+    const int h = is_q ? w.r : turns ? w.r - nq : w.r - nq - nk, seq = rec[0];
+    const int64_t t = t0 + w.tok, l = a.L == 1 ? 0 : t / a.n;
     const int64_t most = is_q ? a.q_rows : a.cap, row = is_q ? rec[3] : rec[2], heads = is_q ? a.N_q : a.N_kv;
-    const bool packed_q = is_q && a.q_rows == 0, live = seq >= 0 && seq < a.B && (packed_q || (row >= 0 && row < most));
-    char *const dst = (char *)(is_q ? a.q_out : turns ? a.k_out : a.v_out) + (packed_q ? t * heads + h : ((l * a.B + seq) * heads + h) * most + row) * kD * E::EB;
-    return Row{(const char *)(is_q ? a.q : turns ? a.k : a.v) + (t * (is_q ? a.ld_q : turns ? a.ld_k : a.ld_v) + h * kD) * E::EB, live ? dst : nullptr, tok, turns};
+    const bool packed_q = is_q && a.q_rows == 0;
+    if (first + tid / LANES >= items || seq < 0 || seq >= a.B || (!packed_q && (row < 0 || row >= most))) return nullptr;
+    return (u32x4 *)((char *)(is_q ? a.q_out : turns ? a.k_out : a.v_out) + (packed_q ? t * heads + h : ((l * a.B + seq) * heads + h) * most + row) * kD * E::EB);
   };
-  auto load = [&](const Row &w, bool any, u32x4 &x0, u32x4 &x1) {
-    if (any ? w.src != nullptr : w.dst != nullptr) {
-      x0 = ld_stream((const u32x4 *)w.src + c0);
-      x1 = ld_stream((const u32x4 *)w.src + c1);
-    }
-  };
-  Row next = row_of(0);
+
+  const uint64_t turn = (tid & 63) < half ? a.turns[tid & 63] : 0;
+  if (tid < here) {
+    const int64_t t = t0 + tid;
+    records[tid] = *(const i32x4 *)(a.map + (a.L == 1 ? t : t % a.n) * 4);
+  }
+  Place now = place(0);
   u32x4 n0{}, n1{};
-  load(next, early != 0, n0, n1);
-  for (int i = tid; i < here * 64; i += kThreads)
-    if ((i & 63) < half) turned(a.map[(t0 + (i >> 6)) % a.n * 4 + 1], a.turns[i & 63], a.gain, sn[i], cs[i]);
+  if (early) {
+    const u32x4 *const x = source(now);
+    n0 = ld_stream(x + c0);
+    n1 = ld_stream(x + c1);
+  }
+  __syncthreads();
+  u32x4 *to = target(now, 0);
+  if (!early && to != nullptr) {
+    const u32x4 *const x = source(now);
+    n0 = ld_stream(x + c0);
+    n1 = ld_stream(x + c1);
+  }
+  for (int i = tid; i < here * 64; i += kThreads) {   // (kThreads is a multiple of 64)
+    const int tok = i >> 6, j = i & 63;
+    float s, c;
+    turned(records[tok][1], turn, a.gain, s, c);
+    if constexpr (ANY) {
+      if (j < half) {
+        sn[tok * kD + j] = -s;
+        sn[tok * kD + j + half] = s;
+        cs[tok * kD + j] = cs[tok * kD + j + half] = c;
+      }
+    } else {
+      sn[i] = s;
+      cs[i] = c;
+    }
+  }
   __syncthreads();
   for (int first = 0; first < items; first += ROWS) {
-    const Row w = next;
-    u32x4 x0 = n0, x1 = n1;
+    u32x4 x0 = n0, x1 = n1, *const dst = to;
+    const int tok = now.tok;
+    const bool turns = dst != nullptr && now.r < nq + nk;
     if (first + ROWS < items) {
-      next = row_of(first + ROWS);
-      load(next, false, n0, n1);
-    }
-    if constexpr (FORM == kHalvesAny) {
-      float f[2 * VEC];
-      E::unpack(x0, (float (&)[VEC])f[0]);
-      E::unpack(x1, (float (&)[VEC])f[VEC]);
-      float *const mine = row_lds + tid / LANES * LDR;   // (a wave's own)
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int e = 0; e < 2 * VEC; e += 4) *(float4 *)(mine + 2 * VEC * p + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      if (w.dst != nullptr && w.turns && 2 * VEC * p < a.rot) {
-#pragma unroll
-        for (int e = 0; e < 2 * VEC; ++e) {
-          const int c = 2 * VEC * p + e;
-          const bool lower = c < half;
-          const int i = min(lower ? c : c - half, 63);
-          const float s = sn[w.tok * 64 + i], k = cs[w.tok * 64 + i], y = mine[min(lower ? c + half : c - half, kD - 1)];
-          const float turned_e = fmaf(f[e], k, lower ? -y * s : y * s);
-          f[e] = c < a.rot ? turned_e : f[e];
-        }
-        const u32x4 y0 = packed<DT>((const float (&)[VEC])f[0]), y1 = packed<DT>((const float (&)[VEC])f[VEC]);
-        // channels that are not turned keep their bits
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          constexpr int per = VEC / 4;   // channels of a word (rot is even: a word of two has both or neither)
-          x0[u] = 2 * VEC * p + u * per < a.rot ? y0[u] : x0[u];
-          x1[u] = 2 * VEC * p + VEC + u * per < a.rot ? y1[u] : x1[u];
-        }
+      now = place(first + ROWS);
+      to = target(now, first + ROWS);
+      if (to != nullptr) {
+        const u32x4 *const x = source(now);
+        n0 = ld_stream(x + c0);
+        n1 = ld_stream(x + c1);
       }
-    } else if (w.dst != nullptr && w.turns && p * VEC < half) {
+    }
+    if constexpr (ANY) {
+      float *const row = mates + tid / LANES * LDR;   // (a wave's own)
+      auto give = [&](const u32x4 &x, int c) {   // the chunk's elements to where their mates look for them
+        if (c >= a.rot) return;
+        float f[VEC];
+        E::unpack(x, f);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (c + e < a.rot) row[c + e < half ? c + e + half : c + e - half] = f[e];
+      };
+      auto turn_chunk = [&](u32x4 &x, int c) {
+        if (!turns || c >= a.rot) return;
+        float f[VEC];
+        E::unpack(x, f);
+        const float *const s = sn + tok * kD + c, *const k = cs + tok * kD + c, *const y = row + c;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f[e] = fmaf(f[e], k[e], y[e] * s[e]);
+        const u32x4 z = packed<DT>(f);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = c + u * (VEC / 4) < a.rot ? z[u] : x[u];   // channels that are not turned keep their bits (rot is even: a word of two has both or neither)
+      };
+      const int c = 2 * VEC * p;
+      give(x0, c);
+      give(x1, c + VEC);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      turn_chunk(x0, c);
+      __builtin_amdgcn_sched_barrier(0);   // (one chunk's operands in registers at a time)
+      turn_chunk(x1, c + VEC);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    } else if (turns && p * VEC < half) {
       float f0[VEC], f1[VEC];
       E::unpack(x0, f0);
       E::unpack(x1, f1);
-      const float *const s = sn + w.tok * 64 + p * VEC, *const k = cs + w.tok * 64 + p * VEC;
+      const float *const s = sn + tok * 64 + p * VEC, *const k = cs + tok * 64 + p * VEC;
       if constexpr (FORM == kHalves) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
@@ -174,17 +208,16 @@ __global__ __launch_bounds__(kThreads) void k_rope(RopeArgs a, int tokens, int p
         }
       }
     }
-    if (w.dst != nullptr) {
-      st_stream((u32x4 *)w.dst + c0, x0);
-      st_stream((u32x4 *)w.dst + c1, x1);
+    if (dst != nullptr) {
+      st_stream(dst + c0, x0);
+      st_stream(dst + c1, x1);
     }
   }
 }
 
 template <int DT>
-const void *kernel_of(const RopeArgs &a) {
-  if (a.layout == THK_ROPE_PAIRS) return (const void *)k_rope<DT, kPairs>;
-  return a.rot / 2 % Elem<DT>::VEC == 0 ? (const void *)k_rope<DT, kHalves> : (const void *)k_rope<DT, kHalvesAny>;
+const void *kernel_of(int form) {
+  return form == kPairs ? (const void *)k_rope<DT, kPairs> : form == kHalves ? (const void *)k_rope<DT, kHalves> : (const void *)k_rope<DT, kHalvesAny>;
 }
 
 }  // namespace
@@ -196,11 +229,12 @@ hipError_t launch_rope(int dtype, const RopeArgs &a, hipStream_t st) {
   RopeArgs copy = a;
   const int pass = dtype == THK_F32 ? 16 : 32;
   const int64_t all = a.L * a.n;
-  const bool large = all * a.rows >= (int64_t)pass * 16 * kCUs;
-  int tokens = large ? std::min(std::max(4 * pass / a.rows, 1), kTokens) : 1;
+  const int form = a.layout == THK_ROPE_PAIRS ? kPairs : a.rot / 2 % (dtype == THK_F32 ? 4 : 8) == 0 ? kHalves : kHalvesAny;
+  const bool large = all >= 2 * kCUs;
+  int tokens = large ? std::min(std::max(2 * pass / a.rows, 1), most_tokens(form)) : 1;
   int part = large ? a.rows : std::min(pass, a.rows), parts = (a.rows + part - 1) / part, early = all * a.rows <= 4 * pass * kCUs;
   void *args[] = {&copy, &tokens, &part, &parts, &early};
-  return launch_main_kernel(dtype == THK_F32 ? kernel_of<THK_F32>(a) : kernel_of<THK_BF16>(a),
+  return launch_main_kernel(dtype == THK_F32 ? kernel_of<THK_F32>(form) : kernel_of<THK_BF16>(form),
                             dim3((unsigned)((all + tokens - 1) / tokens * parts)), dim3(kThreads), args, 0, st);
 }
 
