@@ -26,25 +26,35 @@ __device__ __forceinline__ WaveSum<I> wave_sum(I x) {
 // ---- token map ----------------------------------------------------------------------------
 constexpr int kMapThreads = 256;
 
-// starts[b]: tokens in front of sequence b, at most n, and starts[B].  By one block.
-template <int THREADS, class Put>
-__device__ __forceinline__ void running_sums(const TokenMapArgs &a, int64_t *wave_total, Put put) {
+// starts[b]: tokens in front of sequence b, at most n, and starts[B].  By one block, EACH sequences a thread at a time.
+template <int THREADS, int EACH, class Put>
+__device__ __forceinline__ void running_sums(const TokenMapArgs &a, int64_t (*wave_total)[THREADS / 64], Put put) {
   const int tid = threadIdx.x, wave = tid >> 6;
   int64_t base = 0;
-  for (int b0 = 0; b0 < a.B; b0 += THREADS) {
-    const int b = b0 + tid;
-    const int64_t x = b >= a.B ? 0 : a.n_new == nullptr ? 1 : max(a.n_new[b], 0);
-    const WaveSum<int64_t> w = wave_sum(x);
-    if ((tid & 63) == 63) wave_total[wave] = w.all;
+  for (int b0 = 0, turn = 0; b0 < a.B; b0 += THREADS * EACH, turn ^= 1) {
+    int64_t x[EACH], sum = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int b = b0 + tid * EACH + i;
+      x[i] = a.n_new == nullptr ? 1 : max(a.n_new[min(b, a.B - 1)], 0);
+      if (b >= a.B) x[i] = 0;
+      sum += x[i];
+    }
+    const WaveSum<int64_t> w = wave_sum(sum);
+    if ((tid & 63) == 63) wave_total[turn][wave] = w.all;
     __syncthreads();
     int64_t before = base + w.before;
 #pragma unroll
     for (int i = 0; i < THREADS / 64; ++i) {
-      if (i < wave) before += wave_total[i];
-      base += wave_total[i];
+      if (i < wave) before += wave_total[turn][i];
+      base += wave_total[turn][i];
     }
-    if (b < a.B) put(b, (int)min(before, a.n));
-    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int b = b0 + tid * EACH + i;
+      if (b < a.B) put(b, (int)min(before, a.n));
+      before += x[i];
+    }
   }
   if (tid == 0) put(a.B, (int)min(base, a.n));
 }
@@ -71,8 +81,10 @@ __device__ __forceinline__ void put_token(const TokenMapArgs &a, const int *star
 // Every block makes the running sums of all sequences for itself: a trip to memory and some barriers, less than a second launch.
 __global__ __launch_bounds__(kMapThreads) void k_token_map(TokenMapArgs a) {
   __shared__ int starts[kMapSequences + 1];
-  __shared__ int64_t wave_total[kMapThreads / 64];
-  running_sums<kMapThreads>(a, wave_total, [&](int b, int s) { starts[b] = s; });
+  __shared__ int64_t wave_total[2][kMapThreads / 64];
+  auto put = [&](int b, int s) { starts[b] = s; };
+  if (a.B <= kMapThreads) running_sums<kMapThreads, 1>(a, wave_total, put);
+  else running_sums<kMapThreads, 4>(a, wave_total, put);
   __syncthreads();
   if (blockIdx.x == 0 && a.starts != nullptr)
     for (int b = threadIdx.x; b <= a.B; b += kMapThreads) a.starts[b] = starts[b];
@@ -82,8 +94,8 @@ __global__ __launch_bounds__(kMapThreads) void k_token_map(TokenMapArgs a) {
 
 // More sequences than that: the sums first, in memory.
 __global__ __launch_bounds__(1024) void k_starts(TokenMapArgs a) {
-  __shared__ int64_t wave_total[16];
-  running_sums<1024>(a, wave_total, [&](int b, int s) { a.starts[b] = s; });
+  __shared__ int64_t wave_total[2][16];
+  running_sums<1024, 4>(a, wave_total, [&](int b, int s) { a.starts[b] = s; });
 }
 __global__ __launch_bounds__(kMapThreads) void k_token_map_of(TokenMapArgs a) {
   const int64_t t = (int64_t)blockIdx.x * kMapThreads + threadIdx.x;
@@ -191,7 +203,7 @@ constexpr int kStep = 8 * kPlanThreads;   // pages that a block looks at in a st
 struct PlanLds {
   int start[kPlanSequences], have[kPlanSequences], from[kPlanSequences];
   int64_t wave_total[2][kPlanWaves];
-  int n_ending;
+  int total;
   union {
     struct { int ending[kPlanSequences], held[kPlanSequences]; };
     int pages[kStep];   // free ones, in order
@@ -203,7 +215,7 @@ template <bool ONE, bool MOVES>
 __device__ __forceinline__ int64_t plan_sequences(const ReserveArgs &a, PlanLds &s, MeetingOf<MOVES> &meeting, int (&want)[kPlanEach]) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   int need[kPlanEach], have[kPlanEach], from[kPlanEach], held[kPlanEach];
-  if (tid == 0) s.n_ending = 0;
+  if (tid == 0) s.total = 0;
   if constexpr (MOVES) meeting.m.clear(a.B, tid);
 #pragma unroll
   for (int i = 0; i < kPlanEach; ++i) {
@@ -221,15 +233,15 @@ __device__ __forceinline__ int64_t plan_sequences(const ReserveArgs &a, PlanLds 
 #pragma unroll
     for (int i = 0; i < kPlanEach; ++i) {
       const int b = i * kPlanThreads + tid;
-      if (held[i] > need[i]) s.ending[atomicAdd(&s.n_ending, 1)] = b;
+      if (held[i] > need[i]) s.ending[atomicAdd(&s.total, 1)] = b;
       if (b < a.B) {
         s.have[b] = have[i];
         s.held[b] = held[i];
       }
     }
     __syncthreads();
-    for (int i = wave; i < s.n_ending; i += kPlanWaves) give_back(a, s.ending[i], s.have[s.ending[i]], s.held[s.ending[i]], lane);
-    if (s.n_ending > 0) phase_end();
+    for (int i = wave; i < s.total; i += kPlanWaves) give_back(a, s.ending[i], s.have[s.ending[i]], s.held[s.ending[i]], lane);
+    if (s.total > 0) phase_end();
   }
   if constexpr (MOVES) {
     Meeting &m = meeting.m;
@@ -352,9 +364,9 @@ __global__ __launch_bounds__(kPlanThreads) void k_reserve_one(ReserveArgs a) {
   }
 }
 
-// Pools of more pages than this: four launches.
+// Pools of more pages than this: three launches.
 constexpr int64_t kOnePages = 65536;
-// What is given back by a wave for each sequence, the sequences' plan by one block, the free pages counted by chunk, and given out.
+// What is given back, by a wave for each sequence; the sequences' plan, by one block, and the free pages counted beside it; the pages given out.
 constexpr int kChunk = 4096, kChunkThreads = 1024, kChunkWaves = kChunkThreads / 64, kChunkEach = kChunk / kChunkThreads;   // pages that a block looks at together: its part of the pool is as many of them as make
 constexpr int kMostChunks = 1024;   // at most so many parts
 struct ReserveWs {
@@ -372,20 +384,6 @@ __global__ __launch_bounds__(256) void k_give_back(ReserveArgs a) {
   const int need = needed(a, (int)b), held = held_of(a, (int)b);
   if (held > need) give_back(a, (int)b, need, held, threadIdx.x & 63);
 }
-template <bool MOVES>
-__global__ __launch_bounds__(kPlanThreads) void k_plan_sequences(ReserveArgs a) {
-  __shared__ PlanLds s;
-  __shared__ MeetingOf<MOVES> meeting;
-  int want[kPlanEach];
-  const int64_t wanted = plan_sequences<false, MOVES>(a, s, meeting, want);
-  const ReserveWs w = reserve_ws(a.ws, a.B);
-  if (threadIdx.x == 0) *w.wanted = wanted;
-#pragma unroll
-  for (int i = 0; i < kPlanEach; ++i) {
-    const int b = i * kPlanThreads + threadIdx.x;
-    if (b < a.B) w.plan[b] = {s.have[b], s.have[b] + want[i] - (s.from[b] >= 0), s.from[b], s.start[b]};
-  }
-}
 // A thread's pages of a chunk, in order of waves, 64 pages at a time, lanes.
 __device__ __forceinline__ void chunk_pages(const ReserveArgs &a, int64_t p0, u64 (&free)[kChunkEach]) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -398,20 +396,37 @@ __device__ __forceinline__ void chunk_pages(const ReserveArgs &a, int64_t p0, u6
 #pragma unroll
   for (int i = 0; i < kChunkEach; ++i) free[i] = __ballot(users[i] <= 0 && p0 + (wave * kChunkEach + i) * 64 + lane < a.n_pages);
 }
-__global__ __launch_bounds__(kChunkThreads) void k_count_free(ReserveArgs a, int64_t part) {
-  __shared__ int total;
-  if (threadIdx.x == 0) total = 0;
+// Block 0 plans, block 1 + i counts part i: neither needs what the other writes.
+static_assert(kPlanThreads == kChunkThreads);
+template <bool MOVES>
+__global__ __launch_bounds__(kPlanThreads) void k_plan_and_count(ReserveArgs a, int64_t part) {
+  __shared__ PlanLds s;
+  __shared__ MeetingOf<MOVES> meeting;
+  const ReserveWs w = reserve_ws(a.ws, a.B);
+  if (blockIdx.x == 0) {
+    int want[kPlanEach];
+    const int64_t wanted = plan_sequences<false, MOVES>(a, s, meeting, want);
+    if (threadIdx.x == 0) *w.wanted = wanted;
+#pragma unroll
+    for (int i = 0; i < kPlanEach; ++i) {
+      const int b = i * kPlanThreads + threadIdx.x;
+      if (b < a.B) w.plan[b] = {s.have[b], s.have[b] + want[i] - (s.from[b] >= 0), s.from[b], s.start[b]};
+    }
+    return;
+  }
+  const int64_t i = blockIdx.x - 1;
+  if (threadIdx.x == 0) s.total = 0;
   __syncthreads();
   int n = 0;
-  for (int64_t p0 = blockIdx.x * part; p0 < min((blockIdx.x + 1) * part, a.n_pages); p0 += kChunk) {
+  for (int64_t p0 = i * part; p0 < min((i + 1) * part, a.n_pages); p0 += kChunk) {
     u64 free[kChunkEach];
     chunk_pages(a, p0, free);
 #pragma unroll
-    for (int i = 0; i < kChunkEach; ++i) n += __popcll(free[i]);
+    for (int j = 0; j < kChunkEach; ++j) n += __popcll(free[j]);
   }
-  if ((threadIdx.x & 63) == 0) atomicAdd(&total, n);
+  if ((threadIdx.x & 63) == 0) atomicAdd(&s.total, n);
   __syncthreads();
-  if (threadIdx.x == 0) reserve_ws(a.ws, a.B).counts[blockIdx.x] = total;
+  if (threadIdx.x == 0) w.counts[i] = s.total;
 }
 __global__ __launch_bounds__(kChunkThreads) void k_give_out(ReserveArgs a, int64_t part) {
   __shared__ int start[kPlanSequences], have[kPlanSequences];   // have: its highest bit where a page is to be replaced
@@ -620,8 +635,7 @@ hipError_t launch_reserve(const ReserveArgs &a, hipStream_t st) {
   if (a.n_pages <= kOnePages) return launch(a.now != nullptr ? (const void *)k_reserve_one<true> : (const void *)k_reserve_one<false>, 1, kPlanThreads, st, a);
   const int64_t chunks = (a.n_pages + kChunk - 1) / kChunk, part = (chunks + kMostChunks - 1) / kMostChunks * kChunk, parts = (a.n_pages + part - 1) / part;
   hipError_t e = launch((const void *)k_give_back, (a.B + 3) / 4, 256, st, a);
-  if (e == hipSuccess) e = launch(a.now != nullptr ? (const void *)k_plan_sequences<true> : (const void *)k_plan_sequences<false>, 1, kPlanThreads, st, a);
-  if (e == hipSuccess) e = launch((const void *)k_count_free, parts, kChunkThreads, st, a, part);
+  if (e == hipSuccess) e = launch(a.now != nullptr ? (const void *)k_plan_and_count<true> : (const void *)k_plan_and_count<false>, 1 + parts, kPlanThreads, st, a, part);
   return e == hipSuccess ? launch((const void *)k_give_out, parts, kChunkThreads, st, a, part) : e;
 }
 
