@@ -373,9 +373,15 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
         x.at = to;
       }
       u64 list = sorted(more);
-      for (int i = 64; i < count; i += 64) {
-        more = i + lane < count ? keys[i + lane] : 0;
-        if (__ballot(more > key_at(list, a.K - 1)) != 0) list = joined(list, sorted(more));
+      for (int i = 64; i < count; i += 4 * 64) {
+        u64 four[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) four[u] = keys[min(i + u * 64 + lane, count - 1)];   // (all under way at once)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          more = i + u * 64 + lane < count ? four[u] : 0;
+          if (__ballot(more > key_at(list, a.K - 1)) != 0) list = joined(list, sorted(more));
+        }
       }
       join_sums(x.at, x.sum);
       if (list != 0 && lane < a.K) {   // (a sum that is NaN leaves no score)

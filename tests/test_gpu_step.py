@@ -742,3 +742,73 @@ def test_two_graphs_may_share_a_workspace_and_streams_need_one_each():
     torch.cuda.synchronize()
     for o, w in zip(outs, want):
         assert all(np.array_equal(y.cpu().numpy(), z) for y, z in zip(o, w))
+
+
+# ---- far offsets --------------------------------------------------------------------------
+def test_rope_rows_past_4_gib():
+    """Buffers of more than 2^32 bytes: rows at both ends of the last head of the last sequence."""
+    cap, r = (1 << 23) + 5, Rope("bf16", False, 128)      # 2 x 2 x 2^23 rows of 256 bytes: 8 GiB
+    rec = np.array([[1, 7, 0, -1], [1, 8, cap - 1, -1], [0, 9, 3, -1]])
+    k, v = (torch.randn(1, 3, 2 * D, device="cuda").bfloat16() for _ in range(2))
+    shape = thk.make_shape(1, 2, 2, 2, D, 1, 1, 1, 0, thk.THK_BF16)
+    k_out = torch.empty(2, 2, cap, D, dtype=torch.bfloat16, device="cuda")
+    v_out = torch.empty_like(k_out)
+    thk.thk_rope_qkv(shape, r.rope, r.turns, None, 0, k, 2 * D, v, 2 * D, ints(rec), 3, None, 0, k_out, v_out, cap)
+    torch.cuda.synchronize()
+    want = r.exact(k.reshape(3, 2, D), rec[:, 1])
+    tol = r.bound(k.reshape(3, 2, D), want)
+    for t, (b, _, row, _) in enumerate(rec):
+        assert torch.equal(v_out[b, :, row], v[0, t].reshape(2, D))
+        assert (np.abs(f64(k_out[b, :, row]) - want[t]) <= tol[t]).all()
+
+
+def test_reorder_and_copies_past_4_gib():
+    cap = (1 << 23) + 3
+    shape = thk.make_shape(1, 3, 1, 1, D, 64, 1, 1, 0, thk.THK_BF16)
+    kt = torch.empty(1, 3, 1, cap, D, dtype=torch.bfloat16, device="cuda")      # 6 GiB
+    vt = torch.empty_like(kt)
+    rows = [0, 1 << 20, cap - 1]
+    for x in (kt, vt):
+        for b in range(3):
+            x[0, b, 0, rows] = torch.randn(3, D, device="cuda").bfloat16()
+    before = [x[0, :, 0, rows].clone() for x in (kt, vt)]
+    thk.thk_beam_reorder(shape, None, 3, ints([[2, 0, 1]]), 3, kt, vt, ints([cap, cap, cap - 1]), cap, None, None, None, None)
+    torch.cuda.synchronize()
+    for x, was in zip((kt, vt), before):
+        got = x[0, :, 0, rows]
+        assert torch.equal(got[0, :2], was[2, :2]) and torch.equal(got[0, 2], was[0, 2])      # the parent's last row is not in use
+        assert torch.equal(got[1], was[0]) and torch.equal(got[2], was[1])
+    del kt, vt
+    shape, pages = thk.make_shape(1, 1, 1, 1, D, 64, 1, 128, 0, thk.THK_F32), thk.make_pages(0, 65536, 1, 80)      # 80 pages of 64 MiB
+    pool = torch.empty(thk.thk_paged_pool_bytes(shape, pages), dtype=torch.uint8, device="cuda").reshape(80, 1024, -1)
+    pool[79] = torch.randint(0, 256, pool[79].shape, dtype=torch.uint8, device="cuda")
+    pool[78] = 7
+    thk.thk_paged_copy(shape, pages, ints([[79, 2, 1000, 0], [79, 78, 1, 0]]), 2, pool)
+    torch.cuda.synchronize()
+    assert torch.equal(pool[2, :1000], pool[79, :1000]) and torch.equal(pool[78, 0], pool[79, 0]) and (pool[78, 1:] == 7).all()
+
+
+def test_beam_select_rows_past_4_gib():
+    V, ld = 5000, (1 << 30) + 8
+    x = torch.empty(3 * ld, dtype=torch.bfloat16, device="cuda")      # 6 GiB
+    rng = np.random.default_rng(4)
+    rows = logits(rng, 1, 3, V, "bf16")
+    for w in range(3):
+        x[w * ld:w * ld + V] = rows[0, w]
+    s = -5 * rng.random((1, 3))
+    want = gpu_select(rows, s, None, 6, 1)
+    got = gpu_select(x.reshape(1, 3, ld), s, None, 6, 1, ld=(ld, V))
+    assert all(np.array_equal(a, b) for a, b in zip(got, want))
+
+
+def test_beam_select_largest_vocabulary():
+    """2^24 tokens of one beam: a thousand pieces are joined."""
+    V = 1 << 24
+    x = torch.zeros(1, 1, V, device="cuda")
+    at = torch.randperm(V, generator=torch.Generator().manual_seed(5))[:80]
+    x[0, 0, at.cuda()] = torch.arange(80, device="cuda").float() / 8 + 1
+    parent, token, score, ended = gpu_select(x, np.zeros((1, 1)), None, 64, 0)
+    assert token[0].tolist() == at.flip(0)[:64].tolist() and not parent.any() and not ended[token != 0].any()
+    e = np.arange(80)[::-1] / 8 + 1
+    want = e[:64] - math.log(np.exp(e).sum() + V - 80)
+    assert np.abs(score[0] - want).max() <= sum_error(V) + 2.0 ** -24 * 20
