@@ -573,7 +573,7 @@ thk_status thk_rope_turns(const thk_rope *rope, uint64_t *turns);
  *   k_out, v_out [L][B][N_kv][cap][D] at the map's rows: keys turned, values as they are
  * with cap = S_tail_cap and q_rows = 1 a decode step (thk_tail_append_ragged and the query's turn), with cap = S and q_rows = S_obs the
  * end of a prompt as thk_prune reads it.  Each of the three inputs may be NULL, with its output.  What the map does not name
- * stays as it was.  ld_* are multiples of 16 bytes (THK_ERR_ALIGN).  Outputs must not overlap inputs, but that q_out may be q with
+ * stays as it was.  L n_tokens rows (of heads, all three together) are at most 2^27.  ld_* are multiples of 16 bytes (THK_ERR_ALIGN).  Outputs must not overlap inputs, but that q_out may be q with
  * q_rows = 0 and ld_q = N_q D.  turns [rot / 2] device, 8-byte aligned.  Infinities and NaN stay in their pairs.
  */
 thk_status thk_rope_qkv(const thk_shape *shape, const thk_rope *rope, const uint64_t *turns,
@@ -623,7 +623,8 @@ thk_status thk_paged_copy(const thk_shape *shape, const thk_pages *pages, const 
  *   score_out     [B][K]  (there: -inf); may be scores where K = W
  *   done_out      [B][K]  1 where the token is eos or the parent has ended (there: 0); may be NULL, and done where K = W
  * With K = 2 W a caller can set those that end aside and go on with the W best that do not.  Sums are fp32 in eights and 64
- * bits from there on; scores are 64 bits until they are written.
+ * bits from there on; scores are 64 bits until they are written.  A score is off by at most 2^-23 (13 + 1.2 ln V) in front of its
+ * rounding, the same for beams that are alike: continuations of different beams that are nearer than that may change places.
  *   ws : thk_beam_workspace_bytes() bytes.  Calls that may run at the same time need one each.
  */
 typedef struct {
@@ -660,7 +661,7 @@ thk_status thk_beam_reorder(const thk_shape *shape, const thk_pages *pages, int3
  * Timing hook for benchmarks: the main kernel of the NEXT call made by this host
  * thread (the one-launch prune kernel, or the compaction kernel of the staged
  * form; the attention kernel, not the split merge; the value-score attention
- * kernel) is launched with `ev_start` and `ev_stop` attached to it, so that the
+ * kernel; the first kernel of the calls around a serving step) is launched with `ev_start` and `ev_stop` attached to it, so that the
  * interval between the two events is that kernel's own duration -- begin to end
  * of its execution, as a profiler reports it; nothing extra enters the stream.
  * Both are hipEvent_t handles passed as void*, created by the caller with

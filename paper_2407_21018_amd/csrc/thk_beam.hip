@@ -190,12 +190,13 @@ struct Tile {
 };
 
 // The sum's exponents are relative to a value `at` of the lane, at most 8 below its largest element: sum of 2^(x L - c), L = log2 e in 32 bits
-// and c = at L, one rounding for an element, and what c's rounding leaves is made good when the sum is used.  Where at L has no place in 32
-// bits (values below -1e38, and lanes that have seen nothing but -inf), the difference is taken first.  NaN and +inf make the sum NaN.
-constexpr float kLog2e = 0x1.715476p0f, kFar = -1e38f;
+// and c = at L, one rounding for an element, and what c's rounding leaves is made good when the sum is used.  Where that is no longer a
+// fraction (values beyond 2^20, and lanes that have seen nothing but -inf), the difference is taken first.  NaN and +inf make the sum NaN.
+constexpr float kLog2e = 0x1.715476p0f;
+__device__ __forceinline__ bool is_far(float at) { return !(fabsf(at) <= 0x1p20f); }
 __device__ __forceinline__ double relative(double sum, float at) {   // ... to the value itself
   const float c = at * kLog2e;
-  return at < kFar ? sum : sum * (double)__builtin_amdgcn_exp2f(-fmaf(at, kLog2e, -c));
+  return is_far(at) ? sum : sum * (double)__builtin_amdgcn_exp2f(-fmaf(at, kLog2e, -c));
 }
 
 template <int DT>
@@ -240,8 +241,8 @@ __global__ __launch_bounds__(kWaves * 64, DT == THK_F32 ? 3 : 4) void k_beam_pie
       at = to;
       c = at * kLog2e;
     }
-    if (__ballot(at < kFar) != 0) {
-      const float left = at < kFar ? 0.f : fmaf(at, kLog2e, -c);
+    if (__ballot(is_far(at)) != 0) {
+      const float left = is_far(at) ? 0.f : fmaf(at, kLog2e, -c);
 #pragma unroll
       for (int i = 0; i < 32; ++i) x[i] = fmaf(x[i] - at, kLog2e, left);
     } else {
@@ -558,7 +559,7 @@ hipError_t reorder(int dtype, const ReorderArgs &a, hipStream_t st) {
 
 size_t beam_ws_bytes(const BeamArgs &a) {
   const int64_t pieces = beam_plan(a).pieces, blocks = (int64_t)a.B * a.W * pieces;
-  return blocks * kWaves * 64 > 0xffffffffll ? 0 : (size_t)blocks * (sizeof(PieceStats) + a.K * sizeof(u64));
+  return blocks * kWaves * 64 > 0xffffffffll || (int64_t)a.B * kJoinWaves * 64 > 0xffffffffll ? 0 : (size_t)blocks * (sizeof(PieceStats) + a.K * sizeof(u64));
 }
 
 hipError_t launch_beam_select(int dtype, const BeamArgs &a, hipStream_t st) {

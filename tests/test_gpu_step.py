@@ -393,11 +393,11 @@ def gpu_select(x, scores, done, K, eos, ld=0, in_place=False):
 
 
 # A row's sum is of terms 2^(x L - c), c at most 8 L below x L for the largest element of a lane: the exponent is rounded once, 2^-24 of itself
-# at most, and L, log2 e in 32 bits, is off by 2^-26 (values below -1e38 apart: two roundings).  With |d| = |x - r|, a term is off by 2.25 2^-24 |d|
+# at most, and L, log2 e in 32 bits, is off by 2^-26 (beyond 2^20 the difference x - r is rounded first, once more).  With |d| = |x - r|, a term is off by 2.25 2^-24 |d|
 # of itself; the sum by that of the mean of |d| under its own weights, which is at most 8 + ln V (the largest element's distance to the mean
-# is an entropy's part).  2^y is within 2^-23, and three sums of 2^-24 follow before 64 bits.
+# is an entropy's part).  2^y is within 2^-23, and so is what makes c's own rounding good; three sums of 2^-24 lie between, before 64 bits.
 def sum_error(V):
-    return 2.25 * 2.0 ** -24 * (8 + math.log(V)) + 5 * 2.0 ** -24
+    return 2.25 * 2.0 ** -24 * (8 + math.log(V)) + 7 * 2.0 ** -24
 
 
 def check_select(x, scores, done, K, eos, **kw):
@@ -468,6 +468,19 @@ def test_beam_select_masks(dtype):
     s[0, 0], s[1, 1], s[2, 2], s[5, 0], s[5, 2] = -inf, inf, float("nan"), -inf, 3e38
     check_select(x, s, None, 6, 3)
     check_select(x, s, np.ones((6, 3)), 6, 3)
+
+
+def test_beam_select_far_values():
+    """Logits of any size up to the end of the range, of either sign: what is small about them is their differences, and differences may
+    have no place in 32 bits."""
+    rng = np.random.default_rng(10)
+    for shift in (1e3, -1e4, 2.0 ** 20, -2.0 ** 20 - 1, 3e7, -1e9):
+        x = torch.tensor(np.round(rng.standard_normal((2, 3, 4100)) * 3) * max(1.0, abs(shift) * 2.0 ** -23) + shift, dtype=torch.float32, device="cuda")
+        check_select(x, -np.arange(6).reshape(2, 3) / 7, None, 9, 1)
+    for values in ([3.2e38, 3.1e38, -3.2e38], [-3.2e38, -3.3e38, -3.4e38], [1.5e38, -1.5e38, 9e37], [-9e37, -1.1e38, 0.0], [1e38, 1.0000001e38, 5.0]):
+        x = torch.full((1, 2, 5000), values[2], device="cuda")
+        x[0, 0, 4000], x[0, 0, 17], x[0, 1, 4999], x[0, 1, 4998] = values[0], values[1], values[0], values[0]
+        check_select(x, np.array([[0.0, 0.25]]), None, 3, 1)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -152,7 +152,7 @@ def test_beam_select_refusals():
     def beams(**kw):
         return thk.make_beams(**{**dict(B=2, W=4, K=8, V=1000, eos=2), **kw})
     for kw, want in ((dict(B=0), 2), (dict(W=0), 2), (dict(W=33), 2), (dict(K=0), 2), (dict(K=65), 2), (dict(V=0), 2), (dict(V=(1 << 24) + 1), 2),
-                     (dict(ld=999), 2), (dict(ld=-1), 2), (dict(eos=1000), 2), (dict(eos=-2), 2), (dict(dtype=2), 3), (dict(B=1 << 24), 2)):
+                     (dict(ld=999), 2), (dict(ld=-1), 2), (dict(eos=1000), 2), (dict(eos=-2), 2), (dict(dtype=2), 3), (dict(B=1 << 24), 2), (dict(B=1 << 23, W=1, V=8), 2)):
         b = beams(**kw)
         assert thk.thk_beam_workspace_bytes(b) == 0 and _select(b) == want, kw
     b = beams()
