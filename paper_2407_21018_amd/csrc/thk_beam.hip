@@ -439,28 +439,29 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
 template <int DT, int W>
 __global__ __launch_bounds__(256) void k_reorder_tails(ReorderArgs a, int blocks) {
   constexpr int CPR = kD * Elem<DT>::EB / 16;
-  __shared__ int from[kMostBeams], rows[kMostBeams], most;
+  __shared__ int from[W], rows[W], tail[W], most;
   const int64_t g2 = blockIdx.x / (unsigned)blocks, g = g2 >> 1;    // (layer, prompt, head), keys or values
   const int64_t lp = g / a.N_kv, h = g - lp * a.N_kv, p = lp % a.prompts;
   const int tid = threadIdx.x;
   if (tid == 0) most = 0;
-  if (tid < W) rows[tid] = from[tid] = 0;
+  int par = -1;
+  if (tid < W) {
+    if (tid < a.W) {
+      par = a.parent[p * a.ld_parent + tid];
+      tail[tid] = a.s_tail[p * a.W + tid];
+    }
+    rows[tid] = from[tid] = 0;
+  }
   __syncthreads();
-  if (tid < a.W) {
-    const int par = a.parent[p * a.ld_parent + tid];
-    const bool other = par >= 0 && par < a.W && par != tid;
-    const int n = other ? min(a.s_tail[p * a.W + par], a.cap) : 0;
-    from[tid] = other ? par : 0;
+  if (tid < a.W && par >= 0 && par < a.W && par != tid) {
+    const int n = min(tail[par], a.cap);
+    from[tid] = par;
     rows[tid] = n;
     if (n > 0) atomicMax(&most, n);
   }
   __syncthreads();
-  const int64_t block = blockIdx.x - g2 * blocks;
-  const int64_t c = block * 256 + tid;
-  const int row = (int)(c / CPR);
-  if (row >= most) return;
   const int64_t stride = (int64_t)a.N_kv * a.cap * CPR;
-  u32x4 *const x = (u32x4 *)(g2 & 1 ? a.v_tail : a.k_tail) + ((lp * a.W * a.N_kv + h) * a.cap * CPR + c);
+  u32x4 *const x0 = (u32x4 *)(g2 & 1 ? a.v_tail : a.k_tail) + (lp * a.W * a.N_kv + h) * a.cap * CPR;
   int n[W];
   int64_t at[W];
 #pragma unroll
@@ -468,12 +469,17 @@ __global__ __launch_bounds__(256) void k_reorder_tails(ReorderArgs a, int blocks
     n[j] = __builtin_amdgcn_readfirstlane(rows[j]);
     at[j] = (int64_t)__builtin_amdgcn_readfirstlane(from[j]) * stride;
   }
-  u32x4 v[W];
+  const int64_t last = (int64_t)most * CPR;
+  for (int64_t c = (blockIdx.x - g2 * blocks) * 256 + tid; c < last; c += (int64_t)blocks * 256) {
+    const int row = (int)(c / CPR);
+    u32x4 *const x = x0 + c;
+    u32x4 v[W];
 #pragma unroll
-  for (int j = 0; j < W; ++j) v[j] = x[row < n[j] ? at[j] : at[0]];   // (any of the thread's own places where there is nothing to take)
+    for (int j = 0; j < W; ++j) v[j] = x[row < n[j] ? at[j] : at[0]];   // (any of the thread's own places where there is nothing to take)
 #pragma unroll
-  for (int j = 0; j < W; ++j)
-    if (row < n[j]) x[j * stride] = v[j];
+    for (int j = 0; j < W; ++j)
+      if (row < n[j]) x[j * stride] = v[j];
+  }
 }
 
 // A prompt's table rows and counts, likewise: a thread has one entry of all beams.
@@ -483,6 +489,10 @@ __global__ __launch_bounds__(256) void k_reorder_pages(ReorderArgs a) {
   const int64_t p = blockIdx.x;
   const int tid = threadIdx.x;
   if (tid == 0) most = 0;
+  if (tid < W) {
+    from[tid] = -1;
+    mine[tid] = keep[tid] = 0;     // entries given up, entries taken over
+  }
   if (tid < a.W) {
     const int64_t b = p * a.W + tid;
     const int par = a.parent[p * a.ld_parent + tid];
@@ -495,7 +505,6 @@ __global__ __launch_bounds__(256) void k_reorder_pages(ReorderArgs a) {
   if (tid < a.W) {
     const int64_t b = p * a.W + tid;
     const int f = from[tid];
-    mine[tid] = keep[tid] = 0;     // entries given up, entries taken over
     if (f >= 0) {
       mine[tid] = old_held[tid];
       keep[tid] = (int)min((int64_t)old_held[f], ((int64_t)max(old_pages[f], 0) + ((int64_t)1 << a.page_shift) - 1) >> a.page_shift);
@@ -509,16 +518,19 @@ __global__ __launch_bounds__(256) void k_reorder_pages(ReorderArgs a) {
   const int last = most;
   int32_t *const table = a.table + p * a.W * a.max_pages;
   for (int e = tid; e < last; e += 256) {
-    int old[W], now[W];
+    int old[W], now[W];   // (all loads under way at once)
 #pragma unroll
     for (int j = 0; j < W; ++j) {
-      if (j >= a.W) break;
-      old[j] = e < mine[j] ? table[(int64_t)j * a.max_pages + e] : -1;
-      now[j] = e < keep[j] ? table[(int64_t)from[j] * a.max_pages + e] : -1;
+      old[j] = table[(int64_t)min(j, a.W - 1) * a.max_pages + e];
+      now[j] = table[(int64_t)max(from[j], 0) * a.max_pages + e];
     }
 #pragma unroll
     for (int j = 0; j < W; ++j) {
-      if (j >= a.W) break;
+      old[j] = e < mine[j] ? old[j] : -1;
+      now[j] = e < keep[j] ? now[j] : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
       if (e >= max(mine[j], keep[j])) continue;
       if (now[j] != old[j]) {
         if (old[j] >= 0 && old[j] < a.n_pages) atomicAdd(a.refs + old[j], -1);
@@ -547,9 +559,10 @@ BeamPlan beam_plan(const BeamArgs &a) {
 template <int W>
 hipError_t reorder(int dtype, const ReorderArgs &a, hipStream_t st) {
   if (a.cap > 0) {
-    const int blocks = (int)((a.cap * (int64_t)(dtype == THK_F32 ? 32 : 16) + 255) / 256);
+    const int64_t groups = (int64_t)2 * a.L * a.prompts * a.N_kv, most = (a.cap * (int64_t)(dtype == THK_F32 ? 32 : 16) + 255) / 256;
+    const int blocks = (int)std::min(most, std::max<int64_t>(1, 16 * kCUs / groups));
     const hipError_t e = launch(dtype == THK_F32 ? (const void *)k_reorder_tails<THK_F32, W> : (const void *)k_reorder_tails<THK_BF16, W>,
-                                2 * a.L * a.prompts * a.N_kv * blocks, 256, st, a, blocks);
+                                groups * blocks, 256, st, a, blocks);
     if (e != hipSuccess) return e;
   }
   return launch((const void *)k_reorder_pages<W>, a.prompts, 256, st, a);
