@@ -41,15 +41,16 @@ __device__ __forceinline__ u32x4 packed(const float (&f)[Elem<DT>::VEC]) {
   return r;
 }
 
-// The chunks that a lane has of a row: chunks i and i + half / VEC, pair by pair, where the halves of what is turned are whole chunks (and
-// of the rest, and in the other forms, two neighbours).
+// How a row's pairs lie in its chunks of 16 bytes: in chunks i and i + half / VEC, where the halves of what is turned are whole chunks; inside
+// a chunk; anyhow.
 enum { kHalves = 0, kPairs = 1, kHalvesAny = 2 };
 constexpr int most_tokens(int form) { return form == kHalvesAny ? 8 : 32; }   // of a block: 8 or 16 KB of sines and cosines
 
 // A block has `tokens` tokens (of all layers) and `part` rows of each, a row in the hands of CPR / 2 lanes of a wave.  Its sines and
 // cosines are computed once, while the first rows are under way, and lie in LDS: a lane takes those of its VEC pairs for every row.  Rows are
 // asked for a pass ahead, and nothing in the loop waits for memory but they (a wait for a load is one for all stores in front of it too).
-// early: the first rows are asked for before it is known whether they go anywhere, which spares a short call a trip to memory.
+// The first rows are asked for before it is known whether they go anywhere, which spares a trip to memory, but for queries of which
+// few are kept (early: those too).
 // kHalvesAny has a sine and a cosine for each channel, and the channels' mates change places through LDS.
 template <int DT, int FORM>
 __global__ __launch_bounds__(kThreads, 6) void k_rope(RopeArgs a, int tokens, int part, int parts, int early) {
@@ -65,10 +66,10 @@ __global__ __launch_bounds__(kThreads, 6) void k_rope(RopeArgs a, int tokens, in
   const int r0 = (int)(blockIdx.x - group * parts) * part, rows = min(part, a.rows - r0);
   const int64_t t0 = group * tokens, all = a.L * a.n;
   const int here = (int)min((int64_t)tokens, all - t0), items = here * rows;
-  const int nq = a.q != nullptr ? a.N_q : 0, nk = a.k != nullptr ? a.N_kv : 0;
+  const int nv = a.v != nullptr ? a.N_kv : 0, nk = a.k != nullptr ? a.N_kv : 0;   // rows of a token: values, keys, queries
   const int p = tid % LANES;
-  const bool split = FORM == kHalves && p < half / VEC;
-  const int c0 = split ? p : 2 * p, c1 = split ? p + half / VEC : 2 * p + 1;
+  // (neighbouring lanes have neighbouring chunks in both loads and both stores)
+  const int c0 = FORM != kHalves || p < half / VEC ? p : p + half / VEC, c1 = FORM == kHalves && p < half / VEC ? p + half / VEC : p + LANES;
 
   struct Place { int tok, r; };   // token and row of what a lane has in the pass that begins at `first`
   auto place = [&](int first) {
@@ -76,14 +77,14 @@ __global__ __launch_bounds__(kThreads, 6) void k_rope(RopeArgs a, int tokens, in
     return Place{tok, r0 + i - tok * rows};
   };
   auto source = [&](const Place &w) {
-    const bool is_q = w.r < nq, turns = w.r < nq + nk;
-    const int h = is_q ? w.r : turns ? w.r - nq : w.r - nq - nk;
+    const bool is_q = w.r >= nv + nk, turns = w.r >= nv;
+    const int h = is_q ? w.r - nv - nk : turns ? w.r - nv : w.r;
     return (const u32x4 *)((const char *)(is_q ? a.q : turns ? a.k : a.v) + ((t0 + w.tok) * (is_q ? a.ld_q : turns ? a.ld_k : a.ld_v) + h * kD) * E::EB);
   };
   auto target = [&](const Place &w, int first) -> u32x4 * {   // nullptr: nowhere
     const i32x4 rec = records[w.tok];
-    const bool is_q = w.r < nq, turns = w.r < nq + nk;
-    const int h = is_q ? w.r : turns ? w.r - nq : w.r - nq - nk, seq = rec[0];
+    const bool is_q = w.r >= nv + nk, turns = w.r >= nv;
+    const int h = is_q ? w.r - nv - nk : turns ? w.r - nv : w.r, seq = rec[0];
     const int64_t t = t0 + w.tok, l = a.L == 1 ? 0 : t / a.n;
     const int64_t most = is_q ? a.q_rows : a.cap, row = is_q ? rec[3] : rec[2], heads = is_q ? a.N_q : a.N_kv;
     const bool packed_q = is_q && a.q_rows == 0;
@@ -98,14 +99,15 @@ __global__ __launch_bounds__(kThreads, 6) void k_rope(RopeArgs a, int tokens, in
   }
   Place now = place(0);
   u32x4 n0{}, n1{};
-  if (early) {
+  const bool sure = early || now.r < nv + nk || a.q_rows == 0;
+  if (sure) {
     const u32x4 *const x = source(now);
     n0 = ld_stream(x + c0);
     n1 = ld_stream(x + c1);
   }
   __syncthreads();
   u32x4 *to = target(now, 0);
-  if (!early && to != nullptr) {
+  if (!sure && to != nullptr) {
     const u32x4 *const x = source(now);
     n0 = ld_stream(x + c0);
     n1 = ld_stream(x + c1);
@@ -129,7 +131,7 @@ __global__ __launch_bounds__(kThreads, 6) void k_rope(RopeArgs a, int tokens, in
   for (int first = 0; first < items; first += ROWS) {
     u32x4 x0 = n0, x1 = n1, *const dst = to;
     const int tok = now.tok;
-    const bool turns = dst != nullptr && now.r < nq + nk;
+    const bool turns = dst != nullptr && now.r >= nv;
     if (first + ROWS < items) {
       now = place(first + ROWS);
       to = target(now, first + ROWS);
@@ -160,22 +162,21 @@ __global__ __launch_bounds__(kThreads, 6) void k_rope(RopeArgs a, int tokens, in
 #pragma unroll
         for (int u = 0; u < 4; ++u) x[u] = c + u * (VEC / 4) < a.rot ? z[u] : x[u];   // channels that are not turned keep their bits (rot is even: a word of two has both or neither)
       };
-      const int c = 2 * VEC * p;
-      give(x0, c);
-      give(x1, c + VEC);
+      give(x0, c0 * VEC);
+      give(x1, c1 * VEC);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      turn_chunk(x0, c);
+      turn_chunk(x0, c0 * VEC);
       __builtin_amdgcn_sched_barrier(0);   // (one chunk's operands in registers at a time)
-      turn_chunk(x1, c + VEC);
+      turn_chunk(x1, c1 * VEC);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-    } else if (turns && p * VEC < half) {
-      float f0[VEC], f1[VEC];
-      E::unpack(x0, f0);
-      E::unpack(x1, f1);
-      const float *const s = sn + tok * 64 + p * VEC, *const k = cs + tok * 64 + p * VEC;
-      if constexpr (FORM == kHalves) {
+    } else if constexpr (FORM == kHalves) {
+      if (turns && p * VEC < half) {
+        float f0[VEC], f1[VEC];
+        E::unpack(x0, f0);
+        E::unpack(x1, f1);
+        const float *const s = sn + tok * 64 + p * VEC, *const k = cs + tok * 64 + p * VEC;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
           const float x = f0[e], y = f1[e];
@@ -184,29 +185,25 @@ __global__ __launch_bounds__(kThreads, 6) void k_rope(RopeArgs a, int tokens, in
         }
         x0 = packed<DT>(f0);
         x1 = packed<DT>(f1);
-      } else {
-        const u32x4 was0 = x0, was1 = x1;
+      }
+    } else {
+      auto turn_chunk = [&](u32x4 &x, int c) {   // c: its first channel
+        if (!turns || c >= a.rot) return;
+        float f[VEC];
+        E::unpack(x, f);
+        const float *const s = sn + tok * 64 + c / 2, *const k = cs + tok * 64 + c / 2;
 #pragma unroll
         for (int e = 0; e < VEC; e += 2) {
-          const int h = e / 2, g = (VEC + e) / 2;   // pairs of the two chunks
-          float x = f0[e], y = f0[e + 1];
-          f0[e] = fmaf(x, k[h], -y * s[h]);
-          f0[e + 1] = fmaf(y, k[h], x * s[h]);
-          x = f1[e], y = f1[e + 1];
-          f1[e] = fmaf(x, k[g], -y * s[g]);
-          f1[e + 1] = fmaf(y, k[g], x * s[g]);
+          const float u = f[e], v = f[e + 1];
+          f[e] = fmaf(u, k[e / 2], -v * s[e / 2]);
+          f[e + 1] = fmaf(v, k[e / 2], u * s[e / 2]);
         }
-        x0 = packed<DT>(f0);
-        x1 = packed<DT>(f1);
-        if (p * VEC + VEC > half) {   // pairs behind the last one keep their bits
-          constexpr int per = VEC / 4;
+        const u32x4 z = packed<DT>(f);
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            if (2 * VEC * p + u * per >= a.rot) x0[u] = was0[u];
-            if (2 * VEC * p + VEC + u * per >= a.rot) x1[u] = was1[u];
-          }
-        }
-      }
+        for (int u = 0; u < 4; ++u) x[u] = c + u * (VEC / 4) < a.rot ? z[u] : x[u];   // pairs behind the last one keep their bits
+      };
+      turn_chunk(x0, c0 * VEC);
+      turn_chunk(x1, c1 * VEC);
     }
     if (dst != nullptr) {
       st_stream(dst + c0, x0);
