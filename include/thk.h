@@ -616,7 +616,7 @@ thk_status thk_paged_copy(const thk_shape *shape, const thk_pages *pages, const 
  * Beam search: of every prompt's W beams and V continuations of each the K best,
  *   score = scores[b][w] + (x[v] - max x) - ln sum exp(x - max x),   x = logits[b][w], rows of V, ld elements apart (0: V)
  * in descending order; equal ones by the lower beam and then the lower token.  (Continuations of one beam are in the order of their
- * logits, where the sums' 64 bits do not tell them apart.)  -inf in the logits rules a token out.  A beam with a score that is not
+ * logits also where the sums' 64 bits do not tell them apart.)  -inf in the logits rules a token out.  A beam with a score that is not
  * finite has no continuations, nor has one whose logits hold +inf or NaN, or nothing but -inf.  done (may be NULL): a beam with done != 0 has ended;
  * it goes on as it is, with token eos, its logits not looked at.
  *   parent, token [B][K]  the beam and the token of each; -1 where there are fewer than K

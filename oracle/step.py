@@ -110,7 +110,7 @@ def beam_select(x, scores, done, K, eos):
             if not np.isfinite(scores[b, w]):
                 continue
             if done[b, w]:
-                found.append((-scores[b, w], w, eos))
+                found.append((-scores[b, w], w, 0, eos))
                 continue
             row = x[b, w]
             top = row.max()
@@ -119,9 +119,9 @@ def beam_select(x, scores, done, K, eos):
             with np.errstate(divide="ignore"):
                 s = scores[b, w] + ((row - top) - math.log(np.exp(row - top).sum()))
             best = np.argsort(-row, kind="stable")[:K]   # by the logit, then by the token
-            found += [(-s[v], w, int(v)) for v in best if np.isfinite(s[v])]
+            found += [(-s[v], w, i, int(v)) for i, v in enumerate(best) if np.isfinite(s[v])]
         found = sorted(found)[:K]
-        rows = [(w, v, -s, int(v == eos or done[b, w] != 0)) for s, w, v in found]
+        rows = [(w, v, -s, int(v == eos or done[b, w] != 0)) for s, w, _, v in found]
         out.append(rows + [(-1, -1, -math.inf, 0)] * (K - len(rows)))
     return [np.array([[r[i] for r in rows] for rows in out]) for i in range(4)]
 

@@ -341,7 +341,7 @@ constexpr int kJoinWaves = 8;
 // A block joins a prompt: a wave for each row joins its pieces' lists and sums, then the rows' candidates are ranked by counting.
 __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int pieces) {
   __shared__ double score[kMostBeams * kMostContinuations];
-  __shared__ int at[kMostBeams * kMostContinuations];      // beam * 2^24 + token
+  __shared__ int at[kMostBeams * kMostContinuations];      // tokens; entry beam * K + place in the beam's list
   __shared__ double live_score[kMostBeams * kMostContinuations];
   __shared__ int live_at[kMostBeams * kMostContinuations];
   __shared__ double kth[kMostBeams];
@@ -393,7 +393,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
     }
     if (lane < a.K) {
       score[w * a.K + lane] = s;
-      at[w * a.K + lane] = w << 24 | token;
+      at[w * a.K + lane] = token;
       if (lane == a.K - 1) kth[w] = s;
     }
     if (lane == 0) ended[w] = end;
@@ -406,7 +406,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
     if (score[i] > -INFINITY && score[i] >= floor) {
       const int to = atomicAdd(&n_live, 1);
       live_score[to] = score[i];
-      live_at[to] = at[i];
+      live_at[to] = i;      // (equal scores: by the beam, then by its list, which is by logits and then tokens)
     }
   __syncthreads();
   const int n = n_live;
@@ -418,7 +418,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
     for (int j = 0; j < n; ++j) rank += live_score[j] > s || (live_score[j] == s && live_at[j] < mine);
     if (rank >= a.K) continue;
     const int64_t out = b * a.K + rank;
-    const int w = mine >> 24, token = mine & 0xffffff;
+    const int w = mine / a.K, token = at[mine];
     a.parent[out] = w;
     a.token[out] = token;
     a.score_out[out] = (float)s;

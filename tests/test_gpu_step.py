@@ -500,6 +500,16 @@ def test_beam_select_equal_values(dtype):
             check_select(x, zero, None, 40, 3)
 
 
+@pytest.mark.parametrize("K", [2, 3, 5, 8])
+def test_beam_select_logits_that_64_bits_do_not_tell_apart(K):
+    """Below 1e38 the scores of 5, 4 and 3 are one number: a beam's continuations are in the order of their logits all the same."""
+    x = torch.full((1, 3, 5000), float("-inf"), device="cuda")
+    for w in range(3):
+        x[0, w, 4000], x[0, w, 100 + w], x[0, w, 7], x[0, w, 4999] = 1e38, 5.0, 4.0, 3.0
+    x[0, 2, 8] = 4.0
+    check_select(x, np.array([[0.0, 0.25, -0.5]]), None, K, 1)
+
+
 def test_beam_select_orders_that_keep_the_list_busy():
     V = 70001
     up = torch.arange(V, dtype=torch.float32, device="cuda").div(1000).expand(1, 2, V).contiguous()
