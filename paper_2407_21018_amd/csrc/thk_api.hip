@@ -806,7 +806,7 @@ thk_status check_rope(const thk_rope *r) {
   if (r == nullptr) return THK_ERR_NULL;
   if (r->layout != THK_ROPE_HALVES && r->layout != THK_ROPE_PAIRS) return THK_ERR_UNSUPPORTED;
   if (r->scaling < THK_ROPE_PLAIN || r->scaling > THK_ROPE_BANDS) return THK_ERR_UNSUPPORTED;
-  if (r->rot < 2 || r->rot > kD || r->rot % 2 != 0 || !(r->base > 1) || !isfinite(r->base) || !isfinite(r->gain)) return THK_ERR_SHAPE;
+  if (r->rot < 2 || r->rot > kD || r->rot % 2 != 0 || !(r->base > 1) || !isfinite(r->base) || !isfinite((float)r->gain)) return THK_ERR_SHAPE;
   if (r->scaling == THK_ROPE_PLAIN) return THK_OK;
   if (!(r->factor > 0) || !isfinite(r->factor) || (r->scaling == THK_ROPE_BASE && r->rot < 4)) return THK_ERR_SHAPE;
   if (r->scaling >= THK_ROPE_RAMP && (r->trained < 1 || !(r->low > 0) || !(r->high > r->low) || !isfinite(r->high))) return THK_ERR_SHAPE;
@@ -1478,7 +1478,7 @@ thk_status thk_rope_turns(const thk_rope *r, uint64_t *turns) {
       w = w / f * (1 - g) + w * g;
     }
     const long double turn = w / (2 * pi);
-    turns[i] = (uint64_t)((turn - floorl(turn)) * 0x1p64L + 0.5L);   // (less than a turn: below 2^64)
+    turns[i] = (uint64_t)std::min((turn - floorl(turn)) * 0x1p64L + 0.5L, 0x1p64L - 1);   // (a turn less 2^-64 would be rounded up to 2^64)
   }
   return THK_OK;
 }

@@ -121,6 +121,21 @@ def test_rope_refusals():
     assert _rope(_shape(dtype=thk.THK_F32), ROPE, ld_q=1026) == 4
 
 
+def test_rope_gains_that_32_bits_do_not_hold():
+    for gain, want in ((1e39, 2), (-1e39, 2), (3e38, 0)):
+        r = thk.make_rope(0, 128, gain=gain)
+        assert _status(thk.thk_rope_turns, r) == want and _rope(_shape(), r, n_tokens=0) == want
+
+
+def test_turns_of_a_whole_turn_less_a_little():
+    """A factor that makes a speed as near to a whole turn as 64 bits tell: the table wraps or stays just below, never past its type."""
+    for ulps in range(-3, 4):
+        f = float(np.nextafter(1 / (2 * math.pi), 1)) * (1 + ulps * 2.0 ** -52)
+        got = thk.thk_rope_turns(thk.make_rope(0, 4, thk.THK_ROPE_LINEAR, factor=f))[0] % 2 ** 64
+        turn = Decimal(1) / Decimal(f) / (2 * Decimal("3.14159265358979323846264338327950288419716939937510582097494459")) * 2 ** 64
+        assert abs((turn - got + 2 ** 63) % 2 ** 64 - 2 ** 63) <= 20
+
+
 def test_no_tokens_and_no_moves_are_no_work():
     assert _rope(_shape(), ROPE, n_tokens=0, map=None) == 0
     assert _copy(_shape(), _pages(), n_moves=0, moves=None) == 0
