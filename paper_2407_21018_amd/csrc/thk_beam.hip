@@ -152,7 +152,8 @@ __device__ __forceinline__ uint32_t kth_of_lanes(const float *best, int lane, in
 // The largest of three, as the instruction itself: the library function first brings operands into canonical form.  (NaN are left out.)
 __device__ __forceinline__ float larger(float a, float b, float c) { float r; asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c)); return r; }
 
-// A lane's 32 elements of a tile are 16-byte chunks 64 apart.  Rows start anywhere (the loads are not aligned).  A chunk that ends behind the
+// A lane's 32 elements of a tile are 16-byte chunks 64 apart.  Rows start anywhere (the loads are not aligned), and are read once but
+// for little (non-temporal loads: 512 rows of 131072 bf16 30.7 -> 29.7 us).  A chunk that ends behind the
 // row's end is the row's last 16 bytes, of which what the chunk before it has counts as -inf.
 template <int DT>
 struct Tile {
@@ -162,9 +163,10 @@ struct Tile {
 
   static __device__ __forceinline__ int begin(int tile, int i, int lane) { return tile * kTileElems + (i * 64 + lane) * VEC; }
   static __device__ __forceinline__ int shifted(int V, int e) { return min(e, V - VEC); }
+  typedef uint32_t Chunk __attribute__((ext_vector_type(4), aligned(2)));
   __device__ __forceinline__ void load(const char *row, int V, int tile, int lane) {
 #pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) __builtin_memcpy(&raw[i], row + (int64_t)shifted(V, begin(tile, i, lane)) * E::EB, 16);
+    for (int i = 0; i < CHUNKS; ++i) raw[i] = __builtin_nontemporal_load((const Chunk *)(row + (int64_t)shifted(V, begin(tile, i, lane)) * E::EB));
   }
   // V < VEC: what the shifted chunk has of the row, whose other elements count as -inf anyway
   __device__ __forceinline__ void load_short(const char *row, int V) {
@@ -410,18 +412,36 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
     }
   __syncthreads();
   const int n = n_live;
-  for (int i = tid; i < n; i += kJoinWaves * 64) {
-    const double s = live_score[i];
-    const int mine = live_at[i];
-    int rank = 0;
-#pragma unroll 8
-    for (int j = 0; j < n; ++j) rank += live_score[j] > s || (live_score[j] == s && live_at[j] < mine);
-    if (rank >= a.K) continue;
-    const int64_t out = b * a.K + rank;
-    const int w = mine / a.K, token = at[mine];
+  // A wave ranks four candidates at a time, a lane of it compares them with its part of all (8 x 16 candidates a prompt, 64 prompts: 5.8 us;
+  // a candidate a lane, against all: 8.1).
+  for (int i0 = wave * 4; i0 < n; i0 += kJoinWaves * 4) {
+    double s[4];
+    int mine[4], rank[4] = {};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      s[u] = live_score[min(i0 + u, n - 1)];
+      mine[u] = live_at[min(i0 + u, n - 1)];
+    }
+    for (int j0 = 0; j0 < n; j0 += 64) {
+      const int j = min(j0 + lane, n - 1), y = live_at[j];
+      const double x = j0 + lane < n ? live_score[j] : -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) rank[u] += __popcll(__ballot(x > s[u] || (x == s[u] && y < mine[u])));
+    }
+    int r = rank[0], i = mine[0];
+    double score_of = s[0];
+#pragma unroll
+    for (int u = 1; u < 4; ++u) {
+      r = lane == u ? rank[u] : r;
+      i = lane == u ? mine[u] : i;
+      score_of = lane == u ? s[u] : score_of;
+    }
+    if (lane >= min(4, n - i0) || r >= a.K) continue;
+    const int64_t out = b * a.K + r;
+    const int w = i / a.K, token = at[i];
     a.parent[out] = w;
     a.token[out] = token;
-    a.score_out[out] = (float)s;
+    a.score_out[out] = (float)score_of;
     if (a.done_out != nullptr) a.done_out[out] = token == a.eos || ended[w] != 0;
   }
   for (int k = n + tid; k < a.K; k += kJoinWaves * 64) {
