@@ -172,16 +172,17 @@ __device__ __forceinline__ void settle(const ReserveArgs &a, int b, int64_t foun
 }
 
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
-constexpr int kPlanEach = 4, kPlanSequences = kPlanEach * kPlanThreads;   // sequences of a thread, and of a block, in LDS
+constexpr int kPlanEach = 4, kPlanSequences = kPlanEach * kPlanThreads;   // sequences of a thread, and of a block, in LDS, at most
 
 // Which of the pages that several use have to be replaced for whom: the growing users of a page meet in a table in LDS.
+template <int THREADS, int EACH>
 struct Meeting {
-  int page[2 * kPlanSequences], count[2 * kPlanSequences];   // as many slots are used as twice the sequences, up to a power of two
+  int page[2 * EACH * THREADS], count[2 * EACH * THREADS];   // as many slots are used as twice the sequences, up to a power of two
   uint32_t mask;
   __device__ __forceinline__ void clear(int B, int tid) {
     const uint32_t m = (2u << (32 - __builtin_clz(max(B - 1, 1)))) - 1;
     if (tid == 0) mask = m;
-    for (uint32_t i = tid; i <= m; i += kPlanThreads) {
+    for (uint32_t i = tid; i <= m; i += THREADS) {
       page[i] = -1;
       count[i] = 0;
     }
@@ -196,30 +197,31 @@ struct Meeting {
     return at & mask;
   }
 };
-template <bool MOVES> struct MeetingOf { Meeting m; };
-template <> struct MeetingOf<false> { };
+template <bool MOVES, int THREADS, int EACH> struct MeetingOf { Meeting<THREADS, EACH> m; };
+template <int THREADS, int EACH> struct MeetingOf<false, THREADS, EACH> { };
 
-constexpr int kStep = 8 * kPlanThreads;   // pages that a block looks at in a step
+constexpr int kPagesEach = 8;   // pages that a thread looks at in a step
+template <int THREADS, int EACH>
 struct PlanLds {
-  int start[kPlanSequences], have[kPlanSequences], from[kPlanSequences];
-  int64_t wave_total[2][kPlanWaves];
+  int start[EACH * THREADS], have[EACH * THREADS], from[EACH * THREADS];
+  int64_t wave_total[2][THREADS / 64];
   int total;
   union {
-    struct { int ending[kPlanSequences], held[kPlanSequences]; };
-    int pages[kStep];   // free ones, in order
+    struct { int ending[EACH * THREADS], held[EACH * THREADS]; };
+    int pages[kPagesEach * THREADS];   // free ones, in order
   };
 };
 
 // The block's sequences: what they give back (ONE), whose growing page is to be replaced, and their wishes in order.  Returns all wishes.
-template <bool ONE, bool MOVES>
-__device__ __forceinline__ int64_t plan_sequences(const ReserveArgs &a, PlanLds &s, MeetingOf<MOVES> &meeting, int (&want)[kPlanEach]) {
+template <bool ONE, bool MOVES, int THREADS, int EACH>
+__device__ __forceinline__ int64_t plan_sequences(const ReserveArgs &a, PlanLds<THREADS, EACH> &s, MeetingOf<MOVES, THREADS, EACH> &meeting, int (&want)[EACH]) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  int need[kPlanEach], have[kPlanEach], from[kPlanEach], held[kPlanEach];
+  int need[EACH], have[EACH], from[EACH], held[EACH];
   if (tid == 0) s.total = 0;
   if constexpr (MOVES) meeting.m.clear(a.B, tid);
 #pragma unroll
-  for (int i = 0; i < kPlanEach; ++i) {
-    const int b = i * kPlanThreads + tid;
+  for (int i = 0; i < EACH; ++i) {
+    const int b = i * THREADS + tid;
     need[i] = have[i] = held[i] = 0;
     from[i] = -1;
     if (b >= a.B) continue;
@@ -231,8 +233,8 @@ __device__ __forceinline__ int64_t plan_sequences(const ReserveArgs &a, PlanLds 
   __syncthreads();
   if constexpr (ONE) {
 #pragma unroll
-    for (int i = 0; i < kPlanEach; ++i) {
-      const int b = i * kPlanThreads + tid;
+    for (int i = 0; i < EACH; ++i) {
+      const int b = i * THREADS + tid;
       if (held[i] > need[i]) s.ending[atomicAdd(&s.total, 1)] = b;
       if (b < a.B) {
         s.have[b] = have[i];
@@ -240,46 +242,46 @@ __device__ __forceinline__ int64_t plan_sequences(const ReserveArgs &a, PlanLds 
       }
     }
     __syncthreads();
-    for (int i = wave; i < s.total; i += kPlanWaves) give_back(a, s.ending[i], s.have[s.ending[i]], s.held[s.ending[i]], lane);
+    for (int i = wave; i < s.total; i += (THREADS / 64)) give_back(a, s.ending[i], s.have[s.ending[i]], s.held[s.ending[i]], lane);
     if (s.total > 0) phase_end();
   }
   if constexpr (MOVES) {
-    Meeting &m = meeting.m;
-    int slot[kPlanEach], users[kPlanEach];
+    Meeting<THREADS, EACH> &m = meeting.m;
+    int slot[EACH], users[EACH];
 #pragma unroll
-    for (int i = 0; i < kPlanEach; ++i) {
+    for (int i = 0; i < EACH; ++i) {
       slot[i] = from[i] >= 0 ? m.enter(from[i]) : -1;
       users[i] = from[i] >= 0 ? refs_at(a.refs, from[i]) : 0;
     }
     __syncthreads();
-    bool all[kPlanEach];   // all users of the page grow: the first of them keeps it
+    bool all[EACH];   // all users of the page grow: the first of them keeps it
 #pragma unroll
-    for (int i = 0; i < kPlanEach; ++i) all[i] = slot[i] >= 0 && m.count[slot[i]] >= users[i];
+    for (int i = 0; i < EACH; ++i) all[i] = slot[i] >= 0 && m.count[slot[i]] >= users[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kPlanEach; ++i)
+    for (int i = 0; i < EACH; ++i)
       if (all[i]) m.count[slot[i]] = INT32_MAX;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kPlanEach; ++i)
-      if (all[i]) atomicMin(&m.count[slot[i]], i * kPlanThreads + tid);
+    for (int i = 0; i < EACH; ++i)
+      if (all[i]) atomicMin(&m.count[slot[i]], i * THREADS + tid);
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kPlanEach; ++i)
-      if (all[i] && m.count[slot[i]] == i * kPlanThreads + tid) from[i] = -1;
+    for (int i = 0; i < EACH; ++i)
+      if (all[i] && m.count[slot[i]] == i * THREADS + tid) from[i] = -1;
   }
   int64_t wanted = 0;
 #pragma unroll
-  for (int i = 0; i < kPlanEach; ++i) {
+  for (int i = 0; i < EACH; ++i) {
     want[i] = (from[i] >= 0) + need[i] - have[i];
-    if (i * kPlanThreads >= a.B) continue;
-    const int b = i * kPlanThreads + tid;
+    if (i * THREADS >= a.B) continue;
+    const int b = i * THREADS + tid;
     const WaveSum<uint32_t> w = wave_sum((uint32_t)want[i]);   // (fewer than 2^25 each)
     if (lane == 63) s.wave_total[i & 1][wave] = w.all;
     __syncthreads();
     int64_t before = wanted + w.before;
 #pragma unroll
-    for (int j = 0; j < kPlanWaves; ++j) {
+    for (int j = 0; j < (THREADS / 64); ++j) {
       const int64_t x = s.wave_total[i & 1][j];
       before += j < wave ? x : 0;
       wanted += x;
@@ -305,39 +307,42 @@ __device__ __forceinline__ int wisher(const int *start, int B, int64_t k) {
   return lo;
 }
 
-// Everything by one block: latency is all there is to it.
-template <bool MOVES>
-__global__ __launch_bounds__(kPlanThreads) void k_reserve_one(ReserveArgs a) {
-  constexpr int EACH = kStep / kPlanThreads;   // a wave's pages lie side by side
-  __shared__ PlanLds s;
-  __shared__ MeetingOf<MOVES> meeting;
+// Everything by one block: latency is all there is to it, of memory for few sequences and pages and of instructions otherwise, which sixteen
+// waves of a compute unit share.  A block of four waves takes 3.0 us for 4 sequences and 96 pages, one of sixteen 4.1; 64 sequences and 8000
+// pages 4.2 and 4.6, 64 and 16000 5.1 and 4.5, 200 and 4000 6.4 and 5.2.
+constexpr int kFew = 64, kFewPages = 8192;
+template <bool MOVES, int THREADS, int EACH>
+__global__ __launch_bounds__(THREADS) void k_reserve_one(ReserveArgs a) {
+  constexpr int PAGES = kPagesEach, kStep = PAGES * THREADS;   // a wave's pages lie side by side
+  __shared__ PlanLds<THREADS, EACH> s;
+  __shared__ MeetingOf<MOVES, THREADS, EACH> meeting;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  int want[kPlanEach];
-  const int64_t wanted = plan_sequences<true, MOVES>(a, s, meeting, want);
+  int want[EACH];
+  const int64_t wanted = plan_sequences<true, MOVES, THREADS, EACH>(a, s, meeting, want);
   // free pages in order: the one of rank k fulfils wish k
   int64_t found = 0;
-  int users[EACH];
+  int users[PAGES];
   auto look = [&](int64_t p0) {
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      const int64_t p = p0 + (wave * EACH + i) * 64 + lane;
+    for (int i = 0; i < PAGES; ++i) {
+      const int64_t p = p0 + (wave * PAGES + i) * 64 + lane;
       users[i] = refs_at(a.refs, min(p, a.n_pages - 1));   // (all loads under way at once)
     }
   };
   if (wanted > 0) look(0);
   for (int64_t p0 = 0, step = 0; p0 < a.n_pages && found < wanted; p0 += kStep, ++step) {
-    u64 free[EACH];
+    u64 free[PAGES];
     int mine = 0;
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-      free[i] = __ballot(users[i] <= 0 && p0 + (wave * EACH + i) * 64 + lane < a.n_pages);
+    for (int i = 0; i < PAGES; ++i) {
+      free[i] = __ballot(users[i] <= 0 && p0 + (wave * PAGES + i) * 64 + lane < a.n_pages);
       mine += __popcll(free[i]);
     }
     if (lane == 0) s.wave_total[step & 1][wave] = mine;
     __syncthreads();
     int k = 0, here = 0;
 #pragma unroll
-    for (int j = 0; j < kPlanWaves; ++j) {
+    for (int j = 0; j < THREADS / 64; ++j) {
       const int x = (int)s.wave_total[step & 1][j];
       k += j < wave ? x : 0;
       here += x;
@@ -345,21 +350,21 @@ __global__ __launch_bounds__(kPlanThreads) void k_reserve_one(ReserveArgs a) {
     if (found + here < wanted) look(p0 + kStep);
     const int most = (int)min((int64_t)here, wanted - found);
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
+    for (int i = 0; i < PAGES; ++i) {
       const int rank = k + __popcll(free[i] & ((1ull << lane) - 1));
       k += __popcll(free[i]);
-      if ((free[i] >> lane & 1) != 0 && rank < most) s.pages[rank] = (int)(p0 + (wave * EACH + i) * 64 + lane);
+      if ((free[i] >> lane & 1) != 0 && rank < most) s.pages[rank] = (int)(p0 + (wave * PAGES + i) * 64 + lane);
     }
     __syncthreads();
-    for (int r = tid; r < most; r += kPlanThreads) {
+    for (int r = tid; r < most; r += THREADS) {
       const int b = wisher(s.start, a.B, found + r);
       grant(a, b, found + r, s.start[b], s.have[b], s.from[b], s.pages[r]);
     }
     found += here;
   }
 #pragma unroll
-  for (int i = 0; i < kPlanEach; ++i) {
-    const int b = i * kPlanThreads + tid;
+  for (int i = 0; i < EACH; ++i) {
+    const int b = i * THREADS + tid;
     if (b < a.B) settle(a, b, found, s.start[b], s.have[b], s.from[b], want[i]);
   }
 }
@@ -400,12 +405,12 @@ __device__ __forceinline__ void chunk_pages(const ReserveArgs &a, int64_t p0, u6
 static_assert(kPlanThreads == kChunkThreads);
 template <bool MOVES>
 __global__ __launch_bounds__(kPlanThreads) void k_plan_and_count(ReserveArgs a, int64_t part) {
-  __shared__ PlanLds s;
-  __shared__ MeetingOf<MOVES> meeting;
+  __shared__ PlanLds<kPlanThreads, kPlanEach> s;
+  __shared__ MeetingOf<MOVES, kPlanThreads, kPlanEach> meeting;
   const ReserveWs w = reserve_ws(a.ws, a.B);
   if (blockIdx.x == 0) {
     int want[kPlanEach];
-    const int64_t wanted = plan_sequences<false, MOVES>(a, s, meeting, want);
+    const int64_t wanted = plan_sequences<false, MOVES, kPlanThreads, kPlanEach>(a, s, meeting, want);
     if (threadIdx.x == 0) *w.wanted = wanted;
 #pragma unroll
     for (int i = 0; i < kPlanEach; ++i) {
@@ -628,11 +633,19 @@ hipError_t launch_token_map(const TokenMapArgs &a, hipStream_t st) {
   return e != hipSuccess || a.n == 0 ? e : launch((const void *)k_token_map_of, blocks, kMapThreads, st, a);
 }
 
+template <int THREADS, int EACH>
+hipError_t launch_reserve_one(const ReserveArgs &a, hipStream_t st) {
+  return launch(a.now != nullptr ? (const void *)k_reserve_one<true, THREADS, EACH> : (const void *)k_reserve_one<false, THREADS, EACH>, 1, THREADS, st, a);
+}
+
 size_t reserve_ws_bytes(int64_t B) { return (size_t)B * sizeof(SequencePlan) + 16 + kMostChunks * sizeof(int32_t); }
 hipError_t launch_reserve(const ReserveArgs &a, hipStream_t st) {
   clear_stale_hip_error();
   if (a.B > kPlanSequences) return launch((const void *)k_reserve_many, 1, kPlanThreads, st, a);
-  if (a.n_pages <= kOnePages) return launch(a.now != nullptr ? (const void *)k_reserve_one<true> : (const void *)k_reserve_one<false>, 1, kPlanThreads, st, a);
+  if (a.n_pages <= kOnePages) {
+    if (a.B <= kFew && a.n_pages <= kFewPages) return launch_reserve_one<256, 1>(a, st);
+    return a.B <= kPlanThreads ? launch_reserve_one<kPlanThreads, 1>(a, st) : launch_reserve_one<kPlanThreads, kPlanEach>(a, st);
+  }
   const int64_t chunks = (a.n_pages + kChunk - 1) / kChunk, part = (chunks + kMostChunks - 1) / kMostChunks * kChunk, parts = (a.n_pages + part - 1) / part;
   hipError_t e = launch((const void *)k_give_back, (a.B + 3) / 4, 256, st, a);
   if (e == hipSuccess) e = launch(a.now != nullptr ? (const void *)k_plan_and_count<true> : (const void *)k_plan_and_count<false>, 1 + parts, kPlanThreads, st, a, part);
