@@ -50,10 +50,10 @@ constexpr int most_tokens(int form) { return form == kHalvesAny ? 8 : 32; }   //
 // cosines are computed once, while the first rows are under way, and lie in LDS: a lane takes those of its VEC pairs for every row.  Rows are
 // asked for a pass ahead, and nothing in the loop waits for memory but they (a wait for a load is one for all stores in front of it too).
 // The first rows are asked for before it is known whether they go anywhere, which spares a trip to memory, but for queries of which
-// few are kept (early: those too).
+// few are kept (early: those too).  pick: a block's keys and values come first, then the queries that are kept.
 // kHalvesAny has a sine and a cosine for each channel, and the channels' mates change places through LDS.
 template <int DT, int FORM>
-__global__ __launch_bounds__(kThreads, 6) void k_rope(RopeArgs a, int tokens, int part, int parts, int early) {
+__global__ __launch_bounds__(kThreads, 6) void k_rope(RopeArgs a, int tokens, int part, int parts, int early, int pick) {
   using E = Elem<DT>;
   constexpr int VEC = E::VEC, CPR = kD / VEC, LANES = CPR / 2, ROWS = kThreads / LANES;
   constexpr bool ANY = FORM == kHalvesAny;
@@ -61,31 +61,39 @@ __global__ __launch_bounds__(kThreads, 6) void k_rope(RopeArgs a, int tokens, in
   __shared__ __align__(16) float sn[most_tokens(FORM) * ANGLES], cs[most_tokens(FORM) * ANGLES];
   __shared__ __align__(16) float mates[ANY ? ROWS * LDR : 4];
   __shared__ i32x4 records[most_tokens(FORM)];
+  __shared__ int kept[most_tokens(FORM)], n_kept;   // pick: the tokens whose queries go somewhere
   const int tid = threadIdx.x, half = a.rot / 2;
   const int64_t group = blockIdx.x / (unsigned)parts;
   const int r0 = (int)(blockIdx.x - group * parts) * part, rows = min(part, a.rows - r0);
-  const int64_t t0 = group * tokens, all = a.L * a.n;
-  const int here = (int)min((int64_t)tokens, all - t0), items = here * rows;
+  // (pick: tokens as far apart as there are blocks, so that those whose queries are kept, a sequence's last, are spread over the blocks)
+  const int64_t all = a.L * a.n, apart = pick ? gridDim.x : 1, t0 = pick ? group : group * tokens;
+  const int here = (int)min((int64_t)tokens, (all - t0 + apart - 1) / apart);
   const int nv = a.v != nullptr ? a.N_kv : 0, nk = a.k != nullptr ? a.N_kv : 0;   // rows of a token: values, keys, queries
   const int p = tid % LANES;
   // (neighbouring lanes have neighbouring chunks in both loads and both stores)
   const int c0 = FORM != kHalves || p < half / VEC ? p : p + half / VEC, c1 = FORM == kHalves && p < half / VEC ? p + half / VEC : p + LANES;
 
   struct Place { int tok, r; };   // token and row of what a lane has in the pass that begins at `first`
+  const int others = here * (nv + nk);   // pick: these come first
+  int items = pick ? others : here * rows;
   auto place = [&](int first) {
-    const int i = min(first + tid / LANES, items - 1), tok = tokens == 1 ? 0 : i / rows;
-    return Place{tok, r0 + i - tok * rows};
+    int i = min(first + tid / LANES, items - 1);
+    const bool is_q = pick && i >= others;
+    const int each = pick ? is_q ? a.N_q : nv + nk : rows;
+    i -= is_q ? others : 0;
+    const int t = tokens == 1 ? 0 : i / each;
+    return Place{is_q ? kept[t] : t, r0 + i - t * each + (is_q ? nv + nk : 0)};
   };
   auto source = [&](const Place &w) {
     const bool is_q = w.r >= nv + nk, turns = w.r >= nv;
     const int h = is_q ? w.r - nv - nk : turns ? w.r - nv : w.r;
-    return (const u32x4 *)((const char *)(is_q ? a.q : turns ? a.k : a.v) + ((t0 + w.tok) * (is_q ? a.ld_q : turns ? a.ld_k : a.ld_v) + h * kD) * E::EB);
+    return (const u32x4 *)((const char *)(is_q ? a.q : turns ? a.k : a.v) + ((t0 + w.tok * apart) * (is_q ? a.ld_q : turns ? a.ld_k : a.ld_v) + h * kD) * E::EB);
   };
   auto target = [&](const Place &w, int first) -> u32x4 * {   // nullptr: nowhere
     const i32x4 rec = records[w.tok];
     const bool is_q = w.r >= nv + nk, turns = w.r >= nv;
     const int h = is_q ? w.r - nv - nk : turns ? w.r - nv : w.r, seq = rec[0];
-    const int64_t t = t0 + w.tok, l = a.L == 1 ? 0 : t / a.n;
+    const int64_t t = t0 + w.tok * apart, l = a.L == 1 ? 0 : t / a.n;
     const int64_t most = is_q ? a.q_rows : a.cap, row = is_q ? rec[3] : rec[2], heads = is_q ? a.N_q : a.N_kv;
     const bool packed_q = is_q && a.q_rows == 0;
     if (first + tid / LANES >= items || seq < 0 || seq >= a.B || (!packed_q && (row < 0 || row >= most))) return nullptr;
@@ -94,18 +102,29 @@ __global__ __launch_bounds__(kThreads, 6) void k_rope(RopeArgs a, int tokens, in
 
   const uint64_t turn = (tid & 63) < half ? a.turns[tid & 63] : 0;
   if (tid < here) {
-    const int64_t t = t0 + tid;
-    records[tid] = *(const i32x4 *)(a.map + (a.L == 1 ? t : t % a.n) * 4);
+    const int64_t t = t0 + tid * apart;
+    const i32x4 r = *(const i32x4 *)(a.map + (a.L == 1 ? t : t % a.n) * 4);
+    records[tid] = r;
+    if (pick) {   // (fewer tokens than a wave's lanes)
+      const bool keep = r[0] >= 0 && r[0] < a.B && r[3] >= 0 && r[3] < a.q_rows;
+      const unsigned long long m = __ballot(keep);
+      if (keep) kept[__popcll(m & ((1ull << tid) - 1))] = tid;
+      if (tid == 0) n_kept = __popcll(m);
+    }
   }
   Place now = place(0);
   u32x4 n0{}, n1{};
-  const bool sure = early || now.r < nv + nk || a.q_rows == 0;
+  const bool sure = pick ? tid / LANES < others : early || now.r < nv + nk || a.q_rows == 0;
   if (sure) {
     const u32x4 *const x = source(now);
     n0 = ld_stream(x + c0);
     n1 = ld_stream(x + c1);
   }
   __syncthreads();
+  if (pick) {
+    items = others + n_kept * a.N_q;
+    now = place(0);
+  }
   u32x4 *to = target(now, 0);
   if (!sure && to != nullptr) {
     const u32x4 *const x = source(now);
@@ -220,7 +239,9 @@ const void *kernel_of(int form) {
 }  // namespace
 
 // Large calls: all rows of some tokens a block.  Small ones, which would leave compute units without a block: the rows of one
-// pass.
+// pass.  Large ones that keep few of the queries (pick; as many as the buffers have rows for): a pass of the rows that go somewhere.
+// 2048 tokens of 32 + 16 rows bf16, 32 a sequence kept: 9.1 us, all rows a block 9.6 (a part of the head) and 9.2 (whole); 16384 tokens 30 and 41;
+// 49296 of 7 + 2 fp32: 25 and 47; 1950 of 160 + 80: 59 and 63.  With two passes a block 11, 33, 26 and 59.
 hipError_t launch_rope(int dtype, const RopeArgs &a, hipStream_t st) {
   clear_stale_hip_error();
   RopeArgs copy = a;
@@ -230,7 +251,13 @@ hipError_t launch_rope(int dtype, const RopeArgs &a, hipStream_t st) {
   const bool large = all >= 2 * kCUs;
   int tokens = large ? std::min(std::max(2 * pass / a.rows, 1), most_tokens(form)) : 1;
   int part = large ? a.rows : std::min(pass, a.rows), parts = (a.rows + part - 1) / part, early = all * a.rows <= 4 * pass * kCUs;
-  void *args[] = {&copy, &tokens, &part, &parts, &early};
+  const int64_t kv = ((a.k != nullptr) + (a.v != nullptr)) * (int64_t)a.N_kv, most_q = (int64_t)a.B * a.q_rows;
+  int pick = large && a.q != nullptr && kv > 0 && a.q_rows > 0 && most_q < a.n;
+  if (pick) {
+    const int64_t each = kv + a.N_q * most_q / a.n;   // rows of a token that go somewhere
+    tokens = (int)std::min<int64_t>(std::max<int64_t>((pass + each / 2) / each, 1), most_tokens(form));
+  }
+  void *args[] = {&copy, &tokens, &part, &parts, &early, &pick};
   return launch_main_kernel(dtype == THK_F32 ? kernel_of<THK_F32>(form) : kernel_of<THK_BF16>(form),
                             dim3((unsigned)((all + tokens - 1) / tokens * parts)), dim3(kThreads), args, 0, st);
 }

@@ -179,6 +179,41 @@ def test_rope_batches(dtype, L, B, N_q, N_kv, news, q_rows, cap, pad, joint):
         check_rope(Rope(dtype, pairs, rot), L, B, N_q, N_kv, news, pos0, row0, q_rows, cap, pad, joint=joint)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("L,B,N_q,N_kv,n,q_rows,share", [(1, 5, 6, 2, 900, 20, 1.0), (2, 3, 16, 4, 512, 7, 0.4), (1, 2, 1, 1, 4000, 3, 1.0), (3, 1, 40, 8, 200, 199, 1.0),
+                                                         (1, 1, 8, 1, 3000, 1, 0.0), (1, 7, 40, 40, 640, 90, 1.0)])
+def test_rope_queries_that_are_kept_lie_anywhere(dtype, L, B, N_q, N_kv, n, q_rows, share):
+    """A map of the caller's: of many tokens few queries have a place, in no order; rows likewise; some records are no tokens."""
+    print(f"rope {dtype} L={L} B={B} heads={N_q}/{N_kv} n={n} q_rows={q_rows}", flush=True)
+    rng = np.random.default_rng(n + q_rows)
+    cap = n // B + 5
+    places = rng.permutation(B * cap)[:n]
+    rec = np.stack([places // cap, rng.integers(0, 9000, n), places % cap, np.full(n, -1)], 1)
+    for b in range(B):
+        mine = rng.permutation(np.flatnonzero(rec[:, 0] == b))[:int(q_rows * share)]
+        rec[mine, 3] = rng.permutation(q_rows)[:len(mine)]
+    rec[rng.permutation(n)[:n // 20], 0] = rng.choice([-1, B, B + 7, -2 ** 31])
+    rec[rng.permutation(n)[:n // 20], 2] = rng.choice([-1, cap, 2 ** 31 - 1])
+    for pairs, rot in ((False, 128), (True, 96), (False, 44)):
+        r = Rope(dtype, pairs, rot)
+        g = torch.Generator(device="cuda").manual_seed(n)
+        q, k, v = torch.randn(L, n, (N_q + 2 * N_kv) * D, generator=g, device="cuda").to(TDT[dtype]).split([N_q * D, N_kv * D, N_kv * D], dim=2)
+        for parts in ((q, k, v), (q, None, v), (q, k, None), (q, None, None)):
+            after, before = gpu_rope(r, L, B, N_q, N_kv, *parts, ints(rec), q_rows, cap, ld=[x.stride(-2) if x is not None else 0 for x in parts])
+            for name, x, got, was, heads, col in zip("qkv", parts, after, before, (N_q, N_kv, N_kv), (3, 2, 2)):
+                if x is None:
+                    assert torch.equal(bits_of(got), bits_of(was))
+                    continue
+                for l in range(L):
+                    y = f64(x[l].reshape(n, heads, D)) if name == "v" else r.exact(x[l].reshape(n, heads, D), rec[:, 1])
+                    e = np.zeros_like(y) if name == "v" else r.bound(x[l].reshape(n, heads, D), y)
+                    e[..., r.rot:] = 0
+                    want, tol = f64(was[l]), np.zeros(was[l].shape)
+                    O.place(want, y, rec[:, 0], rec[:, col])
+                    O.place(tol, e, rec[:, 0], rec[:, col])
+                    assert (np.abs(f64(got[l]) - want) <= tol).all(), (name, l, rot)
+
+
 def test_rope_sines_of_far_positions():
     """(1, 0) turned is cosine and sine; positions over the whole range of 32 bits, the angle by whole numbers in the test too."""
     pos = np.concatenate([np.arange(-300, 300), [2 ** 31 - 1, -2 ** 31, 2 ** 30, 12345678, -87654321],
