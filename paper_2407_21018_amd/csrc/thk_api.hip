@@ -1547,7 +1547,7 @@ thk_status thk_paged_copy(const thk_shape *s, const thk_pages *p, const int32_t 
 }
 
 size_t thk_beam_workspace_bytes(const thk_beams *b) {
-  return check_beams(b) == THK_OK ? beam_ws_bytes(beam_args(b)) : 0;
+  return check_beams(b) == THK_OK ? beam_ws_bytes(b->dtype, beam_args(b)) : 0;
 }
 
 thk_status thk_beam_select(const thk_beams *b, const void *logits, const float *scores, const int32_t *done, int32_t *parent,
@@ -1559,7 +1559,7 @@ thk_status thk_beam_select(const thk_beams *b, const void *logits, const float *
   if (!aligned16(logits) || !aligned4(scores) || !aligned4(done) || !aligned4(parent) || !aligned4(token) || !aligned4(score_out) || !aligned4(done_out))
     return THK_ERR_ALIGN;
   BeamArgs a = beam_args(b);
-  const size_t need = beam_ws_bytes(a);
+  const size_t need = beam_ws_bytes(b->dtype, a);
   if (need == 0) return THK_ERR_SHAPE;
   if (ws == nullptr || !aligned16(ws) || ws_bytes < need) return THK_ERR_WORKSPACE;
   a.logits = logits; a.scores = scores; a.done = done; a.parent = parent; a.token = token; a.score_out = score_out; a.done_out = done_out; a.ws = ws;

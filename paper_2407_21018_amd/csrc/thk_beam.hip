@@ -102,6 +102,31 @@ __device__ __forceinline__ void wave_lds() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// A wave's 64 largest keys of all that it is given (of which K are wanted), in descending order, one a lane; keys wait in LDS (128 places) until there
+// are enough of them for the registers' sort.
+struct Best {
+  u64 *buffer;
+  u64 list, least;   // least: keys up to this are not among the K best, or are in the list
+  int n;             // keys that wait
+
+  __device__ __forceinline__ void flush(int K, int lane) {   // the last (up to) 64 of them
+    const int from = max(n - 64, 0);
+    wave_lds();
+    const u64 more = from + lane < n ? buffer[from + lane] : 0;
+    wave_lds();
+    n = from;
+    list = joined(list, sorted(more));
+    const u64 last = key_at(list, K - 1);
+    least = last > least ? last : least;
+  }
+  __device__ __forceinline__ void offer(u64 key, bool take, int K, int lane) {
+    const u64 m = __ballot(take);
+    if (take) buffer[n + __popcll(m & ((1ull << lane) - 1))] = key;
+    n += __popcll(m);
+    if (n >= 64) flush(K, lane);
+  }
+};
+
 // Joins the sums of all lanes, in an order that does not depend on the values.
 template <int J>
 __device__ __forceinline__ void join_step(float &t) { t = fmaxf(t, __uint_as_float(lane_across<J>(__float_as_uint(t)))); }
@@ -266,22 +291,9 @@ __global__ __launch_bounds__(kWaves * 64, DT == THK_F32 ? 3 : 4) void k_beam_pie
   __syncthreads();
 
   // the list
-  u64 *const buffer = waiting[wave];
-  u64 list = 0;
   const uint32_t kth = kth_of_lanes(lane_best, lane, a.K);
-  u64 least = kth != 0 ? ((u64)kth << 32) - 1 : 0;      // keys up to this are not among the K best, or are in the list
+  Best best_keys = {waiting[wave], 0, kth != 0 ? ((u64)kth << 32) - 1 : 0, 0};
   const float least_value = kth != 0 ? value_of((u64)kth << 32) : kLeast;
-  int n = 0;                                            // keys that wait for their way into the list
-  auto flush = [&]() {                                  // the last (up to) 64 of them
-    const int from = max(n - 64, 0);
-    wave_lds();
-    const u64 more = from + lane < n ? buffer[from + lane] : 0;
-    wave_lds();
-    n = from;
-    list = joined(list, sorted(more));
-    const u64 last_of_k = key_at(list, a.K - 1);
-    least = last_of_k > least ? last_of_k : least;
-  };
   int found = 0;
   for (int t0 = 0; t0 < last - first; t0 += 4) {
 #pragma unroll
@@ -307,17 +319,13 @@ __global__ __launch_bounds__(kWaves * 64, DT == THK_F32 ? 3 : 4) void k_beam_pie
 #pragma unroll
     for (int u = 0; u < kLooks; ++u) {
       const u64 key = key_of(y[u], (uint32_t)where[u]);
-      const bool take = where[u] >= 0 && y[u] >= kLeast && y[u] < INFINITY && key > least;
-      const u64 m = __ballot(take);
-      if (take) buffer[n + __popcll(m & ((1ull << lane) - 1))] = key;
-      n += __popcll(m);
-      if (n >= 64) flush();
+      best_keys.offer(key, where[u] >= 0 && y[u] >= kLeast && y[u] < INFINITY && key > best_keys.least, a.K, lane);
     }
   }
   wave_lds();
 #pragma unroll
   for (int part = 0; part < 2; ++part) {   // the waves' keys together
-    const u64 key = part == 0 ? (lane < n ? buffer[lane] : 0) : (lane < a.K ? list : 0);
+    const u64 key = part == 0 ? (lane < best_keys.n ? best_keys.buffer[lane] : 0) : (lane < a.K ? best_keys.list : 0);
     const u64 m = __ballot(key != 0);
     if (m == 0) continue;
     int base = lane == 0 ? atomicAdd(&n_keys, __popcll(m)) : 0;
@@ -332,17 +340,20 @@ __global__ __launch_bounds__(kWaves * 64, DT == THK_F32 ? 3 : 4) void k_beam_pie
   }
   if (wave != 0) return;
   const int total = n_keys;
-  list = sorted(lane < total ? all_keys[lane] : 0);
+  u64 list = sorted(lane < total ? all_keys[lane] : 0);
   for (int i = 64; i < total; i += 64) list = joined(list, sorted(i + lane < total ? all_keys[i + lane] : 0));
   u64 *const out = (u64 *)((PieceStats *)a.ws + (int64_t)a.B * a.W * pieces) + (int64_t)blockIdx.x * a.K;
   if (lane < a.K) out[lane] = list;
 }
 
-constexpr int kJoinWaves = 8;
 
-// A block joins a prompt: a wave for each row joins its pieces' lists and sums, then the rows' candidates are ranked by counting.
-__global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int pieces) {
+// A block of eight waves, or sixteen where that spares them rows (32 beams, the best 64 of 149134 tokens: 51 -> 41 us), joins a prompt: a wave for
+// each row joins its pieces' lists and sums, then the rows' candidates are ranked by counting.
+constexpr int join_waves(int W) { return W <= 8 ? 8 : 16; }
+template <int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void k_beam_join(BeamArgs a, int pieces) {
   __shared__ double score[kMostBeams * kMostContinuations];
+  __shared__ u64 waiting[WAVES][128];
   __shared__ int at[kMostBeams * kMostContinuations];      // tokens; entry beam * K + place in the beam's list
   __shared__ double live_score[kMostBeams * kMostContinuations];
   __shared__ int live_at[kMostBeams * kMostContinuations];
@@ -354,7 +365,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
   const PieceStats *const stats = (const PieceStats *)a.ws;
   if (tid == 0) n_live = 0;
   const int count = pieces * a.K;
-  for (int w = wave; w < a.W; w += kJoinWaves) {
+  for (int w = wave; w < a.W; w += WAVES) {
     const int64_t row = b * a.W + w;
     const float before = a.scores[row];
     const bool end = a.done != nullptr && a.done[row] != 0;
@@ -375,17 +386,17 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
         x.sum = (x.sum != 0 ? x.sum * exp((double)x.at - (double)to) : 0) + (y.sum != 0 ? y.sum * exp((double)y.at - (double)to) : 0);
         x.at = to;
       }
-      u64 list = sorted(more);
+      Best best_keys = {waiting[wave], sorted(more), 0, 0};
+      best_keys.least = key_at(best_keys.list, a.K - 1);
       for (int i = 64; i < count; i += 4 * 64) {
         u64 four[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) four[u] = keys[min(i + u * 64 + lane, count - 1)];   // (all under way at once)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          more = i + u * 64 + lane < count ? four[u] : 0;
-          if (__ballot(more > key_at(list, a.K - 1)) != 0) list = joined(list, sorted(more));
-        }
+        for (int u = 0; u < 4; ++u) best_keys.offer(four[u], i + u * 64 + lane < count && four[u] > best_keys.least, a.K, lane);
       }
+      if (best_keys.n > 0) best_keys.flush(a.K, lane);
+      const u64 list = best_keys.list;
       join_sums(x.at, x.sum);
       if (list != 0 && lane < a.K) {   // (a sum that is NaN leaves no score)
         s = (double)before + (((double)value_of(list) - (double)x.at) - log(x.sum));
@@ -404,7 +415,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
   // what is below the K-th of one row is not among the K best of all
   double floor = -INFINITY;
   for (int w = 0; w < a.W; ++w) floor = fmax(floor, kth[w]);
-  for (int i = tid; i < a.W * a.K; i += kJoinWaves * 64)
+  for (int i = tid; i < a.W * a.K; i += WAVES * 64)
     if (score[i] > -INFINITY && score[i] >= floor) {
       const int to = atomicAdd(&n_live, 1);
       live_score[to] = score[i];
@@ -414,7 +425,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
   const int n = n_live;
   // A wave ranks four candidates at a time, a lane of it compares them with its part of all (8 x 16 candidates a prompt, 64 prompts: 5.8 us;
   // a candidate a lane, against all: 8.1).
-  for (int i0 = wave * 4; i0 < n; i0 += kJoinWaves * 4) {
+  for (int i0 = wave * 4; i0 < n; i0 += WAVES * 4) {
     double s[4];
     int mine[4], rank[4] = {};
 #pragma unroll
@@ -444,7 +455,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void k_beam_join(BeamArgs a, int p
     a.score_out[out] = (float)score_of;
     if (a.done_out != nullptr) a.done_out[out] = token == a.eos || ended[w] != 0;
   }
-  for (int k = n + tid; k < a.K; k += kJoinWaves * 64) {
+  for (int k = n + tid; k < a.K; k += WAVES * 64) {
     const int64_t out = b * a.K + k;
     a.parent[out] = -1;
     a.token[out] = -1;
@@ -567,13 +578,29 @@ hipError_t launch(const void *k, int64_t blocks, int threads, hipStream_t st, A.
   return launch_main_kernel(k, dim3((unsigned)blocks), dim3(threads), args, 0, st);
 }
 
+// Into how many pieces a row is cut, by an estimate in half microseconds, fitted to 180 measured calls of 2 to 205 MB (off by a tenth of the time): a tile
+// of every wave takes the k blocks of a compute unit 0.5 us (fp32: 1) k and 0.25, the rest 0.9 us k, in as many rounds as there are of
+// blocks that fit; the join takes a wave 0.35 us for 64 keys.  512 rows of 131072 bf16: 36.6 us with one piece, 35.8 two, 38.6 four, 44.7
+// eight; 184 of 208660: 25.3 two, 24.1 four, 26.3 five, 28.1 six; 76 of 106494 fp32: 17.1 two, 15.4 three, 16.0 seven; 4 of 32768
+// bf16: 10.4 four, 10.8 two, 12.1 one.
 struct BeamPlan { int pieces, tiles_each; };
-// As many blocks as are on the card at once, four on a compute unit; but two tiles a wave where there are more than one for every wave of a block a
-// compute unit (35 rows of 100003 fp32 logits: 7.7 us, one tile 9.2, four 10.0; 512 rows of 131072 bf16: 56, 39, 35, 32 and 33 us with 1 to 16).
-BeamPlan beam_plan(const BeamArgs &a) {
-  const int64_t tiles = ((int64_t)a.V + kTileElems - 1) / kTileElems, waves = kCUs * kWaves, n = (int64_t)a.B * a.W * tiles;
-  const int64_t each = std::min<int64_t>(std::max<int64_t>(n > waves ? 2 : 1, (n + 4 * waves - 1) / (4 * waves)), kMostTiles);
-  return {(int)((tiles + each * kWaves - 1) / (each * kWaves)), (int)each};
+BeamPlan beam_plan(int dtype, const BeamArgs &a) {
+  const int64_t tiles = ((int64_t)a.V + kTileElems - 1) / kTileElems, rows = (int64_t)a.B * a.W;
+  const int64_t fit = dtype == THK_F32 ? 3 : 4, tile = dtype == THK_F32 ? 2 : 1;   // blocks of a compute unit
+  BeamPlan best{};
+  double least = 0;
+  for (int64_t each = 1; each <= kMostTiles; ++each) {
+    const int64_t pieces = (tiles + each * kWaves - 1) / (each * kWaves);
+    if (pieces == best.pieces) continue;   // (as many with fewer tiles)
+    auto round = [&](int64_t k) { return k == 0 ? 0. : each * (tile * k + 0.5) + 1.8 * k; };
+    const int64_t k = (rows * pieces + kCUs - 1) / kCUs, of_a_wave = (a.W + join_waves(a.W) - 1) / join_waves(a.W);
+    const double t = k / fit * round(fit) + round(k % fit) + 0.7 / 64 * pieces * a.K * of_a_wave;
+    if (best.pieces == 0 || t < least) {
+      least = t;
+      best = {(int)pieces, (int)each};
+    }
+  }
+  return best;
 }
 
 template <int W>
@@ -590,17 +617,18 @@ hipError_t reorder(int dtype, const ReorderArgs &a, hipStream_t st) {
 
 }  // namespace
 
-size_t beam_ws_bytes(const BeamArgs &a) {
-  const int64_t pieces = beam_plan(a).pieces, blocks = (int64_t)a.B * a.W * pieces;
-  return blocks * kWaves * 64 > 0xffffffffll || (int64_t)a.B * kJoinWaves * 64 > 0xffffffffll ? 0 : (size_t)blocks * (sizeof(PieceStats) + a.K * sizeof(u64));
+size_t beam_ws_bytes(int dtype, const BeamArgs &a) {
+  const int64_t pieces = beam_plan(dtype, a).pieces, blocks = (int64_t)a.B * a.W * pieces;
+  return blocks * kWaves * 64 > 0xffffffffll || (int64_t)a.B * 1024 > 0xffffffffll ? 0 : (size_t)blocks * (sizeof(PieceStats) + a.K * sizeof(u64));
 }
 
 hipError_t launch_beam_select(int dtype, const BeamArgs &a, hipStream_t st) {
   clear_stale_hip_error();
-  const BeamPlan p = beam_plan(a);
+  const BeamPlan p = beam_plan(dtype, a);
   const hipError_t e = launch(dtype == THK_F32 ? (const void *)k_beam_pieces<THK_F32> : (const void *)k_beam_pieces<THK_BF16>, (int64_t)a.B * a.W * p.pieces,
                               kWaves * 64, st, a, p.pieces, p.tiles_each);
-  return e != hipSuccess ? e : launch((const void *)k_beam_join, a.B, kJoinWaves * 64, st, a, p.pieces);
+  if (e != hipSuccess) return e;
+  return launch(join_waves(a.W) == 8 ? (const void *)k_beam_join<8> : (const void *)k_beam_join<16>, a.B, join_waves(a.W) * 64, st, a, p.pieces);
 }
 
 hipError_t launch_reorder(int dtype, const ReorderArgs &a, hipStream_t st) {

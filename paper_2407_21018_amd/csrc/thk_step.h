@@ -58,7 +58,7 @@ struct BeamArgs {
   int64_t ld;
   int32_t B, W, K, V, eos;
 };
-size_t beam_ws_bytes(const BeamArgs &a);   // 0: a launch would be too large
+size_t beam_ws_bytes(int dtype, const BeamArgs &a);   // 0: a launch would be too large
 hipError_t launch_beam_select(int dtype, const BeamArgs &a, hipStream_t st);
 
 struct ReorderArgs {
