@@ -390,6 +390,32 @@ def test_reserve_after_sharing(B, W, n_pages, max_pages):
     books.reserve(rows, now)      # everybody has a page of their own now
 
 
+@pytest.mark.parametrize("B,n_pages", [(64, 8192), (64, 8193), (65, 8192), (65, 500), (1024, 20000), (1025, 20000), (1024, 65536), (64, 65537), (4096, 65536), (4097, 30000)])
+def test_reserve_at_the_limits_of_its_forms(B, n_pages):
+    """Each way in which the call is laid out, at its last size and one past it; runs of sequences share the page that they grow in."""
+    print(f"reserve B={B} n_pages={n_pages}", flush=True)
+    rng = np.random.default_rng(B + n_pages)
+    pr, most = 128, max(2, min(40, n_pages // B - 2))
+    refs, order, at = [0] * n_pages, rng.permutation(n_pages).tolist(), 0
+    held, table, now = [], [], []
+    for b in range(B):
+        n = int(rng.integers(0, most * pr))
+        pages, at = order[at:at + -(-n // pr)], at + -(-n // pr)
+        if b and rng.random() < 0.4:
+            n, pages, at = now[b - 1], table[b - 1][:held[b - 1]], at - len(pages)
+        for p in pages:
+            refs[p] += 1
+        held.append(len(pages))
+        now.append(n)
+        table.append(pages + [-1] * (most + 1 - len(pages)))
+    books = Books(B, pr, most + 1, n_pages, held, table, refs)
+    rows = [max(0, n + int(rng.choice([0, 1, 1, 64, pr, -n, -pr]))) for n in now]
+    books.reserve(rows, now)
+    books.reserve(rows, None)
+    room = books.room.tolist()
+    books.reserve([n + int(rng.choice([0, 1, pr])) for n in rows], [min(n, r) for n, r in zip(rows, room)])
+
+
 @pytest.mark.parametrize("dtype,bits,T,page_rows", [("bf16", 4, 64, 256), ("bf16", 0, 51, 128), ("f32", 8, 33, 64), ("f32", 0, 128, 1024), ("bf16", 8, 1, 4096)])
 def test_paged_copy(dtype, bits, T, page_rows):
     L, N, n = 3, 2, 9
@@ -466,6 +492,25 @@ def test_beam_select(dtype, B, W, K, V):
     x, s = logits(rng, B, W, V, dtype), -10 * rng.random((B, W))
     check_select(x, s, None, K, -1)
     check_select(x, s, rng.random((B, W)) < 0.4, K, V // 2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,W,K,V", [(64, 8, 16, 65001), (30, 8, 8, 131073), (64, 16, 16, 40000), (64, 4, 8, 32000), (23, 8, 8, 208660), (300, 32, 5, 7000), (1, 32, 64, 150001), (1, 9, 33, 70001)])
+def test_beam_select_large_calls(dtype, B, W, K, V):
+    """Rows in few pieces of many tiles, blocks in several rounds: two prompts against the oracle, the others are the same two."""
+    print(f"beam {dtype} B={B} W={W} K={K} V={V}", flush=True)
+    rng = np.random.default_rng(V + W)
+    P = min(B, 2)
+    x, s = logits(rng, P, W, V, dtype), (-10 * rng.random((P, W))).astype(np.float32)
+    check_select(x, s, None, K, -1)
+    want = gpu_select(x, s, None, K, -1)
+    which = np.arange(B) % P
+    got = gpu_select(x[torch.tensor(which).cuda()].contiguous(), s[which], None, K, -1)
+    for name, g, w in zip(("parent", "token", "score", "done"), got, want):
+        if name != "score":
+            assert np.array_equal(g, w[which]), name
+        else:      # another number of pieces, another order of the same sum
+            assert (np.abs(g.astype(np.float64) - w[which]) <= 2 * sum_error(V) + 2.0 ** -23 * np.abs(w[which])).all()
 
 
 def test_beam_select_many_rows():
