@@ -312,14 +312,14 @@ __device__ __forceinline__ int wisher(const int *start, int B, int64_t k) {
 // waves of a compute unit share.  A block of four waves takes 3.0 us for 4 sequences and 96 pages, one of sixteen 4.1; 64 sequences and 8000
 // pages 4.2 and 4.6, 64 and 16000 5.1 and 4.5, 200 and 4000 6.4 and 5.2.
 constexpr int kFew = 64, kFewPages = 8192;
-template <bool MOVES, int THREADS, int EACH>
+template <bool MOVES, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_reserve_one(ReserveArgs a) {
   constexpr int PAGES = kPagesEach, kStep = PAGES * THREADS;   // a wave's pages lie side by side
-  __shared__ PlanLds<THREADS, EACH> s;
-  __shared__ MeetingOf<MOVES, THREADS, EACH> meeting;
+  __shared__ PlanLds<THREADS, 1> s;
+  __shared__ MeetingOf<MOVES, THREADS, 1> meeting;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  int want[EACH];
-  const int64_t wanted = plan_sequences<true, MOVES, THREADS, EACH>(a, s, meeting, want);
+  int want[1];
+  const int64_t wanted = plan_sequences<true, MOVES, THREADS, 1>(a, s, meeting, want);
   // free pages in order: the one of rank k fulfils wish k
   int64_t found = 0;
   int users[PAGES];
@@ -363,16 +363,13 @@ __global__ __launch_bounds__(THREADS) void k_reserve_one(ReserveArgs a) {
     }
     found += here;
   }
-#pragma unroll
-  for (int i = 0; i < EACH; ++i) {
-    const int b = i * THREADS + tid;
-    if (b < a.B) settle(a, b, found, s.start[b], s.have[b], s.from[b], want[i]);
-  }
+  if (tid < a.B) settle(a, tid, found, s.start[tid], s.have[tid], s.from[tid], want[0]);
 }
 
-// Pools of more pages than this: three launches, which take a pool of 400000 pages and 1024 sequences 15 us together; a block alone, which looks at
-// 8192 pages in about a microsecond, takes 256 sequences 10 us at 65536 pages.
-constexpr int64_t kOnePages = 65536;
+constexpr int64_t kOnePages = 49152;
+// More sequences than that block has threads, or pages than this: three launches, which cost 9 us and for many sequences grow more slowly (16 sequences
+// and 48000 pages 6.6 us by one block, 8.7 by three launches; 65536 pages 8.8 and 8.8; 1024 sequences and 16000 pages 9.3 and 10.2, 24000 pages 10.5 and
+// 10.0; 2000 sequences, two a thread, and 16000 pages 16.3 and 12.3; 4096 and 16000 26 and 16.6).
 // What is given back, by a wave for each sequence; the sequences' plan, by one block, and the free pages counted beside it; the pages given out.
 constexpr int kChunk = 4096, kChunkThreads = 1024, kChunkWaves = kChunkThreads / 64, kChunkEach = kChunk / kChunkThreads;   // pages that a block looks at together: its part of the pool is as many of them as make
 constexpr int kMostChunks = 1024;   // at most so many parts
@@ -637,19 +634,17 @@ hipError_t launch_token_map(const TokenMapArgs &a, hipStream_t st) {
   return e != hipSuccess || a.n == 0 ? e : launch((const void *)k_token_map_of, blocks, kMapThreads, st, a);
 }
 
-template <int THREADS, int EACH>
+template <int THREADS>
 hipError_t launch_reserve_one(const ReserveArgs &a, hipStream_t st) {
-  return launch(a.now != nullptr ? (const void *)k_reserve_one<true, THREADS, EACH> : (const void *)k_reserve_one<false, THREADS, EACH>, 1, THREADS, st, a);
+  return launch(a.now != nullptr ? (const void *)k_reserve_one<true, THREADS> : (const void *)k_reserve_one<false, THREADS>, 1, THREADS, st, a);
 }
 
 size_t reserve_ws_bytes(int64_t B) { return (size_t)B * sizeof(SequencePlan) + 16 + kMostChunks * sizeof(int32_t); }
 hipError_t launch_reserve(const ReserveArgs &a, hipStream_t st) {
   clear_stale_hip_error();
   if (a.B > kPlanSequences) return launch((const void *)k_reserve_many, 1, kPlanThreads, st, a);
-  if (a.n_pages <= kOnePages) {
-    if (a.B <= kFew && a.n_pages <= kFewPages) return launch_reserve_one<256, 1>(a, st);
-    return a.B <= kPlanThreads ? launch_reserve_one<kPlanThreads, 1>(a, st) : launch_reserve_one<kPlanThreads, kPlanEach>(a, st);
-  }
+  if (a.B <= kFew && a.n_pages <= kFewPages) return launch_reserve_one<256>(a, st);
+  if (a.B <= kPlanThreads && a.n_pages <= kOnePages) return launch_reserve_one<kPlanThreads>(a, st);
   const int64_t chunks = (a.n_pages + kChunk - 1) / kChunk, part = (chunks + kMostChunks - 1) / kMostChunks * kChunk, parts = (a.n_pages + part - 1) / part;
   hipError_t e = launch((const void *)k_give_back, (a.B + 3) / 4, 256, st, a);
   if (e == hipSuccess) e = launch(a.now != nullptr ? (const void *)k_plan_and_count<true> : (const void *)k_plan_and_count<false>, 1 + parts, kPlanThreads, st, a, part);

@@ -390,7 +390,7 @@ def test_reserve_after_sharing(B, W, n_pages, max_pages):
     books.reserve(rows, now)      # everybody has a page of their own now
 
 
-@pytest.mark.parametrize("B,n_pages", [(64, 8192), (64, 8193), (65, 8192), (65, 500), (1024, 20000), (1025, 20000), (1024, 65536), (64, 65537), (4096, 65536), (4097, 30000)])
+@pytest.mark.parametrize("B,n_pages", [(64, 8192), (64, 8193), (65, 8192), (65, 500), (1024, 20000), (1025, 20000), (1024, 49152), (1024, 49153), (64, 49152), (64, 49153), (1500, 3000), (4096, 65536), (4097, 30000)])
 def test_reserve_at_the_limits_of_its_forms(B, n_pages):
     """Each way in which the call is laid out, at its last size and one past it; runs of sequences share the page that they grow in."""
     print(f"reserve B={B} n_pages={n_pages}", flush=True)
