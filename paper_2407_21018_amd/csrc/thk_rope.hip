@@ -239,7 +239,7 @@ const void *kernel_of(int form) {
 }  // namespace
 
 // Large calls: all rows of some tokens a block.  Small ones, which would leave compute units without a block: the rows of one
-// pass.  Large ones that keep few of the queries (pick; as many as the buffers have rows for): a pass of the rows that go somewhere.
+// pass.  Large ones that keep a third of the queries at most (pick; of a half it gains nothing): a pass of the rows that go somewhere.
 // 2048 tokens of 32 + 16 rows bf16, 32 a sequence kept: 9.1 us, all rows a block 9.6 (a part of the head) and 9.2 (whole); 16384 tokens 30 and 41;
 // 49296 of 7 + 2 fp32: 25 and 47; 1950 of 160 + 80: 59 and 63.  With two passes a block 11, 33, 26 and 59.
 hipError_t launch_rope(int dtype, const RopeArgs &a, hipStream_t st) {
@@ -252,7 +252,7 @@ hipError_t launch_rope(int dtype, const RopeArgs &a, hipStream_t st) {
   int tokens = large ? std::min(std::max(2 * pass / a.rows, 1), most_tokens(form)) : 1;
   int part = large ? a.rows : std::min(pass, a.rows), parts = (a.rows + part - 1) / part, early = all * a.rows <= 4 * pass * kCUs;
   const int64_t kv = ((a.k != nullptr) + (a.v != nullptr)) * (int64_t)a.N_kv, most_q = (int64_t)a.B * a.q_rows;
-  int pick = large && a.q != nullptr && kv > 0 && a.q_rows > 0 && most_q < a.n;
+  int pick = large && a.q != nullptr && kv > 0 && a.q_rows > 0 && 3 * most_q <= a.n;
   if (pick) {
     const int64_t each = kv + a.N_q * most_q / a.n;   // rows of a token that go somewhere
     tokens = (int)std::min<int64_t>(std::max<int64_t>((pass + each / 2) / each, 1), most_tokens(form));
