@@ -810,6 +810,54 @@ def test_a_captured_step_is_the_eager_one():
                 assert torch.equal(bits_of(a), bits_of(b)), t
 
 
+def test_steps_on_other_streams_side_by_side():
+    """Two servers, each on a stream of its own and not waiting for the other, and one on the current stream: identical bits."""
+    servers = [Server(70, seed=5, bits=4) for _ in range(3)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream(), torch.cuda.current_stream()]
+    torch.cuda.synchronize()
+    for t in range(70):
+        for s, st in zip(servers, streams):
+            with torch.cuda.stream(st):
+                s.feed(t)
+                s.step()
+    torch.cuda.synchronize()
+    for other in servers[:2]:
+        for a, b in zip(other.state(), servers[2].state()):
+            assert torch.equal(bits_of(a), bits_of(b))
+
+
+@pytest.mark.parametrize("B,n_pages", [(40, 3000), (700, 20000), (1500, 9000), (300, 70000), (4200, 15000)])
+def test_a_captured_plan(B, n_pages):
+    """Pages and token map of every form as a graph, rows that change from replay to replay, against the eager calls."""
+    print(f"captured plan B={B} n_pages={n_pages}", flush=True)
+    rng = np.random.default_rng(B)
+    eager, graphed = (Books(B, 64, 8, n_pages) for _ in range(2))
+    rows, now, new = (torch.zeros(B, dtype=torch.int32, device="cuda") for _ in range(3))
+    maps = [torch.zeros(3 * B, 4, dtype=torch.int32, device="cuda") for _ in range(2)]
+    starts = [torch.zeros(B + 1, dtype=torch.int32, device="cuda") for _ in range(2)]
+
+    def plan(b, m, st):
+        thk.thk_paged_reserve(b.shape, b.pages, rows, now, b.held, b.table, b.refs, b.room, b.moves, b.ws)
+        thk.thk_token_map(b.shape, new, now, None, 64, 1, m, 3 * B, st)
+
+    for b, m, st in zip((eager, graphed), maps, starts):
+        plan(b, m, st)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        plan(graphed, maps[1], starts[1])
+    for _ in range(6):
+        now.copy_(torch.minimum(rows, eager.room))
+        rows.copy_(ints(rng.integers(0, 8 * 64 + 1, B)))
+        new.copy_(ints(rng.integers(0, 4, B)))
+        plan(eager, maps[0], starts[0])
+        g.replay()
+        torch.cuda.synchronize()
+        for name in ("held", "table", "refs", "room", "moves"):
+            assert torch.equal(getattr(eager, name), getattr(graphed, name)), name
+        assert torch.equal(*maps) and torch.equal(*starts)
+
+
 def test_two_graphs_may_share_a_workspace_and_streams_need_one_each():
     rng = np.random.default_rng(12)
     a, b = logits(rng, 2, 4, 30000, "bf16"), logits(rng, 2, 4, 20001, "bf16")
