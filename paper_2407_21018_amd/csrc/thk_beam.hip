@@ -223,10 +223,9 @@ struct Tile {
 // fraction (values beyond 2^20, and lanes that have seen nothing but -inf), the difference is taken first.  NaN and +inf make the sum NaN.
 constexpr float kLog2e = 0x1.715476p0f;
 __device__ __forceinline__ bool is_far(float at) { return !(fabsf(at) <= 0x1p20f); }
-__device__ __forceinline__ double relative(double sum, float at) {   // ... to the value itself
-  const float c = at * kLog2e;
-  return is_far(at) ? sum : sum * (double)__builtin_amdgcn_exp2f(-fmaf(at, kLog2e, -c));
-}
+// What the terms have more than those of exp(x - at), as a power of two's exponent.
+__device__ __forceinline__ float excess(float at) { return is_far(at) ? 0.f : fmaf(at, kLog2e, -(at * kLog2e)); }
+__device__ __forceinline__ double relative(double sum, float at) { return sum * (double)__builtin_amdgcn_exp2f(-excess(at)); }
 
 template <int DT>
 __global__ __launch_bounds__(kWaves * 64, DT == THK_F32 ? 3 : 4) void k_beam_pieces(BeamArgs a, int pieces, int tiles_each) {
@@ -266,7 +265,7 @@ __global__ __launch_bounds__(kWaves * 64, DT == THK_F32 ? 3 : 4) void k_beam_pie
     tile_best[wave][tile - first][lane] = most;
     if (__ballot(most > at + 8.f) != 0) {
       const float to = most > at + 8.f ? most : at;
-      if (to > at) sum = relative(sum, at) * exp((double)at - (double)to);
+      if (to > at) sum = relative(sum, at) * exp((double)at - (double)to) * (double)__builtin_amdgcn_exp2f(excess(to));
       at = to;
       c = at * kLog2e;
     }
