@@ -623,8 +623,8 @@ thk_status thk_paged_copy(const thk_shape *shape, const thk_pages *pages, const 
  *   score_out     [B][K]  (there: -inf); may be scores where K = W
  *   done_out      [B][K]  1 where the token is eos or the parent has ended (there: 0); may be NULL, and done where K = W
  * With K = 2 W a caller can set those that end aside and go on with the W best that do not.  Sums are fp32 in eights and 64
- * bits from there on; scores are 64 bits until they are written.  A score is off by at most 2^-23 (13 + 1.2 ln V) in front of its
- * rounding, the same for beams that are alike: continuations of different beams that are nearer than that may change places.
+ * bits from there on; scores are 64 bits until they are written.  A score is off by at most 2^-20, whatever V and whatever the logits have in
+ * common, in front of its rounding, the same for beams that are alike: continuations of different beams that are nearer than that may change places.
  *   ws : thk_beam_workspace_bytes() bytes.  Calls that may run at the same time need one each.
  */
 typedef struct {

@@ -137,7 +137,8 @@ __device__ __forceinline__ void join_step(double &x) {
   const u64 b = (u64)__double_as_longlong(x);
   x += __longlong_as_double((long long)((u64)lane_across<J>((uint32_t)(b >> 32)) << 32 | lane_across<J>((uint32_t)b)));
 }
-__device__ __forceinline__ void join_sums(float &at, double &sum) {
+// unit: the terms are exp(unit) larger than those of exp(x - at).
+__device__ __forceinline__ void join_sums(float &at, double &sum, double unit = 0) {
   float t = at;
   join_step<1>(t);
   join_step<2>(t);
@@ -146,7 +147,7 @@ __device__ __forceinline__ void join_sums(float &at, double &sum) {
   LanePair p = pair16(t);
   p = pair32(fmaxf(p.a, p.b));
   t = fmaxf(p.a, p.b);
-  sum = sum != 0 ? sum * exp((double)at - (double)t) : 0.0;
+  sum = sum != 0 ? sum * exp((double)at - (double)t - unit) : 0.0;
   join_step<1>(sum);
   join_step<2>(sum);
   join_step<4>(sum);
@@ -218,14 +219,18 @@ struct Tile {
   }
 };
 
-// The sum's exponents are relative to a value `at` of the lane, at most 8 below its largest element: sum of 2^(x L - c), L = log2 e in 32 bits
-// and c = at L, one rounding for an element, and what c's rounding leaves is made good when the sum is used.  Where that is no longer a
-// fraction (values beyond 2^20, and lanes that have seen nothing but -inf), the difference is taken first.  NaN and +inf make the sum NaN.
-constexpr float kLog2e = 0x1.715476p0f;
+// The sum's terms are 2^(x L - c), L = log2 e in 32 bits and c the whole number next to at L, for a value `at` of the lane that is at most
+// kAbove below its largest element: a change of `at` multiplies the sum by a power of two, which is exact.  A term's exponent is rounded once
+// (2^-24 (|x - at| + 0.35) of the term), L is off by 0.23 2^-24, 2^y by 2^-23, and three sums of 2^-24 follow before 64 bits.  The mean of
+// |x - at| under the terms' own weights is at most kAbove and the logarithm of a lane's 512 elements (the largest element's distance to the mean
+// is an entropy's part): 2^-24 (1.23 (2 + 6.3) + 5.4) = 2^-24 15.6.  Exponents in two parts, whole and rest, would leave half of that for four
+// more instructions an element (512 rows of 131072 bf16: 30 -> 34 us).  Where x L leaves no place for a fraction (values beyond 2^20, and
+// lanes that have seen nothing but -inf), x - at, which is exact for what counts, takes the place of x, and c is 0.  NaN and +inf make the sum NaN.
+constexpr float kLog2e = 0x1.715476p0f, kAbove = 2.f;
+constexpr double kLn2 = 0x1.62e42fefa39efp-1;
 __device__ __forceinline__ bool is_far(float at) { return !(fabsf(at) <= 0x1p20f); }
-// What the terms have more than those of exp(x - at), as a power of two's exponent.
-__device__ __forceinline__ float excess(float at) { return is_far(at) ? 0.f : fmaf(at, kLog2e, -(at * kLog2e)); }
-__device__ __forceinline__ double relative(double sum, float at) { return sum * (double)__builtin_amdgcn_exp2f(-excess(at)); }
+__device__ __forceinline__ float whole_of(float at) { return is_far(at) ? 0.f : rintf(at * kLog2e); }
+__device__ __forceinline__ double unit_of(float at) { return is_far(at) ? (double)at * (double)kLog2e : (double)whole_of(at); }   // terms are 2^(x L - this)
 
 template <int DT>
 __global__ __launch_bounds__(kWaves * 64, DT == THK_F32 ? 3 : 4) void k_beam_pieces(BeamArgs a, int pieces, int tiles_each) {
@@ -263,20 +268,20 @@ __global__ __launch_bounds__(kWaves * 64, DT == THK_F32 ? 3 : 4) void k_beam_pie
     most = larger(most, x[31], x[31]);
     best = larger(best, most, most);
     tile_best[wave][tile - first][lane] = most;
-    if (__ballot(most > at + 8.f) != 0) {
-      const float to = most > at + 8.f ? most : at;
-      if (to > at) sum = relative(sum, at) * exp((double)at - (double)to) * (double)__builtin_amdgcn_exp2f(excess(to));
+    if (__ballot(most - at > kAbove) != 0) {
+      const float to = most - at > kAbove ? most : at, c_to = whole_of(to);
+      if (sum != 0 && to > at && (is_far(at) || is_far(to))) sum *= exp2(unit_of(at) - unit_of(to));
+      else if (to > at) sum = ldexp(sum, (int)(c - c_to));
       at = to;
-      c = at * kLog2e;
+      c = c_to;
     }
     if (__ballot(is_far(at)) != 0) {
-      const float left = is_far(at) ? 0.f : fmaf(at, kLog2e, -c);
+      const float off = is_far(at) ? at : 0.f;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) x[i] = fmaf(x[i] - at, kLog2e, left);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 32; ++i) x[i] = fmaf(x[i], kLog2e, -c);
+      for (int i = 0; i < 32; ++i) x[i] -= off;
     }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = fmaf(x[i], kLog2e, -c);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       float p[8];
@@ -286,8 +291,7 @@ __global__ __launch_bounds__(kWaves * 64, DT == THK_F32 ? 3 : 4) void k_beam_pie
     }
   }
   lane_best[threadIdx.x] = best;
-  sum = relative(sum, at);
-  join_sums(at, sum);
+  join_sums(at, sum, kLn2 * ((double)at * (double)kLog2e - unit_of(at)));
   if (lane == 0) stats[wave] = {at, 0, sum};
   __syncthreads();
 

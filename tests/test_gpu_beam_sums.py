@@ -62,3 +62,41 @@ OFFSETS = {"bf16": [0.0, 3.0, 60.0, 100.0, -100.0, 240.0, -1000.0, 5000.0, -7000
 def test_the_reference_of_a_sum_changes(dtype, offset):
     print(f"beam sums {dtype} offset={offset}", flush=True)
     check_offset(dtype, offset, sum_error)
+
+
+# A term's exponent is rounded once: 2^-24 (|x - r| + 0.35) of the term, r at most 2 below the lane's largest element; log2 e in 32 bits is off by 0.23
+# 2^-24 of itself; 2^y is within 2^-23; three sums of 2^-24 lie before 64 bits.  Under the terms' own weights |x - r| is on average at most 2 and the
+# logarithm of the 512 elements that a lane has at most.
+SUM = (1.23 * (2 + math.log(512)) + 5.4) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype,offset", [(d, o) for d in OFFSETS for o in OFFSETS[d]])
+def test_a_sum_is_as_near_whatever_its_length_and_offset(dtype, offset):
+    print(f"beam sums {dtype} offset={offset}", flush=True)
+    check_offset(dtype, offset, lambda V: SUM)
+
+
+def check_scores(x, s, K):
+    """Every score within the bound; and the continuations themselves, for neighbours that are further apart than two of them can be off."""
+    parent, token, score, _ = O.beam_select(f64(x), s.astype(np.float64), np.zeros(s.shape, int), K + 1, -1)
+    near = (np.diff(score) != 0) & (np.abs(np.diff(score)) < 2 * SUM) & (parent[:, 1:] != parent[:, :-1])
+    assert not near.any(), "two beams' continuations are too near for a test"
+    got = gpu_select(x, s, None, K, -1)
+    assert np.array_equal(got[0], parent[:, :K]) and np.array_equal(got[1], token[:, :K])
+    assert (np.abs(got[2].astype(np.float64) - score[:, :K]) <= SUM + 2.0 ** -24 * np.abs(score[:, :K])).all()
+
+
+def test_random_scores_of_many_rows():
+    rng = np.random.default_rng(5)
+    x = torch.tensor(rng.standard_normal((300, 8, 3001)) * 2, dtype=torch.float32).bfloat16().cuda()
+    check_scores(x, (-10 * rng.random((300, 8))).astype(np.float32), 16)
+
+
+@pytest.mark.parametrize("V", [262144, 1 << 20, (1 << 22) + 3])
+def test_long_rows_whose_weight_lies_far_below_their_largest(V):
+    """One large element a lane and tile, the others so far below that both halves of the sum count: the sum's size is that of the scores' places."""
+    rng = np.random.default_rng(V)
+    x = torch.full((1, 2, V), -5.25, device="cuda") + torch.tensor(rng.random((1, 2, V)) / 8, dtype=torch.float32).cuda()
+    x[..., ::512] = 0.375
+    x[0, 1, ::7] -= 40
+    check_scores(x, np.array([[12.5, 12.0]], np.float32), 5)
