@@ -594,10 +594,11 @@ thk_status thk_rope_qkv(const thk_shape *shape, const thk_rope *rope, const uint
  * order, entries in order, as many as there are.  The result depends on the arguments' values alone.
  * now and moves (both or neither NULL): now [B] is the rows that a sequence has in its pages.  One that is to grow (rows > now > 0)
  * inside a page that holds some of them and that others use as well gets a page in its place, in front of its other new ones; where
- * all users of the page are such sequences the first of them keeps it.  moves [B][4] receives { from, to, tiles of 64 rows, 0 },
+ * all users of the page are such sequences the one with the most rows in it keeps it, of several the first: it writes behind the others' rows,
+ * which those for whom no page is left still read.  moves [B][4] receives { from, to, tiles of 64 rows, 0 },
  * or { -1, -1, 0, 0 }; thk_paged_copy, next in the stream, does what it says.  Where no page is left for that, room[b] is now[b]:
  * the sequence must not be written to.  (Shared pages behind the rows in use are not looked for: share pages that hold rows.)
- * Values outside a bound are clamped to it.  A sequence's entries are pages of the pool (others are given back to nobody) and differ.
+ * Values outside a bound are clamped to it.  B is at most 2^30.  A sequence's entries are pages of the pool (others are given back to nobody) and differ.
  *   ws : thk_workspace_bytes(shape, THK_OP_PAGED_RESERVE) bytes.
  */
 thk_status thk_paged_reserve(const thk_shape *shape, const thk_pages *pages, const int32_t *rows,

@@ -79,7 +79,10 @@ def reserve(rows, now, held, table, refs, page_rows):
             e = now[b] // page_rows
             if 0 < now[b] < rows[b] and now[b] % page_rows and e < held[b] and valid(table[b][e]):
                 users.setdefault(table[b][e], []).append(b)
-    moving = {b for p, u in users.items() for b in (u if len(u) < refs[p] else u[1:])}
+    moving = set()
+    for p, u in users.items():      # where all users of a page grow, the one with the most rows in it stays, the first of several
+        keeper = max(u, key=lambda b: (now[b] % page_rows, -b)) if len(u) >= refs[p] else None
+        moving |= {b for b in u if b != keeper}
     free = [p for p, r in enumerate(refs) if r <= 0]
     room, moves = [], []
     for b in range(B):

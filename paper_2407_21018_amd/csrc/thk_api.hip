@@ -927,7 +927,7 @@ size_t thk_workspace_bytes(const thk_shape *s, int32_t op) {
     case THK_OP_DECODE_PAGED:
       return check_paged_shape(s) == THK_OK && s->S <= INT32_MAX - kTile ? paged_ws_bytes(s, paged_most_pieces(s)) : 0;
     case THK_OP_PAGED_RESERVE:
-      return check_paged_shape(s) == THK_OK ? reserve_ws_bytes(s->B) : 0;
+      return check_paged_shape(s) == THK_OK && s->B <= kMostSequences ? reserve_ws_bytes(s->B) : 0;
     case THK_OP_SCORE_VALUE:
       if (s->S_obs < 1 || (int64_t)s->S_obs > s->S) return 0;
       return value_ws_bytes(s, value_split(s).n);
@@ -1522,6 +1522,7 @@ thk_status thk_paged_reserve(const thk_shape *s, const thk_pages *p, const int32
   if (st != THK_OK) return st;
   if (rows == nullptr || held == nullptr || table == nullptr || refs == nullptr || room == nullptr || (now == nullptr) != (moves == nullptr))
     return THK_ERR_NULL;
+  if (s->B > kMostSequences) return THK_ERR_SHAPE;
   if (!aligned4(rows) || !aligned4(now) || !aligned4(held) || !aligned4(table) || !aligned4(refs) || !aligned4(room) || !aligned16(moves))
     return THK_ERR_ALIGN;
   if (ws == nullptr || !aligned16(ws) || ws_bytes < reserve_ws_bytes(s->B)) return THK_ERR_WORKSPACE;

@@ -120,7 +120,6 @@ struct SequencePlan {
   int from;         // page that is to be replaced, -1: none
   int start;        // wishes of the sequences in front
 };
-constexpr int kOwner = -(1 << 30);   // + b: marks a page whose users all grow with the first of them
 
 __device__ __forceinline__ int held_of(const ReserveArgs &a, int b) { return min(max(a.held[b], 0), a.max_pages); }
 __device__ __forceinline__ int needed(const ReserveArgs &a, int b) {
@@ -134,6 +133,9 @@ __device__ __forceinline__ int growing_page(const ReserveArgs &a, int b, int hav
   const int p = a.table[(int64_t)b * a.max_pages + e];
   return p >= 0 && p < a.n_pages ? p : -1;
 }
+// Rows that a growing sequence has in that page, fewer than 2^16.  Of users that all grow the one with the most of them keeps the page, of several the
+// first: it writes behind them, so that those for whom no page is left, and who stay in it, keep their rows.
+__device__ __forceinline__ int rows_inside(const ReserveArgs &a, int b) { return a.now[b] & ((1 << a.page_shift) - 1); }
 // A wave gives back the entries [from, to) of sequence b.
 __device__ __forceinline__ void give_back(const ReserveArgs &a, int b, int from, int to, int lane) {
   int32_t *const row = a.table + (int64_t)b * a.max_pages;
@@ -156,8 +158,7 @@ __device__ __forceinline__ void grant(const ReserveArgs &a, int b, int64_t k, in
   a.table[(int64_t)b * a.max_pages + e] = p;
   refs_set(a.refs, p, 1);
   if (nth < 0) {
-    const int rows = a.now[b] & ((1 << a.page_shift) - 1);
-    *(i32x4 *)(a.moves + (int64_t)b * 4) = i32x4{from, p, (rows + kTile - 1) / kTile, 0};
+    *(i32x4 *)(a.moves + (int64_t)b * 4) = i32x4{from, p, (rows_inside(a, b) + kTile - 1) / kTile, 0};
     refs_add(a.refs, from, -1);
   }
 }
@@ -255,21 +256,25 @@ __device__ __forceinline__ int64_t plan_sequences(const ReserveArgs &a, PlanLds<
       users[i] = from[i] >= 0 ? refs_at(a.refs, from[i]) : 0;
     }
     __syncthreads();
-    bool all[EACH];   // all users of the page grow: the first of them keeps it
+    bool all[EACH];   // all users of the page grow: one of them keeps it
 #pragma unroll
     for (int i = 0; i < EACH; ++i) all[i] = slot[i] >= 0 && m.count[slot[i]] >= users[i];
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < EACH; ++i)
-      if (all[i]) m.count[slot[i]] = INT32_MAX;
+      if (all[i]) m.count[slot[i]] = 0;
+    __syncthreads();
+    int rank[EACH];   // by its rows, then backwards by its number
+    static_assert(EACH * THREADS <= 1 << 12 && kMostTilesOfPage * kTile <= 1 << 16);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      rank[i] = all[i] ? rows_inside(a, i * THREADS + tid) << 12 | ((1 << 12) - 1 - (i * THREADS + tid)) : 0;
+      if (all[i]) atomicMax(&m.count[slot[i]], rank[i]);
+    }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < EACH; ++i)
-      if (all[i]) atomicMin(&m.count[slot[i]], i * THREADS + tid);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < EACH; ++i)
-      if (all[i] && m.count[slot[i]] == i * THREADS + tid) from[i] = -1;
+      if (all[i] && m.count[slot[i]] == rank[i]) from[i] = -1;
   }
   int64_t wanted = 0;
 #pragma unroll
@@ -522,30 +527,26 @@ __global__ __launch_bounds__(kPlanThreads) void k_reserve_many(ReserveArgs a) {
     phase_end();
   }
   // Pages that several use and at least one of them is to write: the growing users take themselves off the page's count, and where
-  // nobody is left the first of them marks it as his.
+  // nobody is left they mark it, by the most rows first and then by the first sequence that has so many.  The marks lie below
+  // one another, and below all counts.  (start: the sequence is still in question.)
   if (a.now != nullptr) {
-    for (int b = tid; b < a.B; b += kPlanThreads)
-      if (plan[b].from >= 0) refs_add(a.refs, plan[b].from, -1);
-    phase_end();
-    for (int b = tid; b < a.B; b += kPlanThreads)
-      if (plan[b].from >= 0 && refs_at(a.refs, plan[b].from) <= 0) __hip_atomic_fetch_min(a.refs + plan[b].from, kOwner + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    phase_end();
-    for (int b = tid; b < a.B; b += kPlanThreads)
-      if (plan[b].from >= 0 && refs_at(a.refs, plan[b].from) == kOwner + b) plan[b].from = -2 - plan[b].from;
-    phase_end();
-    for (int b = tid; b < a.B; b += kPlanThreads)
-      if (plan[b].from < -1) {
-        refs_set(a.refs, -2 - plan[b].from, 0);
-        plan[b].from = -2 - plan[b].from;
-        plan[b].start = 1;
-      }
-    phase_end();
-    for (int b = tid; b < a.B; b += kPlanThreads)   // the counts as they were
-      if (plan[b].from >= 0) {
-        refs_add(a.refs, plan[b].from, 1);
-        if (plan[b].start != 0) plan[b].from = -1;
-      }
-    phase_end();
+    constexpr int kMostRows = -(1 << 29), kFirst = INT32_MIN;   // less the rows; plus the sequence's number, which is below 2^30
+    auto mark = [&](int p, int x) { __hip_atomic_fetch_min(a.refs + p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+    auto each = [&](auto f) {
+      for (int b = tid; b < a.B; b += kPlanThreads)
+        if (plan[b].from >= 0) f(b, plan[b]);
+      phase_end();
+    };
+    each([&](int, SequencePlan &s) { refs_add(a.refs, s.from, -1); });
+    each([&](int b, SequencePlan &s) { if (refs_at(a.refs, s.from) <= 0) mark(s.from, kMostRows - rows_inside(a, b)); });
+    each([&](int b, SequencePlan &s) { s.start = refs_at(a.refs, s.from) == kMostRows - rows_inside(a, b); });
+    each([&](int b, SequencePlan &s) { if (s.start != 0) mark(s.from, kFirst + b); });
+    each([&](int b, SequencePlan &s) { s.start = refs_at(a.refs, s.from) == kFirst + b; });
+    each([&](int, SequencePlan &s) { if (s.start != 0) refs_set(a.refs, s.from, 0); });
+    each([&](int, SequencePlan &s) {   // the counts as they were
+      refs_add(a.refs, s.from, 1);
+      if (s.start != 0) s.from = -1;
+    });
   }
   int64_t wanted = 0;
   for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {

@@ -37,6 +37,7 @@ struct ReserveArgs {
   int64_t n_pages;
   int32_t B, max_pages, page_shift;     // page_shift: log2 of a page's rows
 };
+constexpr int kMostSequences = 1 << 30;   // of one call
 size_t reserve_ws_bytes(int64_t B);
 hipError_t launch_reserve(const ReserveArgs &a, hipStream_t st);
 
