@@ -545,7 +545,7 @@ thk_status thk_token_map(const thk_shape *shape, const int32_t *n_new, const int
  *   THK_ROPE_BASE    w_i of the base  base * factor^(rot / (rot - 2))
  *   THK_ROPE_RAMP    w_i (1 - g_i) + w_i / factor g_i,  g_i = (i - lo) / (hi - lo) in [0, 1] (0.001 for hi = lo), with at(t) the index of the pair that
  *                    turns t times over `trained` positions, rot ln(trained / (2 pi t)) / (2 ln base): lo = floor(at(high)), at least
- *                    0, hi = ceil(at(low)), at most rot - 1; the gain is 0.1 ln(factor) + 1 unless given  (arXiv 2309.00071)
+ *                    0, hi = ceil(at(low)), at most rot - 1; the gain is 0.1 ln(factor) + 1, of factors below 1 it is 1, unless given  (arXiv 2309.00071)
  *   THK_ROPE_BANDS   w_i / factor (1 - g_i) + w_i g_i,  g_i = (r_i - low) / (high - low) in [0, 1], r_i = trained w_i / (2 pi)
  * thk_rope_turns (host only) writes the rot / 2 speeds, as 2^64ths of a turn per position, to HOST memory; the caller keeps them on
  * the device.  With them an angle is a product of whole numbers in which full turns fall away: as exact at position 2^31 as at 1.

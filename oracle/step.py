@@ -22,7 +22,7 @@ def speeds(rot, scaling, base, factor=1.0, trained=0, low=0.0, high=0.0):
         at = [rot * math.log(trained / (t * 2 * math.pi)) / (2 * math.log(base)) for t in (high, low)]
         lo, hi = max(math.floor(at[0]), 0), min(math.ceil(at[1]), rot - 1)
         g = np.clip((np.arange(half) - lo) / max(hi - lo, 0.001), 0, 1)
-        w, gain = w / factor * g + w * (1 - g), 0.1 * math.log(factor) + 1
+        w, gain = w / factor * g + w * (1 - g), 0.1 * math.log(max(factor, 1.0)) + 1
     if scaling == "bands":
         g = np.clip((trained * w / (2 * math.pi) - low) / (high - low), 0, 1)
         w = w / factor * (1 - g) + w * g

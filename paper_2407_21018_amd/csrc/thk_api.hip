@@ -812,7 +812,7 @@ thk_status check_rope(const thk_rope *r) {
   if (r->scaling >= THK_ROPE_RAMP && (r->trained < 1 || !(r->low > 0) || !(r->high > r->low) || !isfinite(r->high))) return THK_ERR_SHAPE;
   return THK_OK;
 }
-double rope_gain(const thk_rope *r) { return r->gain != 0 ? r->gain : r->scaling == THK_ROPE_RAMP ? 0.1 * log(r->factor) + 1 : 1; }
+double rope_gain(const thk_rope *r) { return r->gain != 0 ? r->gain : r->scaling == THK_ROPE_RAMP && r->factor > 1 ? 0.1 * log(r->factor) + 1 : 1; }
 
 thk_status check_beams(const thk_beams *b) {
   if (b == nullptr) return THK_ERR_NULL;
