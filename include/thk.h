@@ -549,7 +549,7 @@ thk_status thk_token_map(const thk_shape *shape, const int32_t *n_new, const int
  *   THK_ROPE_BANDS   w_i / factor (1 - g_i) + w_i g_i,  g_i = (r_i - low) / (high - low) in [0, 1], r_i = trained w_i / (2 pi)
  * thk_rope_turns (host only) writes the rot / 2 speeds, as 2^64ths of a turn per position, to HOST memory; the caller keeps them on
  * the device.  With them an angle is a product of whole numbers in which full turns fall away: as exact at position 2^31 as at 1.
- * Sines and cosines are within 2^-22 of the true ones; the sum of products is fp32 and rounded once to the element type.
+ * Sines and cosines are within 2^-24 of the true ones; the sum of products is fp32 and rounded once to the element type.
  * A negative position turns back, by the same gain: the gradient of the inputs from that of the outputs.
  */
 typedef enum { THK_ROPE_HALVES = 0, THK_ROPE_PAIRS = 1 } thk_rope_layout;

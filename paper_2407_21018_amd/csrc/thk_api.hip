@@ -1510,7 +1510,7 @@ thk_status thk_rope_qkv(const thk_shape *s, const thk_rope *r, const uint64_t *t
   int64_t all = 0;
   if (__builtin_mul_overflow((int64_t)s->L * n_tokens, rows, &all) || all > (int64_t)1 << 27 || rows > 1 << 20) return THK_ERR_SHAPE;
   a.rows = (int32_t)rows;
-  a.gain = (float)rope_gain(r);
+  a.gain = rope_gain(r);
   if (n_tokens == 0) return THK_OK;
   return failed(launch_rope(s->dtype, a, (hipStream_t)stream)) ? THK_ERR_HIP : THK_OK;
 }

@@ -26,7 +26,7 @@ struct RopeArgs {
   int64_t n, ld_q, ld_k, ld_v, cap;     // n: tokens of a layer
   int32_t L, B, N_q, N_kv, q_rows, rot, layout;
   int32_t rows;                         // rows (of 128 channels) per token: those of the inputs that are there
-  float gain;
+  double gain;
 };
 hipError_t launch_rope(int dtype, const RopeArgs &a, hipStream_t st);
 

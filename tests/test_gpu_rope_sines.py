@@ -38,3 +38,17 @@ def test_the_ramp_has_a_gain_of_its_own_from_factor_1_on(factor, want):
         cos, sin = turned_ones(r, np.zeros(3, np.int64))
         assert (cos == np.float32(given or want)).all() and (sin == 0).all()
     assert O.speeds(D, "ramp", 10000.0, factor, 4096, 1.0, 32.0)[1] == want
+
+
+@pytest.mark.parametrize("gain", [0.0, 1.75])
+def test_sines_and_cosines_are_rounded_once(gain):
+    """Half a step of the type below 1 is 2^-25; the angle is known to 2^-33 of a turn, 2^-30.3 radians, and the series to 2^-33: together less than
+    2^-30.  Positions over the whole range of 32 bits, the test's angles from whole numbers."""
+    pos = np.concatenate([np.arange(-200, 4000), [2 ** 31 - 1, -2 ** 31, 2 ** 30, -2 ** 30], np.random.default_rng(7).integers(-2 ** 31, 2 ** 31, 4000)]).astype(np.int64)
+    r = Turn(base=500000.0, gain=gain)
+    cos, sin = turned_ones(r, pos)
+    at = np.array([[((int(p) * t) % 2 ** 64) / 2.0 ** 64 for t in r.turns.tolist()] for p in pos]) * 2 * math.pi
+    g = gain or 1.0
+    for got, want in ((cos, g * np.cos(at)), (sin, g * np.sin(at))):
+        step = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(want), 2.0 ** -20))) - 24)      # half a step at the value
+        assert (np.abs(got - want) <= step * (1 + 2.0 ** -6) + g * 2.0 ** -30).all()
