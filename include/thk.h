@@ -587,8 +587,8 @@ thk_status thk_rope_qkv(const thk_shape *shape, const thk_rope *rope, const uint
  *   rows  [B]   rows that each sequence has to have pages for (0: none, its pages are given back)
  *   held  [B]   in/out: pages that it holds, the first entries of its row of the table
  *   table [B][max_pages]  in/out: entries given back become -1
- *   refs  [n_pages]  in/out: users of each page; a page without any (0 or less) is free.  A caller that shares pages counts them
- *               here, and pages it keeps for itself.
+ *   refs  [n_pages]  in/out: users of each page; a page without any (0 or less) is free, and its count stays as it is until
+ *               the page is given out.  A caller that shares pages counts them here, and pages it keeps for itself.
  *   room  [B]   out: rows that the sequence now has pages for; less than rows[b] where the pool has run out
  * Pages past ceil(rows / page_rows) are given back first; then pages are given out, the lowest free numbers first, to sequences in
  * order, entries in order, as many as there are.  The result depends on the arguments' values alone.

@@ -81,3 +81,19 @@ def test_more_sequences_than_there_are_marks_are_refused():
         status.append(e.value.status)
     assert status == [2, 2]      # THK_ERR_SHAPE
     assert thk.thk_workspace_bytes(thk.make_shape(1, 1 << 30, 1, 1, 128, 64, 1, 1), thk.THK_OP_PAGED_RESERVE) > 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,n_pages", [(1, 3), (60, 500), (60, 9000), (900, 3000), (900, 60000), (2000, 9000), (4100, 9000)])
+def test_free_pages_with_negative_counts(B, n_pages):
+    """They are free as those with none are, and the count of one that nobody gets stays what it was."""
+    print(f"negative counts B={B} n_pages={n_pages}", flush=True)
+    rng = np.random.default_rng(n_pages)
+    refs = rng.choice([0, -1, -2, -1000, 1, 3], n_pages)
+    books = Books(B, 128, 3, n_pages, refs=refs)
+    rows = rng.integers(0, 200, B)
+    books.reserve(rows)
+    books.reserve(rows + rng.integers(0, 100, B), rows)
+    books.reserve([0] * B)
+    after = books.refs.cpu().numpy()
+    assert (after[refs > 0] == refs[refs > 0]).all() and ((after == refs) | (after == 0)).all()
