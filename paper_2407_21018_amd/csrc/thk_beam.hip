@@ -16,7 +16,7 @@ typedef unsigned long long u64;
 // largest says what is certainly not among the K best, and the lanes' tiles that have something above it, little more than K of them, are looked at
 // again, element by element, for the piece's list.  A second launch joins the pieces of a prompt's rows.  Memory bounds the pass over large calls (512
 // rows of 131072 bf16: 27 of the launch's 30 us for 134 MB, 25 without the exponentials), latency the rest: the list takes a block 3 us, the
-// join 4 to 6.  An element is a key: its
+// join 4 to 6 for up to eight beams.  An element is a key: its
 // value in the order of unsigned numbers, above the complement of its index, so that of equal values the first is the larger key; 0
 // is no element.
 constexpr int kWaves = 4;
@@ -25,7 +25,7 @@ constexpr int kMostTiles = 16;       // of a wave
 constexpr int kLooks = 4;
 constexpr float kLeast = -3.402823466e38f;   // the lowest finite value
 
-struct PieceStats { float at; uint32_t none; double sum; };   // sum of exp(x - at)
+struct PieceStats { float at; double sum; };   // sum of exp(x - at)
 
 __device__ __forceinline__ u64 key_of(float x, uint32_t at) {
   const uint32_t b = __float_as_uint(x + 0.f);   // -0 is 0
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(kWaves * 64, DT == THK_F32 ? 3 : 4) void k_beam_pie
   }
   lane_best[threadIdx.x] = best;
   join_sums(at, sum, kLn2 * ((double)at * (double)kLog2e - unit_of(at)));
-  if (lane == 0) stats[wave] = {at, 0, sum};
+  if (lane == 0) stats[wave] = {at, sum};
   __syncthreads();
 
   // the list
@@ -339,7 +339,7 @@ __global__ __launch_bounds__(kWaves * 64, DT == THK_F32 ? 3 : 4) void k_beam_pie
   }
   __syncthreads();
   if (wave == 1) {
-    PieceStats s = lane < kWaves ? stats[lane] : PieceStats{kLeast, 0, 0.0};
+    PieceStats s = lane < kWaves ? stats[lane] : PieceStats{kLeast, 0.0};
     join_sums(s.at, s.sum);
     if (lane == 0) ((PieceStats *)a.ws)[blockIdx.x] = s;
   }
@@ -352,8 +352,10 @@ __global__ __launch_bounds__(kWaves * 64, DT == THK_F32 ? 3 : 4) void k_beam_pie
 }
 
 
-// A block of eight waves, or sixteen where that spares them rows (32 beams, the best 64 of 149134 tokens: 51 -> 41 us), joins a prompt: a wave for
-// each row joins its pieces' lists and sums, then the rows' candidates are ranked by counting.
+// A block of eight waves, or sixteen where that spares them rows (32 beams, the best 64 of 149134 tokens: 51 -> 41 us for the call of then), joins a
+// prompt: a wave for each row joins its pieces' lists and sums, then the rows' candidates are ranked by counting.  Pieces and join: one prompt of 32 beams,
+// the best 64 of 149134 bf16, 12.3 + 20.2 us, four prompts 17.3 + 15.9 (fp32: 13.0 + 20.0, 21.5 + 15.8); 16 beams, the best 32, 8.2 + 8.9 and
+// 10.6 + 7.6; 8 beams, the best 16, 7.2 + 5.6 and 8.3 + 5.9.  One block sorts and ranks for a prompt, which bounds the long lists of many beams.
 constexpr int join_waves(int W) { return W <= 8 ? 8 : 16; }
 template <int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void k_beam_join(BeamArgs a, int pieces) {
@@ -377,7 +379,7 @@ __global__ __launch_bounds__(WAVES * 64) void k_beam_join(BeamArgs a, int pieces
     // (asked for before it is known whether they are there)
     const u64 *const keys = (const u64 *)(stats + (int64_t)a.B * a.W * pieces) + row * count;
     u64 more = lane < count ? keys[lane] : 0;
-    PieceStats x = lane < pieces ? stats[row * pieces + lane] : PieceStats{kLeast, 0, 0.0};
+    PieceStats x = lane < pieces ? stats[row * pieces + lane] : PieceStats{kLeast, 0.0};
     double s = -INFINITY;
     int token = 0;
     if (!(fabsf(before) < INFINITY)) {
@@ -472,7 +474,8 @@ __global__ __launch_bounds__(WAVES * 64) void k_beam_join(BeamArgs a, int pieces
 // ---- caches that follow -------------------------------------------------------------------
 // A thread has one place of 16 bytes in the keys' (or values') tails of all beams of a prompt: it reads the parents' before it writes any, so
 // that beams may go on from each other in place.  (Parents and row counts are the same for a block: they go through the scalar unit.)  Memory bounds it:
-// 64 beams of 8 layers and 8 heads, 190 MB read and written, 36 us, 5.2 TB/s.
+// 64 beams of 8 layers and 8 heads, 190 MB read and written, 36 us, 5.2 TB/s, for prompts of 8 beams; of 16 beams 48 us, of 32 47 (five and three
+// waves a SIMD instead of eight, for a thread's W places).
 template <int DT, int W>
 __global__ __launch_bounds__(256) void k_reorder_tails(ReorderArgs a, int blocks) {
   constexpr int CPR = kD * Elem<DT>::EB / 16;
@@ -519,7 +522,8 @@ __global__ __launch_bounds__(256) void k_reorder_tails(ReorderArgs a, int blocks
   }
 }
 
-// A prompt's table rows and counts, likewise: a thread has one entry of all beams.  Latency: two trips, 3.1 us for 4 beams, 5.0 for 8 of 16 pages.
+// A prompt's table rows and counts, likewise: a thread has one entry of all beams.  Latency: two trips, 3.1 us for 4 beams, 5.0 for 8 of 16 pages; 7.6 for 16, 12.3
+// for 32, each entry's loads and stores by one thread.
 template <int W>
 __global__ __launch_bounds__(256) void k_reorder_pages(ReorderArgs a) {
   __shared__ int from[W], mine[W], keep[W], old_held[W], old_pages[W], old_tail[W], most;

@@ -1,5 +1,5 @@
 // Rotary positions: queries, keys and values of new tokens to where attention and the caches read them.  Memory bounds it: every row
-// is read once and written once (16384 tokens of 64 + 16 heads, bf16: 671 MB in 115 us, 5.8 TB/s); small calls a launch and two trips (one token: 2.8 us).
+// is read once and written once (16384 tokens of 64 + 16 heads, bf16: 671 MB in 115 us, 5.8 TB/s); small calls a launch and two trips (one token: 3.0 us).
 #include "thk_step.h"
 
 #include <algorithm>
